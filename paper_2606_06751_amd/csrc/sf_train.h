@@ -1,0 +1,59 @@
+// sf_train.h -- element types and small device helpers shared by the kernels
+// of stagefrontier_train.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "stagefrontier_train.h"
+
+namespace sfk {
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<SF_F32> {
+    typedef float T;
+};
+template <>
+struct Elem<SF_BF16> {
+    typedef __bf16 T;
+};
+template <>
+struct Elem<SF_F16> {
+    typedef _Float16 T;
+};
+
+// Elements of 16 bytes, and such a vector at element alignment (gfx950 loads
+// and stores 16 bytes at any address).
+template <int DT>
+constexpr int kVec = 16 / (int)sizeof(typename Elem<DT>::T);
+template <int DT>
+using VecU = typename Elem<DT>::T __attribute__((ext_vector_type(kVec<DT>), aligned(sizeof(typename Elem<DT>::T))));
+template <int DT>
+using VecF = float __attribute__((ext_vector_type(kVec<DT>)));
+
+static inline int elem_size(int dtype) { return dtype == SF_F32 ? 4 : 2; }
+
+// Elements from p up to the next 16-byte boundary, at most n.
+template <int DT>
+__device__ __forceinline__ int64_t head_elems(const void* p, int64_t n)
+{
+    const int64_t h = (int64_t)((0 - (uintptr_t)p) & 15) / (int64_t)sizeof(typename Elem<DT>::T);
+    return h < n ? h : n;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kF32Max = 3.402823466e38f;
+
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ double wave_sum_f64(double v)
+{
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+}  // namespace sfk

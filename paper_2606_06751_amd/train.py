@@ -1,0 +1,324 @@
+"""Python binding of libstagefrontier's second header (ctypes; argument
+marshalling only): the numbers that a training step itself yields.
+
+Every function has the name of the C entry point it wraps (declared in
+``include/stagefrontier_train.h``).  As in ``stagefrontier``, arrays are torch
+tensors on the GPU, outputs and workspaces that are not given are allocated on
+the call's stream, and every step of the computation runs in the library's HIP
+kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .stagefrontier import (SF_EINVAL, SF_EHIP, SF_ERANGE, SF_MAX_R, SF_OK, StageFrontierError,  # noqa: F401
+                            _check, _lib, _new, _stream_handle)
+
+SF_F32, SF_BF16, SF_F16 = 0, 1, 2
+SF_MEAN_TOKENS, SF_MEAN_SEQUENCES, SF_SUM_TOKENS = 0, 1, 2
+
+_DTYPES = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16}
+
+
+def _declare(lib):
+    i64, i32, f32, vp, ci = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_int
+    for name, res, args in (
+            ("sf_token_logp", ci, [vp, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp, i64, vp]),
+            ("sf_token_logp_workspace", i64, [i64, i64]),
+            ("sf_token_logp_grad", ci, [vp, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]),
+            ("sf_policy_loss", ci, [vp, vp, vp, vp, i32, vp, vp, i64, i64, i32, f32, f32, f32, f32, vp, vp, vp,
+                                    i64, vp]),
+            ("sf_policy_loss_workspace", i64, [i64, i64]),
+            ("sf_grad_list_bytes", i64, [i32]),
+            ("sf_grad_list_init", ci, [vp, i64, vp, vp, vp, i32]),
+            ("sf_grad_norm", ci, [vp, vp, vp, vp, vp, i64, vp]),
+            ("sf_grad_norm_workspace", i64, [vp]),
+            ("sf_grad_clip", ci, [vp, vp, vp, i64, f32, f32, vp, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
+
+
+_declare(_lib)
+
+
+def sf_token_logp_workspace(N: int, V: int) -> int:
+    return int(_lib.sf_token_logp_workspace(N, V))
+
+
+def sf_policy_loss_workspace(N: int, B: int) -> int:
+    return int(_lib.sf_policy_loss_workspace(N, B))
+
+
+def _space(workspace, need: int, where: str, like: torch.Tensor, stream):
+    """The call's workspace: the caller's uint8 tensor, or a new one."""
+    if need < 0:
+        raise StageFrontierError(SF_EINVAL, where)
+    if workspace is None:
+        return _new((need,), torch.uint8, like.device, stream)
+    _check(workspace, "workspace", torch.uint8, workspace.shape, like)
+    if workspace.numel() < need:
+        raise ValueError("workspace has %d bytes, %d are needed" % (workspace.numel(), need))
+    return workspace
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Checks a matrix of logits and returns its row stride."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
+        raise TypeError("%s must be a float32, bfloat16 or float16 torch.Tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError("%s must be [N, V] with V >= 1" % name)
+    N, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have its rows' entries next to each other" % name)
+    if N > 1 and t.stride(0) < V:
+        raise ValueError("%s must have rows that do not overlap" % name)
+    return t.stride(0) if N > 1 else V
+
+
+def sf_token_logp(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: float = 1.0, entropy: bool = True,
+                  out_logp: torch.Tensor | None = None, out_lse: torch.Tensor | None = None,
+                  out_entropy: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Log-probability of the taken token, normaliser and entropy of each row
+    of logits (``sf_token_logp``).
+
+    ``logits`` [N, V] float32, bfloat16 or float16, rows any distance apart;
+    ``targets`` [N] int64, a row whose target lies outside [0, V) takes no
+    part.  Returns ``(out_logp, out_lse, out_entropy)``, [N] float32 each;
+    ``out_entropy`` is None with ``entropy=False``.
+    """
+    stride = _rows(logits, "logits")
+    N, V = logits.shape
+    dev = logits.device
+    _check(targets, "targets", torch.int64, (N,), logits)
+    if out_logp is None:
+        out_logp = _new((N,), torch.float32, dev, stream)
+    if out_lse is None:
+        out_lse = _new((N,), torch.float32, dev, stream)
+    if out_entropy is None and entropy:
+        out_entropy = _new((N,), torch.float32, dev, stream)
+    _check(out_logp, "out_logp", torch.float32, (N,), logits)
+    _check(out_lse, "out_lse", torch.float32, (N,), logits)
+    if out_entropy is not None:
+        _check(out_entropy, "out_entropy", torch.float32, (N,), logits)
+    need = _lib.sf_token_logp_workspace(N, V)
+    if need != 0:
+        workspace = _space(workspace, need, "sf_token_logp", logits, stream)
+    rc = _lib.sf_token_logp(logits.data_ptr(), _DTYPES[logits.dtype], N, V, stride, targets.data_ptr(),
+                            inv_temperature, out_logp.data_ptr(), out_lse.data_ptr(),
+                            None if out_entropy is None else out_entropy.data_ptr(),
+                            None if need == 0 else workspace.data_ptr(), need, _stream_handle(stream, dev))
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_token_logp")
+    return out_logp, out_lse, out_entropy
+
+
+def sf_token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_logp: torch.Tensor,
+                       entropy: torch.Tensor | None = None, grad_entropy: torch.Tensor | None = None,
+                       inv_temperature: float = 1.0, out_grad: torch.Tensor | None = None, stream=None):
+    """Gradient of ``sf_token_logp``'s outputs back to the logits
+    (``sf_token_logp_grad``).
+
+    ``grad_logp`` and ``grad_entropy`` [N] float32 are the loss's gradients;
+    ``entropy`` is needed with the second.  ``out_grad`` [N, V] of the logits'
+    type may be the logits themselves.  Returns ``out_grad``.
+    """
+    stride = _rows(logits, "logits")
+    N, V = logits.shape
+    dev = logits.device
+    _check(targets, "targets", torch.int64, (N,), logits)
+    _check(lse, "lse", torch.float32, (N,), logits)
+    _check(grad_logp, "grad_logp", torch.float32, (N,), logits)
+    if grad_entropy is not None:
+        _check(grad_entropy, "grad_entropy", torch.float32, (N,), logits)
+        if entropy is None:
+            raise ValueError("entropy is needed with grad_entropy")
+    if entropy is not None:
+        _check(entropy, "entropy", torch.float32, (N,), logits)
+    if out_grad is None:
+        out_grad = _new((N, V), logits.dtype, dev, stream)
+    out_stride = _rows(out_grad, "out_grad")
+    if out_grad.dtype is not logits.dtype or out_grad.shape != logits.shape or out_grad.device != dev:
+        raise ValueError("out_grad must have the logits' type, shape and device")
+    rc = _lib.sf_token_logp_grad(logits.data_ptr(), _DTYPES[logits.dtype], N, V, stride, targets.data_ptr(),
+                                 inv_temperature, lse.data_ptr(), grad_logp.data_ptr(),
+                                 None if entropy is None else entropy.data_ptr(),
+                                 None if grad_entropy is None else grad_entropy.data_ptr(), out_grad.data_ptr(),
+                                 out_stride, _stream_handle(stream, dev))
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_token_logp_grad")
+    return out_grad
+
+
+def sf_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor, seq_start: torch.Tensor,
+                   ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                   advantage_per_token: bool = False, reduction: int = SF_MEAN_TOKENS, scale: float = 1.0,
+                   clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                   out_terms: torch.Tensor | None = None, out_grad: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None):
+    """Clipped policy loss with a KL term over ragged sequences, and its
+    gradient (``sf_policy_loss``).
+
+    ``logp``, ``old_logp``, ``ref_logp`` [N] float32; ``advantage`` [B], or [N]
+    with ``advantage_per_token``; ``mask`` [N] uint8 or bool; ``seq_start``
+    [B + 1] int64.  Returns ``(out_terms [4], out_grad [N])``: loss, policy
+    term, KL and clipped share, and the gradient of the loss.
+    """
+    if logp.dim() != 1 or seq_start.dim() != 1 or seq_start.shape[0] < 1:
+        raise ValueError("logp must be [N] and seq_start [B + 1]")
+    N, B = logp.shape[0], seq_start.shape[0] - 1
+    f32 = torch.float32
+    _check(logp, "logp", f32, (N,))
+    _check(old_logp, "old_logp", f32, (N,), logp)
+    _check(advantage, "advantage", f32, (N if advantage_per_token else B,), logp)
+    _check(seq_start, "seq_start", torch.int64, (B + 1,), logp)
+    if ref_logp is not None:
+        _check(ref_logp, "ref_logp", f32, (N,), logp)
+    if mask is not None:
+        _check(mask, "mask", torch.bool if mask.dtype is torch.bool else torch.uint8, (N,), logp)
+    dev = logp.device
+    if out_terms is None:
+        out_terms = _new((4,), f32, dev, stream)
+    if out_grad is None:
+        out_grad = _new((N,), f32, dev, stream)
+    _check(out_terms, "out_terms", f32, (4,), logp)
+    _check(out_grad, "out_grad", f32, (N,), logp)
+    need = _lib.sf_policy_loss_workspace(N, B)
+    workspace = _space(workspace, need, "sf_policy_loss", logp, stream)
+    rc = _lib.sf_policy_loss(logp.data_ptr(), old_logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(),
+                             advantage.data_ptr(), bool(advantage_per_token),
+                             None if mask is None else mask.data_ptr(), seq_start.data_ptr(), N, B, reduction, scale,
+                             clip_low, clip_high, kl_coef, out_terms.data_ptr(), out_grad.data_ptr(),
+                             workspace.data_ptr(), need, _stream_handle(stream, dev))
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_policy_loss")
+    return out_terms, out_grad
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the entries fill one piece of memory, in any order of dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+class GradSet:
+    """A list of gradient tensors laid out for ``sf_grad_norm`` and
+    ``sf_grad_clip`` (``sf_grad_list_init``), checked once.
+
+    Tensors are dense float32, bfloat16 or float16 ones on one GPU, mixed as
+    they come.  The set keeps them: it stands for these tensors, so a program
+    that gives its parameters new gradient tensors makes a new set of them.
+    """
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        self.device = None
+        for k, t in enumerate(self.tensors):
+            if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
+                raise TypeError("gradient %d must be a float32, bfloat16 or float16 torch.Tensor" % k)
+            if not t.is_cuda:
+                raise ValueError("gradient %d must be a GPU tensor" % k)
+            if self.device is None:
+                self.device = t.device
+            if t.device != self.device:
+                raise ValueError("gradient %d is on %s, the others on %s" % (k, t.device, self.device))
+            if not _dense(t):
+                raise ValueError("gradient %d must fill its memory without gaps" % k)
+        size = _lib.sf_grad_list_bytes(n)
+        if size < 0:
+            raise StageFrontierError(SF_EINVAL, "sf_grad_list_init")
+        self._list = (ctypes.c_int64 * ((size + 7) // 8))()
+        ptrs = (ctypes.c_void_p * n)(*(t.data_ptr() for t in self.tensors))
+        numel = (ctypes.c_int64 * n)(*(t.numel() for t in self.tensors))
+        dtype = (ctypes.c_int32 * n)(*(_DTYPES[t.dtype] for t in self.tensors))
+        rc = _lib.sf_grad_list_init(self._list, size, ptrs, numel, dtype, n)
+        if rc != SF_OK:
+            raise StageFrontierError(rc, "sf_grad_list_init")
+        self._order = [None if t.is_contiguous() else t.stride() for t in self.tensors]
+        self.workspace_bytes = int(_lib.sf_grad_norm_workspace(self._list))
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def sf_grad_norm_workspace(grads) -> int:
+    return (grads if isinstance(grads, GradSet) else GradSet(grads)).workspace_bytes
+
+
+def sf_grad_norm(grads, out_norms: torch.Tensor | None = None, out_total: torch.Tensor | None = None,
+                 out_nonfinite: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """L2 norms of gradients and their counts of entries that are not finite
+    (``sf_grad_norm``).
+
+    ``grads``: a ``GradSet``, or tensors to make one of for this call.  Returns
+    ``(out_norms [n] float32, out_total [1] float32, out_nonfinite [n] int64)``.
+    """
+    if not isinstance(grads, GradSet):
+        grads = GradSet(grads)
+    n = len(grads)
+    if n == 0 and out_total is None:
+        raise ValueError("out_total is needed where there are no gradients")
+    like = grads.tensors[0] if n else out_total
+    dev = like.device
+    if out_norms is None:
+        out_norms = _new((n,), torch.float32, dev, stream)
+    if out_total is None:
+        out_total = _new((1,), torch.float32, dev, stream)
+    if out_nonfinite is None:
+        out_nonfinite = _new((n,), torch.int64, dev, stream)
+    _check(out_norms, "out_norms", torch.float32, (n,), like)
+    _check(out_total, "out_total", torch.float32, (1,), like)
+    _check(out_nonfinite, "out_nonfinite", torch.int64, (n,), like)
+    workspace = _space(workspace, grads.workspace_bytes, "sf_grad_norm", like, stream)
+    rc = _lib.sf_grad_norm(grads._list, out_norms.data_ptr(), out_total.data_ptr(), out_nonfinite.data_ptr(),
+                           workspace.data_ptr(), workspace.numel(), _stream_handle(stream, dev))
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_grad_norm")
+    return out_norms, out_total, out_nonfinite
+
+
+def sf_grad_clip(grads, norms: torch.Tensor, max_norm: float, eps: float = 1e-6, out=None,
+                 status: torch.Tensor | None = None, stream=None):
+    """Scales gradients to a largest norm (``sf_grad_clip``).
+
+    ``grads``: a ``GradSet`` or tensors.  ``norms`` [m] float32: ``out_total``
+    of ``sf_grad_norm``, or that of every rank.  ``out``: where the scaled
+    gradients go (a ``GradSet`` or tensors of the same types and layouts), by
+    default in place.  ``status``, a one-element int32 tensor, takes
+    ``SF_ERANGE`` where the norm is not finite and the gradients are left as
+    they are.  Returns the set of scaled gradients.
+    """
+    if not isinstance(grads, GradSet):
+        grads = GradSet(grads)
+    if out is None:
+        out = grads
+    elif not isinstance(out, GradSet):
+        out = GradSet(out)
+    if norms.dim() != 1:
+        raise ValueError("norms must be [m]")
+    if len(out) != len(grads):
+        raise ValueError("out has %d tensors, grads %d" % (len(out), len(grads)))
+    if out is not grads:
+        if out._order != grads._order:
+            raise ValueError("out must have the gradients' order of dimensions")
+        if out.device != grads.device:
+            raise ValueError("out is on %s, the gradients on %s" % (out.device, grads.device))
+    like = grads.tensors[0] if len(grads) else norms
+    _check(norms, "norms", torch.float32, norms.shape, like)
+    if status is not None:
+        _check(status, "status", torch.int32, (1,), like)
+    rc = _lib.sf_grad_clip(grads._list, out._list, norms.data_ptr(), norms.shape[0], max_norm, eps,
+                           None if status is None else status.data_ptr(), _stream_handle(stream, like.device))
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_grad_clip")
+    return out

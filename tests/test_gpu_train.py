@@ -1,0 +1,544 @@
+"""The operators of stagefrontier_train.h against their definitions in 64 bits
+(train_ref.py), at the sizes, masks and layouts where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+import train_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+KINDS = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def tr():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_06751_amd import train
+    return train
+
+
+def same_or_close(got, want, bound, what):
+    """Elementwise |got - want| <= bound; infinities and NaN where they belong."""
+    got, want, bound = (np.atleast_1d(np.asarray(a, np.float64)) for a in (got, want, bound))
+    odd = ~np.isfinite(want)
+    np.testing.assert_array_equal(got[odd], want[odd], err_msg=what)
+    off = np.abs(got[~odd] - want[~odd])
+    ok = off <= bound[~odd]
+    assert ok.all(), "%s: %d of %d off, worst %g against %g (at %d: %g for %g)" % (
+        what, (~ok).sum(), ok.size, off[~ok].max(), bound[~odd][np.argmax(off)], np.argmax(off),
+        got[~odd][np.argmax(off)], want[~odd][np.argmax(off)])
+
+
+# -- log-probabilities -----------------------------------------------------
+
+def matrix(N, V, kind, seed, pad=0, shift=0):
+    """Logits as rows of a larger buffer that starts ``shift`` entries in."""
+    g = torch.Generator().manual_seed(seed)
+    buf = (torch.randn(N * (V + pad) + shift, generator=g) * 3.0).to(KINDS[kind])
+    return buf.to(DEV)[shift:].view(N, V + pad)[:, :V]
+
+
+def check_logp(tr, logits, targets, inv_t, **kw):
+    logp, lse, ent = tr.sf_token_logp(logits, targets, inv_temperature=inv_t, **kw)
+    torch.cuda.synchronize()
+    x, t = logits.float().cpu().numpy(), targets.cpu().numpy()
+    inv32 = float(np.float32(inv_t))
+    for i in range(len(t)):
+        want, bound = ref.token_logp(x[i], int(t[i]), inv32)
+        for name, got, w, b in zip(("logp", "lse", "entropy"), (logp, lse, ent), want, bound):
+            same_or_close(got[i].item(), w, b, "%s of row %d" % (name, i))
+    return logp, lse, ent
+
+
+def check_grad(tr, logits, targets, inv_t, lse, ent, with_h, out=None, **kw):
+    N, V = logits.shape
+    g = torch.Generator().manual_seed(N + V)
+    gl = torch.randn(N, generator=g).to(DEV)
+    gh = torch.randn(N, generator=g).to(DEV) * 0.1 if with_h else None
+    kind = {v: k for k, v in KINDS.items()}[logits.dtype]
+    x = logits.float().cpu().numpy()
+    got = tr.sf_token_logp_grad(logits, targets, lse, gl, entropy=ent if with_h else None, grad_entropy=gh,
+                                inv_temperature=inv_t, out_grad=out, **kw)
+    torch.cuda.synchronize()
+    got = got.float().cpu().numpy()
+    inv32 = float(np.float32(inv_t))
+    for i in range(N):
+        want, bound = ref.token_logp_grad(x[i], int(targets[i]), inv32, lse[i].item(), ent[i].item(), gl[i].item(),
+                                          gh[i].item() if with_h else 0.0, kind)
+        same_or_close(got[i], want, bound, "gradient of row %d" % i)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,V,pad,shift", [
+    (1, 1, 0, 0), (1, 2, 0, 1), (3, 5, 0, 3), (2, 8, 0, 0), (5, 9, 2, 7), (7, 63, 0, 1), (4, 64, 3, 0), (9, 257, 0, 5),
+    (3, 1023, 1, 0), (2, 4096, 0, 0), (5, 8191, 0, 1), (2, 8192, 8, 0), (1, 16385, 0, 3), (3, 40001, 0, 1),
+    (1, 131072, 0, 0), (2, 200003, 5, 1), (1100, 515, 0, 1), (300, 2050, 6, 2), (130, 9001, 0, 1)])
+def test_logp_and_gradient(tr, kind, N, V, pad, shift):
+    logits = matrix(N, V, kind, 7 * N + V, pad, shift)
+    targets = torch.randint(-1 if N > 2 else 0, V, (N,), generator=torch.Generator().manual_seed(V)).to(DEV)
+    inv_t = 1.0 / 0.7
+    _, lse, ent = check_logp(tr, logits, targets, inv_t)
+    if N <= 300:
+        check_grad(tr, logits, targets, inv_t, lse, ent, True)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_gradient_without_entropy(tr, kind):
+    logits = matrix(6, 301, kind, 5, 1, 1)
+    targets = torch.tensor([0, 300, -100, 301, 17, 5], device=DEV)
+    _, lse, _ = tr.sf_token_logp(logits, targets, entropy=False)
+    check_grad(tr, logits, targets, 1.0, lse, torch.zeros(6, device=DEV), False)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_logp_masked_and_extreme_logits(tr, kind):
+    low = torch.finfo(KINDS[kind]).min
+    V = 9000
+    rows = [np.random.default_rng(k).normal(size=V) for k in range(11)]
+    rows[1][:] = -np.inf                       # nothing left
+    rows[2][:] = -np.inf
+    rows[2][4321] = 2.0                        # one left, and it is the taken one
+    rows[3][::2] = -np.inf
+    rows[4][:] = low                           # all at the type's lowest value: uniform
+    rows[5][1:] = low
+    rows[6][100] = np.inf
+    rows[7][8999] = np.nan
+    rows[8][:] = -60000.0                      # masked by a large number throughout
+    rows[9][:] = 0.0
+    rows[9][7] = 1000.0                        # one certain
+    rows[10][:] = -np.inf
+    rows[10][8000:] = 1.0                      # whole parts of the row masked
+    logits = torch.tensor(np.array(rows), dtype=torch.float32).clamp(min=-math.inf).to(KINDS[kind]).to(DEV)
+    logits[4] = low
+    logits[5, 1:] = low
+    targets = torch.tensor([3, 3, 4321, 1, 5, 0, 5, 5, 8, 7, 8500], device=DEV)
+    logp, lse, ent = check_logp(tr, logits, targets, 1.0)
+    assert torch.isnan(logp[6:8]).all() and torch.isnan(lse[6:8]).all() and torch.isnan(ent[6:8]).all()
+    # the taken token itself masked
+    assert tr.sf_token_logp(logits[3:4], torch.tensor([0], device=DEV))[0].item() == -math.inf
+    keep = [0, 1, 2, 3, 5, 8, 9, 10]
+    check_grad(tr, logits[keep], targets[keep], 1.0, lse[keep], ent[keep], True)
+    # many such rows, too: parts of rows and whole rows take the same values
+    big = logits.repeat(120, 1)
+    for one, many in zip((logp, lse, ent), tr.sf_token_logp(big, targets.repeat(120))):
+        torch.testing.assert_close(many.view(120, -1), one.expand(120, -1), rtol=1e-5, atol=1e-5, equal_nan=True)
+
+
+def test_logp_rows_out_of_reach(tr):
+    """Rows that take no part are 0, whatever they hold, and give no gradient."""
+    logits = torch.full((4, 700), float("nan"), dtype=torch.bfloat16, device=DEV)
+    logits[1] = 0.0
+    targets = torch.tensor([-1, 3, 700, -(1 << 62)], device=DEV)
+    logp, lse, ent = tr.sf_token_logp(logits, targets)
+    keep = torch.tensor([0, 2, 3], device=DEV)
+    assert not logp[keep].any() and not lse[keep].any() and not ent[keep].any()
+    grad = tr.sf_token_logp_grad(logits, targets, lse, torch.ones(4, device=DEV), entropy=ent,
+                                 grad_entropy=torch.ones(4, device=DEV))
+    assert not grad[keep].any() and torch.isfinite(grad).all()
+
+
+def test_gradient_in_place_and_strides(tr):
+    logits = matrix(5, 777, "bf16", 3, 7, 1)
+    targets = torch.tensor([0, 776, -1, 5, 400], device=DEV)
+    _, lse, ent = tr.sf_token_logp(logits, targets)
+    g, h = torch.randn(5, device=DEV), torch.randn(5, device=DEV)
+    want = tr.sf_token_logp_grad(logits, targets, lse, g, entropy=ent, grad_entropy=h)
+    wide = torch.full((5, 1000), 9.0, dtype=torch.bfloat16, device=DEV)
+    tr.sf_token_logp_grad(logits, targets, lse, g, entropy=ent, grad_entropy=h, out_grad=wide[:, 3:780])
+    assert torch.equal(wide[:, 3:780], want)
+    assert (wide[:, :3] == 9).all() and (wide[:, 780:] == 9).all()
+    tr.sf_token_logp_grad(logits, targets, lse, g, entropy=ent, grad_entropy=h, out_grad=logits)
+    assert torch.equal(logits, want)
+
+
+def test_logp_offsets_past_32_bits(tr):
+    """Rows whose entries lie past 2^31 and 2^32 elements."""
+    V, N = 1 << 20, 4100
+    buf = torch.empty((N, V), dtype=torch.bfloat16, device=DEV)
+    targets = torch.full((N,), -1, dtype=torch.int64, device=DEV)
+    rows = [0, 2047, 2048, 2049, 4095, 4096, 4099]
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for k in rows:
+        buf[k] = torch.randn(V, generator=g, device=DEV).to(torch.bfloat16)
+        targets[k] = k * 17
+    logp, lse, ent = tr.sf_token_logp(buf, targets)
+    gl = torch.full((N,), 2.0, device=DEV)
+    grad = tr.sf_token_logp_grad(buf, targets, lse, gl, out_grad=buf.clone())
+    for k in rows:
+        want, bound = ref.token_logp(buf[k].float().cpu().numpy(), k * 17, 1.0)
+        for got, w, b in zip((logp, lse, ent), want, bound):
+            same_or_close(got[k].item(), w, b, "row %d" % k)
+        want, bound = ref.token_logp_grad(buf[k].float().cpu().numpy(), k * 17, 1.0, lse[k].item(), 0.0, 2.0, 0.0, "bf16")
+        same_or_close(grad[k].float().cpu().numpy(), want, bound, "gradient of row %d" % k)
+    assert not grad[1].any() and not grad[4098].any() and not logp[1] and not logp[4098]
+
+
+# -- policy loss -----------------------------------------------------------
+
+def policy_inputs(N, B, seed, steps=True):
+    rng = np.random.default_rng(seed)
+    lp = -np.abs(rng.normal(size=N)) * 2
+    old, r = lp + 0.25 * rng.normal(size=N), lp + 0.4 * rng.normal(size=N)
+    if N > 20:
+        old[5], r[7], r[9], old[11] = lp[5] + 30, lp[7] - 40, lp[9] + 30, lp[11] - 6
+    lp, old, r = (np.round(v * 16384) / 16384 for v in (lp, old, r))  # differences exact in 32 bits
+    cuts = np.sort(rng.integers(0, N + 1, B - 1)) if B > 1 else np.zeros(0, np.int64)
+    start = np.concatenate([[0], cuts, [N]]).astype(np.int64)
+    return lp.astype(np.float32), old.astype(np.float32), r.astype(np.float32), start, rng
+
+
+def run_policy(tr, lp, old, r, adv, per, mask, start, red, scale, lo, hi, beta, **kw):
+    dev = [None if v is None else torch.tensor(v).to(DEV) for v in (lp, old, r, adv, mask, start)]
+    terms, grad = tr.sf_policy_loss(dev[0], dev[1], dev[3], dev[5], ref_logp=dev[2], mask=dev[4],
+                                    advantage_per_token=per, reduction=red, scale=scale, clip_low=lo, clip_high=hi,
+                                    kl_coef=beta, **kw)
+    return terms.cpu().numpy(), grad.cpu().numpy()
+
+
+@pytest.mark.parametrize("reduction", [0, 1, 2])
+@pytest.mark.parametrize("N,B", [(1, 1), (2, 5), (3, 1), (65, 3), (257, 257), (1023, 7), (1025, 1), (4099, 300),
+                                 (9000, 2), (20000, 5000), (70001, 11)])
+def test_policy(tr, N, B, reduction):
+    lp, old, r, start, rng = policy_inputs(N, B, N + B)
+    for per, masked, with_ref in ((False, True, True), (True, False, False), (True, True, True), (False, False, True)):
+        adv = rng.normal(size=N if per else B).astype(np.float32)
+        adv[::5] = 0.0
+        mask = rng.integers(0, 3, N).astype(np.uint8) if masked else None
+        args = (lp, old, r if with_ref else None, adv, per, mask, start, reduction, 0.75, 0.2, 0.3, 0.05)
+        terms, grad = run_policy(tr, *args)
+        f32 = [float(np.float32(v)) for v in (0.2, 0.3, 0.05)]
+        want, size, wgrad, bound = ref.policy(*args[:9], *f32)
+        same_or_close(grad, wgrad, bound + 1e-37, "gradient")
+        same_or_close(terms, want, size + 1e-37, "terms")
+
+
+def test_policy_masked_garbage_and_tokens_of_no_sequence(tr):
+    N, start = 3000, np.array([100, 100, 900, 900, 2500, 2500], np.int64)
+    lp, old, r, _, rng = policy_inputs(N, 1, 4)
+    adv, mask = rng.normal(size=5).astype(np.float32), (rng.random(N) < 0.5).astype(np.uint8)
+    mask[900:1500] = 0
+    args = [lp, old, r, adv, False, mask, start, 1, 1.0, 0.2, 0.2, 0.1]
+    terms, grad = run_policy(tr, *args)
+    want, size, wgrad, bound = ref.policy(*args[:9], *(float(np.float32(v)) for v in args[9:]))
+    same_or_close(grad, wgrad, bound + 1e-37, "gradient")
+    same_or_close(terms, want, size + 1e-37, "terms")
+    off = (mask == 0) | (np.arange(N) < 100) | (np.arange(N) >= 2500)
+    assert not grad[off].any()
+    for v, junk in zip((lp, old, r), (np.nan, np.inf, -np.inf)):
+        v[off] = junk
+    adv[[0, 2, 4]] = np.nan  # advantages of sequences without tokens
+    again, ggrad = run_policy(tr, *args)
+    np.testing.assert_array_equal(again, terms)
+    np.testing.assert_array_equal(ggrad, grad)
+
+
+@pytest.mark.parametrize("N,B,masked", [(0, 0, False), (0, 3, False), (50, 0, False), (50, 3, True), (5000, 40, True)])
+@pytest.mark.parametrize("reduction", [0, 1, 2])
+def test_policy_with_nothing_taking_part(tr, N, B, masked, reduction):
+    z = np.zeros(N, np.float32)
+    start = np.linspace(0, N, B + 1).astype(np.int64)
+    terms, grad = run_policy(tr, z, z, z, np.ones(B, np.float32), False, np.zeros(N, np.uint8) if masked else None,
+                             start, reduction, 1.0, 0.2, 0.2, 0.1)
+    assert not terms.any() and not grad.any()
+
+
+def test_policy_large_ratios_stay_numbers(tr):
+    lp = np.array([0.0, 0.0, 0.0, -200.0], np.float32)
+    old = np.array([-200.0, -200.0, 0.0, 0.0], np.float32)
+    r = np.array([0.0, 0.0, 0.0, -1.0], np.float32)
+    adv = np.array([0.0, 1.0, 2.0, -1.0], np.float32)
+    args = (lp, old, None, adv, True, None, np.array([0, 4], np.int64), 0, 1.0, 0.2, 0.2, 0.0)
+    terms, grad = run_policy(tr, *args)
+    want, size, wgrad, bound = ref.policy(*args[:9], *(float(np.float32(v)) for v in args[9:]))
+    same_or_close(terms, want, size, "terms")
+    same_or_close(grad, wgrad, bound, "gradient")
+    # a reference far above: e^x is held at the largest float
+    terms, grad = run_policy(tr, lp[3:], lp[3:], r[3:], adv[:1], True, None, np.array([0, 1], np.int64), 0, 1.0, 0.2,
+                             0.2, 0.0)
+    assert np.isfinite(terms[:2]).all() and terms[2] == np.finfo(np.float32).max
+
+
+def test_policy_bool_mask_and_unaligned_views(tr):
+    N = 2051
+    lp, old, r, start, rng = policy_inputs(N, 9, 8)
+    adv = rng.normal(size=9).astype(np.float32)
+    mask = rng.random(N) < 0.6
+    want = run_policy(tr, lp, old, r, adv, False, mask.astype(np.uint8), start, 1, 1.0, 0.2, 0.2, 0.1)
+
+    def shifted(v, k):
+        buf = torch.zeros(len(v) + k, dtype=torch.tensor(v).dtype, device=DEV)
+        buf[k:] = torch.tensor(v).to(DEV)
+        return buf[k:]
+
+    got = tr.sf_policy_loss(shifted(lp, 1), shifted(old, 2), shifted(adv, 3), shifted(start, 1),
+                            ref_logp=shifted(r, 3), mask=shifted(mask, 5), reduction=1, kl_coef=0.1,
+                            out_grad=torch.zeros(N + 1, device=DEV)[1:])
+    np.testing.assert_array_equal(got[0].cpu().numpy(), want[0])
+    np.testing.assert_array_equal(got[1].cpu().numpy(), want[1])
+
+
+# -- gradient norm and clipping --------------------------------------------
+
+def tensors(sizes, kinds, seed, shift=0):
+    """Views of one buffer per type, ``shift`` entries in and one after the
+    other, so they start at any entry."""
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    bufs = {}
+    for k in set(kinds):
+        total = sum(n for n, q in zip(sizes, kinds) if q == k) + shift
+        bufs[k] = [(torch.randn(total, generator=g) * 0.02).to(KINDS[k]).to(DEV), shift]
+    for n, k in zip(sizes, kinds):
+        buf, at = bufs[k]
+        out.append(buf[at:at + n])
+        bufs[k][1] += n
+    return out
+
+
+def check_norm(tr, grads, **kw):
+    norms, total, wrong = tr.sf_grad_norm(grads, **kw)
+    torch.cuda.synchronize()
+    per, whole, count = ref.norms([g.double().cpu().numpy() for g in grads])
+    # 64-bit sums: one rounding to 32 bits is all that shows
+    same_or_close(norms.cpu().numpy(), per, np.array(per) * 2.0 ** -23, "norms")
+    same_or_close(total.item(), whole, whole * 2.0 ** -23, "total")
+    assert wrong.tolist() == count
+    return norms, total
+
+
+SIZES = [
+    [1], [0], [0, 0, 3], [7, 1, 0, 2, 2049, 64, 0], [2048], [2047, 2049, 1], [100003], [5] * 193, [3] * 400 + [70000],
+    [1 << 20, 33, 0, 999999], [1] * 1000]
+
+
+@pytest.mark.parametrize("kinds", [["f32"], ["bf16"], ["f16"], ["bf16", "f32", "f16"]])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%dx%d" % (len(s), sum(s)))
+def test_norm_and_clip(tr, sizes, kinds):
+    kinds = (kinds * len(sizes))[:len(sizes)]
+    grads = tensors(sizes, kinds, len(sizes), shift=1)
+    _, total = check_norm(tr, grads)
+    before = [g.double().cpu().numpy() for g in grads]
+    norm = total.item()
+    if norm == 0:
+        return
+    out = [torch.full_like(g, 5.0) for g in grads]
+    for max_norm in (norm * 0.37, norm * 2):
+        limit = float(np.float32(max_norm))
+        c = min(1.0, limit / (norm + float(np.float32(1e-6))))
+        tr.sf_grad_clip(grads, total, max_norm, out=out)
+        for g, o, b, k in zip(grads, out, before, kinds):
+            # the factor rounds once, the product once and once more to its type
+            want = b * c
+            same_or_close(o.double().cpu().numpy(), want,
+                          np.abs(want) * (2.0 ** -23 + ref.HALF_ULP[k] * (1 + 2.0 ** -22)) + ref.TINY[k], "clipped")
+            assert np.array_equal(g.double().cpu().numpy(), b)
+    scaled = [o.clone() for o in out]
+    tr.sf_grad_clip(grads, total, norm * 2)
+    assert all(torch.equal(g, s) for g, s in zip(grads, scaled))
+    tr.sf_grad_clip(grads, total, norm * 0.37, out=out)
+    tr.sf_grad_clip(grads, total, norm * 0.37)  # in place
+    assert all(torch.equal(g, o) for g, o in zip(grads, out))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_norm_counts_what_is_not_finite(tr, kind):
+    grads = tensors([5000, 300, 7, 40000], [kind] * 4, 3, shift=3)
+    grads[0][[0, 17, 4999]] = float("inf")
+    grads[1][299] = float("nan")
+    grads[3][20000:20100] = float("-inf")
+    norms, total, wrong = tr.sf_grad_norm(grads)
+    assert wrong.tolist() == [3, 1, 0, 100]
+    assert norms[0] == math.inf and torch.isnan(norms[1]) and torch.isfinite(norms[2]) and norms[3] == math.inf
+    assert torch.isnan(total).all()
+    before = [g.clone() for g in grads]
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = [torch.zeros_like(g) for g in grads]
+    tr.sf_grad_clip(grads, total, 1.0, out=out, status=status)
+    tr.sf_grad_clip(grads, norms[2:3], 1e9)
+    tr.sf_grad_clip(grads, norms[:1], 1.0)
+    assert status.item() == tr.SF_ERANGE
+    for g, b, o in zip(grads, before, out):
+        assert torch.equal(g.nan_to_num(7.0), b.nan_to_num(7.0)) and torch.equal(o.nan_to_num(7.0), b.nan_to_num(7.0))
+
+
+def test_norm_of_large_and_small_entries(tr):
+    """Squares past the range of 32 bits, on either side."""
+    grads = [torch.full((3000,), 1e30, device=DEV), torch.full((5,), 1e-30, device=DEV),
+             torch.tensor([3.0e38], dtype=torch.bfloat16, device=DEV)]
+    norms, total = check_norm(tr, grads)
+    assert torch.isfinite(total).all() and norms[1] > 0
+
+
+def test_clip_combines_the_norms_of_ranks(tr):
+    g = tensors([70001, 12], ["f32", "bf16"], 2)
+    for m in (1, 8, 255, 65536):
+        norms = torch.rand(m, generator=torch.Generator().manual_seed(m)).to(DEV)
+        whole = math.sqrt((norms.double() ** 2).sum().item())
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out = [torch.zeros_like(x) for x in g]
+        tr.sf_grad_clip(g, norms, 0.25, eps=0.5, out=out, status=status)
+        c = min(1.0, 0.25 / (whole + 0.5))
+        for x, o, k in zip(g, out, ("f32", "bf16")):
+            want = x.double().cpu().numpy() * c
+            same_or_close(o.double().cpu().numpy(), want,
+                          np.abs(want) * (2.0 ** -23 + ref.HALF_ULP[k] * (1 + 2.0 ** -22)), "m = %d" % m)
+        assert status.item() == 0
+
+
+def test_grads_of_any_dense_layout(tr):
+    base = torch.randn(12, 7, 5, device=DEV)
+    g = [base.permute(2, 0, 1), torch.randn(6, 4, device=DEV).t(), torch.randn(1, 9, device=DEV)[:, :]]
+    check_norm(tr, g)
+    out = [torch.empty_strided(x.shape, x.stride(), device=DEV) for x in g]
+    tr.sf_grad_clip(g, torch.tensor([4.0], device=DEV), 1.0, eps=0.0, out=out)
+    for x, o in zip(g, out):
+        assert torch.equal(o, x * 0.25)
+
+
+def test_norm_of_no_gradients(tr):
+    total = torch.full((1,), 3.0, device=DEV)
+    norms, got, wrong = tr.sf_grad_norm([], out_total=total)
+    assert got.item() == 0 and norms.numel() == 0 and wrong.numel() == 0
+
+
+def test_norm_past_32_bit_offsets(tr):
+    n = (1 << 32) + 4099
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    g[0], g[(1 << 31) + 5], g[n - 1] = 3.0, 4.0, 12.0
+    norms, total, wrong = tr.sf_grad_norm([g])
+    assert norms.item() == 13.0 and total.item() == 13.0 and wrong.item() == 0
+    tr.sf_grad_clip([g], total, 6.5, eps=0.0)
+    assert (g[0].item(), g[(1 << 31) + 5].item(), g[n - 1].item()) == (1.5, 2.0, 6.0)
+
+
+# -- streams, repetition, graphs --------------------------------------------
+
+def chain(tr, x, t, old, r, adv, start, grads, stream=None):
+    logp, lse, ent = tr.sf_token_logp(x, t, stream=stream)
+    terms, gl = tr.sf_policy_loss(logp, old, adv, start, ref_logp=r, kl_coef=0.1, stream=stream)
+    gx = tr.sf_token_logp_grad(x, t, lse, gl, stream=stream)
+    norms, total, wrong = tr.sf_grad_norm(grads, stream=stream)
+    return logp, lse, ent, terms, gl, gx, norms, total, wrong
+
+
+def chain_inputs(N=600, V=9001):
+    x = matrix(N, V, "bf16", 1)
+    t = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(2)).to(DEV)
+    z = torch.log_softmax(x.float(), 1).gather(1, t[:, None])[:, 0]
+    start = torch.tensor([0, 100, 100, 450, N], device=DEV)
+    return x, t, z + 0.1 * torch.randn(N, device=DEV), z - 0.2, torch.randn(4, device=DEV), start
+
+
+def test_same_bits_on_any_stream_and_every_time(tr):
+    args = chain_inputs()
+    grads = tr.GradSet(tensors([100000, 1, 4097, 1 << 20], ["bf16", "f32", "bf16", "f32"], 9, shift=1))
+    first = chain(tr, *args, grads)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(DEV)
+    for stream in (None, side, side.cuda_stream):
+        busy = torch.randn(4096, 4096, device=DEV)
+        for _ in range(3):
+            busy = busy @ busy * 1e-3  # work on the current stream meanwhile
+        got = chain(tr, *args, grads, stream=stream)
+        side.synchronize()
+        torch.cuda.synchronize()
+        for a, b in zip(first, got):
+            assert torch.equal(a, b)
+
+
+def test_captured_chain_replays(tr):
+    x, t, old, r, adv, start = chain_inputs(200, 4001)
+    g = tensors([50000, 3, 2049], ["bf16", "f32", "bf16"], 5)
+    grads = tr.GradSet(g)
+    N, V = x.shape
+    f = lambda *s: torch.empty(s, device=DEV)  # noqa: E731
+    o = dict(logp=f(N), lse=f(N), ent=f(N), terms=f(4), gl=f(N), gx=torch.empty_like(x), norms=f(3), total=f(1),
+             wrong=torch.empty(3, dtype=torch.int64, device=DEV), out=[torch.empty_like(q) for q in g],
+             w1=torch.empty(tr.sf_token_logp_workspace(N, V), dtype=torch.uint8, device=DEV),
+             w2=torch.empty(tr.sf_policy_loss_workspace(N, 4), dtype=torch.uint8, device=DEV),
+             w3=torch.empty(grads.workspace_bytes, dtype=torch.uint8, device=DEV))
+    outset = tr.GradSet(o["out"])
+
+    def step():
+        tr.sf_token_logp(x, t, out_logp=o["logp"], out_lse=o["lse"], out_entropy=o["ent"], workspace=o["w1"])
+        tr.sf_policy_loss(o["logp"], old, adv, start, ref_logp=r, kl_coef=0.1, reduction=1, out_terms=o["terms"],
+                          out_grad=o["gl"], workspace=o["w2"])
+        tr.sf_token_logp_grad(x, t, o["lse"], o["gl"], out_grad=o["gx"])
+        tr.sf_grad_norm(grads, o["norms"], o["total"], o["wrong"], workspace=o["w3"])
+        tr.sf_grad_clip(grads, o["total"], 0.5, out=outset)
+
+    def outputs():
+        torch.cuda.synchronize()
+        return [v.clone() for k in ("logp", "lse", "ent", "terms", "gl", "gx", "norms", "total", "wrong") for v in [o[k]]] \
+            + [v.clone() for v in o["out"]]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        # eager work between replays that changes every input
+        x.copy_(matrix(N, V, "bf16", 50 + k))
+        for q in g:
+            q.mul_(1.5)
+        step()
+        want = outputs()
+        for v in o.values():
+            for q in (v if isinstance(v, list) else [v]):
+                q.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        for a, b in zip(want, outputs()):
+            assert torch.equal(a, b)
+
+
+def test_binding_refusals(tr):
+    x = torch.zeros(4, 10, device=DEV)
+    t = torch.zeros(4, dtype=torch.int64, device=DEV)
+    f = torch.zeros(4, device=DEV)
+    bad = [
+        (TypeError, lambda: tr.sf_token_logp(x.double(), t)),
+        (ValueError, lambda: tr.sf_token_logp(x.cpu(), t)),
+        (TypeError, lambda: tr.sf_token_logp(x, t.int())),
+        (ValueError, lambda: tr.sf_token_logp(x, t[:3])),
+        (ValueError, lambda: tr.sf_token_logp(x.t(), torch.zeros(10, dtype=torch.int64, device=DEV))),
+        (ValueError, lambda: tr.sf_token_logp(x[0], t)),
+        (ValueError, lambda: tr.sf_token_logp(x[:1].expand(4, 10), t)),
+        (tr.StageFrontierError, lambda: tr.sf_token_logp(x, t, inv_temperature=0.0)),
+        (tr.StageFrontierError, lambda: tr.sf_token_logp(x, t, inv_temperature=float("nan"))),
+        (tr.StageFrontierError, lambda: tr.sf_token_logp(x, t, out_logp=x.view(-1)[:4])),
+        (ValueError, lambda: tr.sf_token_logp_grad(x, t, f, f, grad_entropy=f)),
+        (ValueError, lambda: tr.sf_token_logp_grad(x, t, f, f, out_grad=x.bfloat16())),
+        (tr.StageFrontierError, lambda: tr.sf_token_logp_grad(x[:2], t[:2], f[:2], f[:2], out_grad=x[1:3])),
+        (ValueError, lambda: tr.sf_policy_loss(f, f, f[:2], t)),
+        (TypeError, lambda: tr.sf_policy_loss(f, f, f[:3], t.int())),
+        (TypeError, lambda: tr.sf_policy_loss(f, f, f[:3], t, mask=f)),
+        (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, clip_low=1.0)),
+        (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, reduction=3)),
+        (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, out_grad=f)),
+        (ValueError, lambda: tr.sf_policy_loss(f, f, f[:3], t, workspace=torch.zeros(8, dtype=torch.uint8, device=DEV))),
+        (TypeError, lambda: tr.GradSet([x.double()])),
+        (ValueError, lambda: tr.GradSet([x, x.cpu()])),
+        (ValueError, lambda: tr.GradSet([x[:, :5]])),
+        (ValueError, lambda: tr.sf_grad_norm([])),
+        (tr.StageFrontierError, lambda: tr.sf_grad_norm([x], out_total=x.view(-1)[:1])),
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x, x], f, 1.0)),               # one tensor twice, in place
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x], f, 0.0)),
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x], f, 1.0, eps=-1.0)),
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x], x.view(-1)[:1], 1.0)),     # the norm inside a gradient
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x[:2]], f, 1.0, out=[x[1:3]])),
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x[:2], x[2:]], f, 1.0, out=[x[2:], x[:2]])),
+        (tr.StageFrontierError, lambda: tr.sf_grad_clip([x], f, 1.0, out=[x.bfloat16()])),
+        (ValueError, lambda: tr.sf_grad_clip([x], f, 1.0, out=[x.clone(), f])),
+        (ValueError, lambda: tr.sf_grad_clip([x.t()], f, 1.0, out=[torch.zeros(10, 4, device=DEV)])),
+    ]
+    for k, (err, call) in enumerate(bad):
+        with pytest.raises(err):
+            call()
+            pytest.fail("refusal %d" % k)
