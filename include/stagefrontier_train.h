@@ -50,7 +50,7 @@ enum {
  *   row_stride       elements from one row to the next, >= V.
  *   targets          [N] int64.  A row whose target lies outside [0, V) takes
  *                    no part: it is not read, and its outputs are 0.
- *   inv_temperature  > 0, finite.
+ *   inv_temperature  0 < inv_temperature <= 2^100.
  *   out_logp         [N] float.
  *   out_lse          [N] float.
  *   out_entropy      [N] float, or NULL where the entropy is not wanted.

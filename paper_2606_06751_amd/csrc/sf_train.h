@@ -45,10 +45,48 @@ __device__ __forceinline__ int64_t head_elems(const void* p, int64_t n)
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLog2eD = 1.44269504088896340736;
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLn2Low = -1.90465429995776804525e-9f;  // ln 2 - kLn2
 constexpr float kF32Max = 3.402823466e38f;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// One DPP move; lanes outside ROW_MASK get `old`.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_f32(float old, float v)
+{
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, ROW_MASK, 0xF, false));
+}
+__device__ __forceinline__ float last_lane(float v)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Sum and maximum over a wave, wave-uniform: within rows of 16 lanes by
+// exchanges that pair each lane with one of the other half, then row by row
+// into the last lane.
+__device__ __forceinline__ float wave_sum_f32(float v)
+{
+    v += dpp_f32<0xB1, 0xF>(0.0f, v);   // quad_perm [1,0,3,2]
+    v += dpp_f32<0x4E, 0xF>(0.0f, v);   // quad_perm [2,3,0,1]
+    v += dpp_f32<0x141, 0xF>(0.0f, v);  // row_half_mirror
+    v += dpp_f32<0x140, 0xF>(0.0f, v);  // row_mirror
+    v += dpp_f32<0x142, 0xA>(0.0f, v);  // row_bcast:15 -> rows 1, 3
+    v += dpp_f32<0x143, 0xC>(0.0f, v);  // row_bcast:31 -> rows 2, 3
+    return last_lane(v);
+}
+__device__ __forceinline__ float wave_max_f32(float v)
+{
+    v = fmaxf(v, dpp_f32<0xB1, 0xF>(v, v));
+    v = fmaxf(v, dpp_f32<0x4E, 0xF>(v, v));
+    v = fmaxf(v, dpp_f32<0x141, 0xF>(v, v));
+    v = fmaxf(v, dpp_f32<0x140, 0xF>(v, v));
+    v = fmaxf(v, dpp_f32<0x142, 0xA>(v, v));
+    v = fmaxf(v, dpp_f32<0x143, 0xC>(v, v));
+    return last_lane(v);
+}
 
 __device__ __forceinline__ double wave_sum_f64(double v)
 {

@@ -1,12 +1,19 @@
 // tokens.hip -- log-probability of the taken token, normaliser and entropy of
 // rows of logits (sf_token_logp), and their gradient (sf_token_logp_grad).
 //
-// Forward: one pass over a row with the running maximum m and, relative to it,
-//     s = sum e^((x - m) / T),   u = sum e^((x - m) / T) (x - m) / T
-// (the exponent in base 2, c = log2(e) / T): log p, lse and the entropy
-// H = log s - u / s come from m, s, u and the taken token's logit.  The
-// difference is taken before it is scaled, so the largest term is exactly 1
-// and a row of very low logits, all masked alike, still has its distribution.
+// Forward: one pass over a row.  With c = log2(e) / T, each wave keeps a
+// reference (b, R), R a whole number, and its lanes
+//     s = sum 2^t,   u = sum 2^t t,   t = (x - b) c - R,
+// from which log p, lse and the entropy H = log s - ln 2 u / s follow.  b is 0
+// but for rows of huge logits, so t is one multiply-add whose only error is its
+// own rounding, and a change of R scales by a power of two, without any.
+//
+// What bounds it is HBM and, close behind, the VALU: one exponential (a quarter
+// of the VALU's rate), a conversion, two multiply-adds and an add per logit.  So
+// the running maximum is not taken per logit: a chunk is added relative to the
+// wave's reference as it stands, and only where its sum shows that a logit lies
+// far above (or a product was not a number: -inf) is the chunk done again with
+// its maximum.  The reference is a wave's, not a lane's, so that this is rare.
 
 #include "sf_device.h"
 #include "sf_host.h"
@@ -16,83 +23,169 @@ namespace sfk {
 
 constexpr int kRowWG = 256;
 
+// Terms relative to (m, lo): s = sum 2^((x - m) c + lo), u = sum 2^t t with t
+// that exponent.  lo is the rounding of m c, so that t is one multiply-add of
+// x whose only error is its own rounding, and the largest term is 2^lo.
 struct RowState {
-    float m, s, u;
+    float b, R, s, u;  // R = -inf: nothing but -inf so far
 };
 
-// e^((x - m) / T) and its share of u.  A logit of -inf has e = 0; the bound
-// keeps 0 * -inf out of u.  NaN passes through e.
-__device__ __forceinline__ void row_add(RowState& a, float x, float ref, float c)
-{
-    const float t = (x - ref) * c;
-    const float e = fast_exp2(t);
-    a.s += e;
-    a.u = fmaf(e, fmaxf(t, -1000.0f), a.u);
-}
+struct RowScale {
+    float inv_t, c, eps;  // c (1 + eps) = inv_t log2(e) more exactly than c is
+};
 
-// The state's terms relative to a larger maximum.
-__device__ __forceinline__ void row_rebase(RowState& a, float m, float ref, float c)
+// A reference's place on the exponents' scale, -inf where there is none yet.
+__device__ __forceinline__ double row_height(float b, float R, float c) { return fma((double)b, (double)c, (double)R); }
+
+// The state's sums relative to another reference.  In 64 bits, where nothing
+// of the type's range overflows; a state without terms weighs 0.
+__device__ __forceinline__ void row_rebase(RowState& a, float b, float R, float c)
 {
-    const float t = (a.m - ref) * c;
+    const float t = (float)fma((double)a.b - (double)b, (double)c, (double)a.R - (double)R);
     const float e = fast_exp2(t);
     a.u = e * fmaf(fmaxf(t, -1000.0f), a.s, a.u);
     a.s *= e;
-    a.m = m;
+    a.b = b;
+    a.R = R;
 }
 
-// What the terms are taken relative to: 0 while every logit was -inf.
-__device__ __forceinline__ float row_ref(float m) { return m == -INFINITY ? 0.0f : m; }
+constexpr int kRowU = 4;  // vectors of a chunk per lane
 
-__device__ __forceinline__ RowState row_merge(RowState a, RowState b, float c)
+// Adds `live` vectors a lane and an edge logit (-inf: none) after taking their
+// maximum.  Lanes without a logit hold -inf, whose e is 0; the bound keeps
+// 0 * -inf out of u; NaN passes through e.  From |m| = 2^20 on the reference is
+// the maximum itself, taken off before the product: a row of very low logits,
+// all masked alike, keeps its distribution.
+template <int DT>
+__device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU], int live, float edge, float c)
 {
-    const float m = fmaxf(a.m, b.m), ref = row_ref(m);
-    row_rebase(a, m, ref, c);
-    row_rebase(b, m, ref, c);
-    return {m, a.s + b.s, a.u + b.u};
-}
-
-__device__ __forceinline__ RowState row_wave(RowState a, float c)
-{
-    for (int off = 32; off > 0; off >>= 1) {
-        const RowState b = {__shfl_xor(a.m, off, 64), __shfl_xor(a.s, off, 64), __shfl_xor(a.u, off, 64)};
-        a = row_merge(a, b, c);
+    constexpr int E = kVec<DT>;
+    float m = edge;
+#pragma unroll
+    for (int k = 0; k < kRowU; ++k)
+        if (k < live)
+#pragma unroll
+            for (int j = 0; j < E; ++j) m = fmaxf(m, (float)y[k][j]);
+    m = wave_max_f32(m);
+    if (m != -INFINITY) {
+        const bool huge = !(fabsf(m) < 1048576.0f);
+        const float b = huge ? m : 0.0f, R = huge ? 0.0f : rintf(m * c);
+        if (row_height(b, R, c) > row_height(a.b, a.R, c)) row_rebase(a, b, R, c);
     }
+    const float R = a.R == -INFINITY ? 0.0f : a.R;
+    auto add = [&](float v) {
+        const float t = fmaf(v - a.b, c, -R);
+        const float e = fast_exp2(t);
+        a.s += e;
+        a.u = fmaf(e, fmaxf(t, -1000.0f), a.u);
+    };
+    add(edge);
+#pragma unroll
+    for (int k = 0; k < kRowU; ++k)
+        if (k < live)
+#pragma unroll
+            for (int j = 0; j < E; ++j) add((float)y[k][j]);
+}
+
+// Adds a full chunk relative to the reference as it is; false where that would
+// lose digits (a term far above 1) or is not a number.
+template <int DT>
+__device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[kRowU], float c)
+{
+    constexpr int E = kVec<DT>, K = kRowU * E;
+    float s = 0.0f, u = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kRowU; ++k)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float t = fmaf((float)y[k][j], c, -a.R);
+            const float e = fast_exp2(t);
+            s += e;
+            u = fmaf(e, t, u);
+        }
+    // no term above 2^(1/2) gives K * 1.42 at most
+    if (__any(!(s < 2.0f * K) || u != u)) return false;
+    a.s += s;
+    a.u += u;
+    return true;
+}
+
+// The wave's sums in every lane.
+__device__ __forceinline__ RowState row_wave(RowState a)
+{
+    a.s = wave_sum_f32(a.s);
+    a.u = wave_sum_f32(a.u);
     return a;
 }
 
-__device__ __forceinline__ void row_write(RowState a, float xt, float inv_t, int64_t i, float* logp,
-                                          float* lse, float* entropy)
+// Two states as one, relative to the higher reference.
+__device__ __forceinline__ RowState row_merge(RowState a, RowState o, float c)
 {
-    if (a.m == -INFINITY && a.s == 0.0f) {
+    if (row_height(o.b, o.R, c) > row_height(a.b, a.R, c))
+        row_rebase(a, o.b, o.R, c);
+    else if (a.R != -INFINITY)
+        row_rebase(o, a.b, a.R, c);
+    a.s += o.s;
+    a.u += o.u;
+    return a;
+}
+
+// Joins the states of aligned groups of LANES lanes, in every lane of them.
+template <int LANES>
+__device__ __forceinline__ RowState row_join(RowState a, float c)
+{
+    for (int off = LANES / 2; off > 0; off >>= 1)
+        a = row_merge(a, {__shfl_xor(a.b, off, 64), __shfl_xor(a.R, off, 64), __shfl_xor(a.s, off, 64),
+                          __shfl_xor(a.u, off, 64)}, c);
+    return a;
+}
+
+__device__ __forceinline__ void row_write(RowState a, float xt, RowScale z, int64_t i, float* logp, float* lse,
+                                          float* entropy)
+{
+    if (a.s == 0.0f) {
         logp[i] = lse[i] = -INFINITY;
         if (entropy) entropy[i] = 0.0f;
         return;
     }
-    const float ls = logf(a.s);
-    logp[i] = (xt - a.m) * inv_t - ls;
-    lse[i] = fmaf(a.m, inv_t, ls);
-    if (entropy) entropy[i] = fmaxf(ls - kLn2 * (a.u / a.s), 0.0f) + 0.0f * a.s;
+    const float ls = logf(a.s), mean = a.u / a.s;  // mean exponent
+    const float t = fmaf(xt - a.b, z.c, -a.R);
+    const float turn = z.eps * kLn2;
+    // the exponents are off by c's own rounding, which turns log p by their
+    // distance from the mean and lse by the mean
+    logp[i] = fmaf(t, kLn2, -ls) + (t > -1000.0f ? turn * (t - mean) : 0.0f);
+    lse[i] = a.b == 0.0f ? fmaf(a.R, kLn2, fmaf(a.R, kLn2Low, ls)) + turn * (a.R + mean) : fmaf(a.b, z.inv_t, ls);
+    if (entropy) {
+        const float h = ls - kLn2 * mean;
+        entropy[i] = h < 0.0f ? 0.0f : h;
+    }
 }
 
-// One workgroup per (row, part): part p of P takes the p-th share of the row's
-// 16-byte vectors; with P > 1 its state goes to the workspace.
-template <int DT>
-__global__ __launch_bounds__(kRowWG) void k_token_logp(const typename Elem<DT>::T* __restrict__ logits,
-                                                       int64_t N, int64_t V, int64_t stride,
-                                                       const int64_t* __restrict__ targets, float inv_t,
-                                                       int P, float* __restrict__ logp,
-                                                       float* __restrict__ lse, float* __restrict__ entropy,
-                                                       RowState* __restrict__ parts)
+// WAVES waves per row; a workgroup of WG threads takes WG / 64 / WAVES rows,
+// or, with gridDim.y > 1, part blockIdx.y of one row (`share` 16-byte vectors
+// each), whose state goes to the workspace.  The elements before the first and
+// after the last whole vector join the last chunk, one a lane.  Every chunk
+// that needs its maximum goes through one piece of code: where few rows give a
+// compute unit little work, fetching the code is a good part of the time.
+template <int DT, int WG, int WAVES>
+__global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* __restrict__ logits, int64_t N, int V,
+                                                   int64_t stride, const int64_t* __restrict__ targets, RowScale z,
+                                                   int share, float* __restrict__ logp, float* __restrict__ lse,
+                                                   float* __restrict__ entropy, RowState* __restrict__ parts)
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
-    constexpr int U = 4;
-    __shared__ RowState wave_state[kRowWG / 64];
-    const float c = inv_t * kLog2e;
-    const int tid = threadIdx.x;
-    for (int64_t blk = blockIdx.x; blk < N * P; blk += gridDim.x) {
-        const int64_t i = blk / P;
-        const int p = (int)(blk - i * P);
+    constexpr int U = kRowU;
+    constexpr int LANES = WAVES * 64;
+    constexpr int ROWS = WG / LANES;
+    static_assert(ROWS == 1 || WAVES == 1, "rows of one wave, or one row");
+    __shared__ RowState wave_state[WAVES];
+    const int tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63;  // within the row
+    const int wave0 = __builtin_amdgcn_readfirstlane(tid & ~63);
+    const int p = ROWS == 1 ? blockIdx.y : 0, P = ROWS == 1 ? gridDim.y : 1;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    for (int64_t i = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+         i < N; i += step) {
         const int64_t t = targets[i];
         if (t < 0 || t >= V) {
             if (tid == 0 && p == 0) {
@@ -102,53 +195,50 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp(const typename Elem<DT>::
             continue;
         }
         const T* row = logits + i * stride;
-        const int64_t head = head_elems<DT>(row, V);
-        const int64_t nv = (V - head) / E;
-        const int64_t v0 = nv * p / P, v1 = nv * (p + 1) / P;
-        RowState a = {-INFINITY, 0.0f, 0.0f};
+        const int head = (int)head_elems<DT>(row, V);
+        const int nv = (V - head) / E, tail0 = head + nv * E;
         const T* body = row + head;
-        for (int64_t v = v0 + tid; v < v1; v += U * kRowWG) {
-            VecU<DT> x[U];
-            int n = 0;
+        const int v0 = min(nv, p * share), v1 = min(nv, v0 + share);
+        const int nh = p == 0 ? head : 0, nt = p == P - 1 ? V - tail0 : 0;
+        const T xt = row[t];
+        const bool has_edge = tid < nh + nt;
+        const T edge = row[has_edge ? (tid < nh ? tid : tail0 + (tid - nh)) : 0];
+        RowState a = {0.0f, -INFINITY, 0.0f, 0.0f};
+        for (int w = v0 + wave0;; w += U * LANES) {
+            const int v = w + (tid & 63);
+            const bool last = w + U * LANES >= v1;
+            VecU<DT> y[U];
+            if (!last) {
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int64_t w = v + k * kRowWG;
-                x[k] = *(const VecU<DT>*)(body + (w < v1 ? w : v) * E);
-                n += w < v1;
+                for (int k = 0; k < U; ++k) y[k] = __builtin_nontemporal_load((const VecU<DT>*)(body + (int64_t)(v + k * LANES) * E));
+                if (a.b == 0.0f && a.R != -INFINITY && row_try<DT>(a, y, z.c)) continue;
+            } else {
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    y[k] = (VecU<DT>)(T)-INFINITY;
+                    if (v + k * LANES < v1) y[k] = __builtin_nontemporal_load((const VecU<DT>*)(body + (int64_t)(v + k * LANES) * E));
+                }
             }
-            float m = a.m;
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-#pragma unroll
-                for (int j = 0; j < E; ++j) m = fmaxf(m, (float)x[k][j]);
-            const float ref = row_ref(m);
-            row_rebase(a, m, ref, c);
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-                if (k < n)
-#pragma unroll
-                    for (int j = 0; j < E; ++j) row_add(a, (float)x[k][j], ref, c);
+            const int live = last ? (v1 - w + LANES - 1) / LANES : U;
+            row_add<DT>(a, y, live, last && has_edge ? (float)edge : -INFINITY, z.c);
+            if (last) break;
         }
-        // the elements before the first and after the last whole vector
-        const int64_t tail0 = head + nv * E;
-        const int nh = p == 0 ? (int)head : 0;
-        const int nt = p == P - 1 ? (int)(V - tail0) : 0;
-        if (tid < nh + nt) {
-            const float x = (float)row[tid < nh ? tid : tail0 + (tid - nh)];
-            const float m = fmaxf(a.m, x), ref = row_ref(m);
-            row_rebase(a, m, ref, c);
-            row_add(a, x, ref, c);
+        a = row_wave(a);
+        if (ROWS > 1) {
+            if (tid == 0) row_write(a, (float)xt, z, i, logp, lse, entropy);
+            continue;
         }
-        a = row_wave(a, c);
         if ((tid & 63) == 0) wave_state[tid >> 6] = a;
         __syncthreads();
-        if (tid == 0) {
-#pragma unroll
-            for (int w = 1; w < kRowWG / 64; ++w) a = row_merge(a, wave_state[w], c);
-            if (P == 1)
-                row_write(a, (float)row[t], inv_t, i, logp, lse, entropy);
-            else
-                parts[blk] = a;
+        if (tid < 64) {
+            a = tid < WAVES ? wave_state[tid] : RowState{0.0f, -INFINITY, 0.0f, 0.0f};
+            a = row_join<WAVES>(a, z.c);
+            if (tid == 0) {
+                if (P == 1)
+                    row_write(a, (float)xt, z, i, logp, lse, entropy);
+                else
+                    parts[i * P + p] = a;
+            }
         }
         __syncthreads();
     }
@@ -156,23 +246,23 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp(const typename Elem<DT>::
 
 // Joins a row's parts: one wave per row.
 template <int DT>
-__global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<DT>::T* __restrict__ logits,
-                                                            int64_t N, int64_t V, int64_t stride,
-                                                            const int64_t* __restrict__ targets, float inv_t,
-                                                            int P, float* __restrict__ logp,
+__global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
+                                                            int V, int64_t stride, const int64_t* __restrict__ targets,
+                                                            RowScale z, int P, float* __restrict__ logp,
                                                             float* __restrict__ lse, float* __restrict__ entropy,
                                                             const RowState* __restrict__ parts)
 {
-    const float c = inv_t * kLog2e;
+    const float c = z.c;
     const int lane = threadIdx.x & 63;
     const int64_t waves = (int64_t)gridDim.x * (kRowWG / 64);
     for (int64_t i = (int64_t)blockIdx.x * (kRowWG / 64) + (threadIdx.x >> 6); i < N; i += waves) {
         const int64_t t = targets[i];
         if (t < 0 || t >= V) continue;
-        RowState a = {-INFINITY, 0.0f, 0.0f};
+        const float xt = (float)logits[i * stride + t];
+        RowState a = {0.0f, -INFINITY, 0.0f, 0.0f};
         for (int p = lane; p < P; p += 64) a = row_merge(a, parts[i * P + p], c);
-        a = row_wave(a, c);
-        if (lane == 0) row_write(a, (float)logits[i * stride + t], inv_t, i, logp, lse, entropy);
+        a = row_join<64>(a, c);
+        if (lane == 0) row_write(a, xt, z, i, logp, lse, entropy);
     }
 }
 
@@ -239,19 +329,34 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
     }
 }
 
-// Parts of a row: enough workgroups for the chip, at least 16 KB each.
-static inline int row_parts(int64_t N, int64_t V)
+// How rows are shared out: a wave each (wg = 64), a workgroup of wg threads
+// each, or P such workgroups each.
+struct RowShape {
+    int wg, P;
+};
+
+// Measured (bf16, us, a wave / 256 / 1024 threads a row / 256 threads in parts):
+//   300 x 1000: 3.4 / 4.0 / 6.4;  4096 x 16000: 27 / 30 / 64;  2048 x 32000:
+//   26.5 / 28.3 / 46;  3072 x 65536: 78 / 70 / 103;  1024 x 16000: 13.0 / 11.7 / 18;
+//   512 x 16000: 11.5 / 7.8 / 9.5;  256 x 32000: 17.8 / 8.7 / 7.5;  128 x 65536:
+//   32 / 11.8 / 9.1 / 9.9;  64 x 131072: 59 / 19 / 12.5 / 9.9;  1 x 65536: 25 / 10 /
+//   7.8 / 5.2;  1 x 262144: 105 / 31 / 18 / 6.3.
+// Parts cost a second launch, so a row of up to 128 KB stays with one workgroup.
+static inline RowShape row_shape(int64_t N, int64_t V, int bytes)
 {
-    const int64_t want = (1024 + N - 1) / N;
-    const int64_t most = V / 8192;
-    const int64_t p = want < most ? want : most;
-    return p < 1 ? 1 : p > 64 ? 64 : (int)p;
+    const int64_t row = V * bytes;
+    if (row <= 4096 || (N >= 2048 && row <= 65536)) return {64, 1};
+    if (row > 131072 && N <= 64) {
+        const int64_t want = 1024 / N, most = row / 8192;
+        return {256, (int)(want < most ? want : most)};
+    }
+    return {N <= 256 ? 1024 : 256, 1};
 }
 
 static inline bool rows_ok(int32_t dtype, int64_t N, int64_t V, int64_t stride, float inv_t)
 {
     return (dtype == SF_F32 || dtype == SF_BF16 || dtype == SF_F16) && N >= 0 && V >= 1 &&
-           V <= ((int64_t)1 << 30) && stride >= V && inv_t > 0.0f && inv_t <= kF32Max &&
+           V <= ((int64_t)1 << 30) && stride >= V && inv_t > 0.0f && inv_t <= 0x1p100f &&
            (N == 0 || stride <= (((int64_t)1 << 56) / N));
 }
 
@@ -265,7 +370,11 @@ SF_API int64_t sf_token_logp_workspace(int64_t N, int64_t V)
 {
     if (N < 0 || V < 1 || V > ((int64_t)1 << 30) || N > ((int64_t)1 << 56)) return -1;
     if (N == 0) return 0;
-    const int P = row_parts(N, V);
+    int P = 1;
+    for (int b = 2; b <= 4; b += 2) {
+        const int p = row_shape(N, V, b).P;
+        P = p > P ? p : P;
+    }
     return P == 1 ? 0 : N * P * (int64_t)sizeof(RowState);
 }
 
@@ -291,16 +400,28 @@ SF_API int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V
         for (int b = a + 1; b < 4; ++b)
             if (sizes[b] > 0 && !disjoint(outs[a], sizes[a], outs[b], sizes[b])) return SF_EINVAL;
     }
-    int P = row_parts(N, V);
-    void* args[] = {(void*)&logits,   (void*)&N,       (void*)&V,           (void*)&row_stride,
-                    (void*)&targets,  (void*)&inv_temperature, (void*)&P,   (void*)&out_logp,
-                    (void*)&out_lse,  (void*)&out_entropy,     (void*)&workspace};
-    const void* fn[3] = {(const void*)&k_token_logp<SF_F32>, (const void*)&k_token_logp<SF_BF16>,
-                         (const void*)&k_token_logp<SF_F16>};
+    const RowShape shape = row_shape(N, V, elem_size(dtype));
+    int P = shape.P, Vi = (int)V;
+    int share = (Vi / (16 / elem_size(dtype)) + P - 1) / P;
+    RowScale z;
+    z.inv_t = inv_temperature;
+    z.c = (float)((double)inv_temperature * kLog2eD);
+    z.eps = (float)(((double)inv_temperature * kLog2eD - (double)z.c) / (double)z.c);
+    void* args[] = {(void*)&logits, (void*)&N,     (void*)&Vi,       (void*)&row_stride, (void*)&targets,    (void*)&z,
+                    (void*)&share,  (void*)&out_logp, (void*)&out_lse, (void*)&out_entropy, (void*)&workspace};
+    const void* fn[3][3] = {{(const void*)&k_token_logp<SF_F32, 256, 1>, (const void*)&k_token_logp<SF_BF16, 256, 1>,
+                             (const void*)&k_token_logp<SF_F16, 256, 1>},
+                            {(const void*)&k_token_logp<SF_F32, 256, 4>, (const void*)&k_token_logp<SF_BF16, 256, 4>,
+                             (const void*)&k_token_logp<SF_F16, 256, 4>},
+                            {(const void*)&k_token_logp<SF_F32, 1024, 16>, (const void*)&k_token_logp<SF_BF16, 1024, 16>,
+                             (const void*)&k_token_logp<SF_F16, 1024, 16>}};
+    const int rows = shape.wg == 64 ? 4 : 1;
+    const int rc = launch(fn[shape.wg == 64 ? 0 : shape.wg == 256 ? 1 : 2][dtype], dim3(grid_of((N + rows - 1) / rows), P),
+                          dim3(shape.wg == 64 ? 256 : shape.wg), args, 0, stream);
+    if (rc != SF_OK || P == 1) return rc;
     const void* join[3] = {(const void*)&k_token_logp_join<SF_F32>, (const void*)&k_token_logp_join<SF_BF16>,
                            (const void*)&k_token_logp_join<SF_F16>};
-    const int rc = launch(fn[dtype], dim3(grid_of(N * P)), dim3(kRowWG), args, 0, stream);
-    if (rc != SF_OK || P == 1) return rc;
+    args[6] = (void*)&P;
     return launch(join[dtype], dim3(grid_of((N + kRowWG / 64 - 1) / (kRowWG / 64))), dim3(kRowWG), args, 0, stream);
 }
 
