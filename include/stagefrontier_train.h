@@ -54,7 +54,7 @@ enum {
  *   out_logp         [N] float.
  *   out_lse          [N] float.
  *   out_entropy      [N] float, or NULL where the entropy is not wanted.
- *   workspace        sf_token_logp_workspace(N, V) bytes, 16-byte aligned;
+ *   workspace        sf_token_logp_workspace(dtype, N, V) bytes, 16-byte aligned;
  *                    may be NULL where that is 0.
  *
  * Logits of -inf have probability 0.  A row of nothing else has no
@@ -67,9 +67,9 @@ int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V, int64
                   sf_stream_t stream);
 
 /* sf_token_logp_workspace -- bytes that sf_token_logp needs for N rows of V
- * logits (0 where every row is one workgroup's), -1 where N or V is out of
- * range.  Host only. */
-int64_t sf_token_logp_workspace(int64_t N, int64_t V);
+ * logits of a type (0 where every row is one workgroup's), -1 where an argument
+ * is out of range.  Host only. */
+int64_t sf_token_logp_workspace(int32_t dtype, int64_t N, int64_t V);
 
 /*
  * sf_token_logp_grad -- the gradient of sf_token_logp's outputs back to the
@@ -136,7 +136,8 @@ enum {
  *   kl_coef          finite.
  *   out_terms        [4] float.
  *   out_grad         [N] float.
- *   workspace        sf_policy_loss_workspace(N, B) bytes, 16-byte aligned.
+ *   workspace        sf_policy_loss_workspace(N, B) bytes, 16-byte aligned;
+ *                    may be NULL where that is 0 (small inputs).
  *
  * With nothing taking part the terms and the gradient are 0.  Returns SF_OK,
  * SF_EINVAL or SF_EHIP.

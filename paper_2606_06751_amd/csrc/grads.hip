@@ -21,13 +21,14 @@ constexpr int kNormBatch = 192;  // tensors per launch: 20 bytes each of 4 KB of
 constexpr int kClipBatch = 128;  // 28 bytes each
 constexpr uint64_t kListMagic = 0x7366677261643031ull;
 constexpr int64_t kGradMax = (int64_t)1 << 40;
+constexpr int64_t kChunkMax = 1 << 16, kChunkWant = 4096;
+constexpr int64_t kClipChunk = 8192;
 
 struct GradItem {
     uintptr_t ptr;
     int64_t numel;
-    int32_t dtype;
-    int32_t pad;
-    int64_t first;  // index of its first chunk in the list
+    int64_t dtype;
+    int64_t first, clip_first;  // index of its first chunk in the list, for the norm and the clip
 };
 struct GradSpan {
     uintptr_t lo, hi;
@@ -37,8 +38,10 @@ struct GradList {
     uint64_t magic;
     int32_t n;
     int32_t overlaps;  // some two of its tensors overlap
-    int64_t chunk;     // elements
+    int64_t chunk;     // elements, for the norm
     int64_t chunks;
+    int64_t most;      // chunks of a tensor, at most
+    int64_t clip_chunks;
     const GradItem* items() const { return reinterpret_cast<const GradItem*>(this + 1); }
     const GradSpan* spans() const { return reinterpret_cast<const GradSpan*>(items() + n); }
 };
@@ -75,33 +78,45 @@ __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x)
 
 // Sum of squares of a chunk in 64 bits; a thread whose own sum is not finite
 // (no finite input makes it so) reads its elements again and counts.
+constexpr int kNormU = 4;  // vectors per lane in flight
+
 template <int DT>
-__device__ __forceinline__ void chunk_norm(const typename Elem<DT>::T* p, int64_t n, double* sum, int64_t* wrong)
+__device__ __forceinline__ void chunk_norm(uintptr_t at, int n, double* sum, int64_t* wrong)
 {
     constexpr int E = kVec<DT>;
+    constexpr int U = kNormU;
     const int tid = threadIdx.x;
-    const int64_t head = head_elems<DT>(p, n);
-    const int64_t nv = (n - head) / E, tail0 = head + nv * E;
-    const typename Elem<DT>::T* body = p + head;
+    const GlobalElem<DT>* p = (const GlobalElem<DT>*)at;
+    const int head = (int)head_elems<DT>((const void*)at, n);
+    const int nv = (n - head) / E, tail0 = head + nv * E;
+    const GlobalVec<DT>* body = (const GlobalVec<DT>*)(p + head);
     double s = 0.0;
-    for (int64_t v = tid; v < nv; v += kGradWG) {
-        const VecU<DT> x = *(const VecU<DT>*)(body + v * E);
+    auto add = [&](const VecU<DT>& x) {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const double y = (double)(float)x[j];
             s = fma(y, y, s);
         }
+    };
+    int v = tid;
+    for (; v + (U - 1) * kGradWG < nv; v += U * kGradWG) {
+        VecU<DT> x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) x[k] = __builtin_nontemporal_load(body + v + k * kGradWG);
+#pragma unroll
+        for (int k = 0; k < U; ++k) add(x[k]);
     }
-    const int64_t j = tid < head ? tid : tail0 + (tid - head);
+    for (; v < nv; v += kGradWG) add(__builtin_nontemporal_load(body + v));
     const bool edge = tid < head + (n - tail0);
+    const int j = tid < head ? tid : tail0 + (tid - head);
     if (edge) {
         const double y = (double)(float)p[j];
         s = fma(y, y, s);
     }
     int64_t w = 0;
     if (!(s < (double)INFINITY)) {
-        for (int64_t v = tid; v < nv; v += kGradWG) {
-            const VecU<DT> x = *(const VecU<DT>*)(body + v * E);
+        for (v = tid; v < nv; v += kGradWG) {
+            const VecU<DT> x = body[v];
             for (int i = 0; i < E; ++i) w += not_finite((float)x[i]);
         }
         if (edge) w += not_finite((float)p[j]);
@@ -112,33 +127,32 @@ __device__ __forceinline__ void chunk_norm(const typename Elem<DT>::T* p, int64_
 
 __global__ __launch_bounds__(kGradWG) void k_grad_norm(NormArgs a, int n, int64_t chunk, int64_t base,
                                                        int64_t item0, Partial* __restrict__ partial,
-                                                       uint32_t* __restrict__ table, uint32_t* __restrict__ done)
+                                                       uint32_t* __restrict__ table)
 {
     __shared__ double sums[kGradWG / 64];
     __shared__ int64_t wrongs[kGradWG / 64];
     const int tid = threadIdx.x;
     const uint32_t b = blockIdx.x;
     if (b == 0) {
-        // where each tensor's chunks begin, and the join's counter
+        // where each tensor's chunks begin, for the join
         for (int i = tid; i <= n; i += kGradWG) table[item0 + i] = (uint32_t)(base + a.first[i]);
-        if (item0 == 0 && tid == 0) *done = 0;
     }
     if (b >= a.first[n]) return;
     const int i = find_item<kNormBatch>(a.first, b);
     const int64_t count = a.numel[i] >> 2;
     const int dtype = (int)(a.numel[i] & 3);
     const int64_t e0 = (int64_t)(b - a.first[i]) * chunk;
-    const int64_t len = count - e0 < chunk ? count - e0 : chunk;
+    const int len = (int)(count - e0 < chunk ? count - e0 : chunk);
     double s;
     int64_t w;
     if (dtype == SF_F32)
-        chunk_norm<SF_F32>((const float*)a.ptr[i] + e0, len, &s, &w);
+        chunk_norm<SF_F32>(a.ptr[i] + e0 * 4, len, &s, &w);
     else if (dtype == SF_BF16)
-        chunk_norm<SF_BF16>((const __bf16*)a.ptr[i] + e0, len, &s, &w);
+        chunk_norm<SF_BF16>(a.ptr[i] + e0 * 2, len, &s, &w);
     else
-        chunk_norm<SF_F16>((const _Float16*)a.ptr[i] + e0, len, &s, &w);
+        chunk_norm<SF_F16>(a.ptr[i] + e0 * 2, len, &s, &w);
     s = wave_sum_f64(s);
-    w = wave_sum64(w);
+    w = wave_sum_i64(w);
     if ((tid & 63) == 0) {
         sums[tid >> 6] = s;
         wrongs[tid >> 6] = w;
@@ -153,74 +167,139 @@ __global__ __launch_bounds__(kGradWG) void k_grad_norm(NormArgs a, int n, int64_
     }
 }
 
-// One wave per tensor adds its chunks' sums in order; the workgroup that
-// finishes last adds the tensors'.
-__global__ __launch_bounds__(kGradWG) void k_grad_norm_join(int64_t n, const Partial* __restrict__ partial,
-                                                            const uint32_t* __restrict__ table, double* squares,
-                                                            uint32_t* done, float* __restrict__ norms,
-                                                            float* __restrict__ total,
+// Joins, in a fixed order.  Few tensors of few chunks: one workgroup for all,
+// 16 lanes a tensor, and one launch.
+constexpr int kJoinWG = 1024;
+constexpr int kJoinLanes = 16;
+constexpr int kJoinItems = kJoinWG;  // at most
+constexpr int kJoinChunks = 16 * kJoinLanes;  // of a tensor, at most
+
+__global__ __launch_bounds__(kJoinWG) void k_grad_norm_join(int n, const Partial* __restrict__ partial,
+                                                            const uint32_t* __restrict__ table,
+                                                            float* __restrict__ norms, float* __restrict__ total,
                                                             int64_t* __restrict__ nonfinite)
 {
-    __shared__ double sums[kGradWG / 64];
-    __shared__ bool last;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t i = (int64_t)blockIdx.x * (kGradWG / 64) + (tid >> 6);
-    if (i < n) {
+    __shared__ double squares[kJoinItems];
+    __shared__ double sums[kJoinWG / 64];
+    const int tid = threadIdx.x, lane = tid & (kJoinLanes - 1);
+    for (int i = tid / kJoinLanes; i < n; i += kJoinWG / kJoinLanes) {
         double s = 0.0;
         int64_t w = 0;
-        for (uint32_t k = table[i] + lane; k < table[i + 1]; k += 64) {
+        const uint32_t end = table[i + 1];
+        for (uint32_t k = table[i] + lane; k < end; k += kJoinLanes) {
             s += partial[k].sum;
             w += partial[k].wrong;
         }
-        s = wave_sum_f64(s);
-        w = wave_sum64(w);
+        for (int off = kJoinLanes / 2; off > 0; off >>= 1) {
+            s += __shfl_xor(s, off, kJoinLanes);
+            w += __shfl_xor(w, off, kJoinLanes);
+        }
         if (lane == 0) {
             norms[i] = (float)sqrt(s);
             nonfinite[i] = w;
             squares[i] = s;
         }
     }
-    __threadfence();
     __syncthreads();
-    if (tid == 0) last = atomicAdd(done, 1u) == gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double s = 0.0;
-    for (int64_t k = tid; k < n; k += kGradWG) s += squares[k];
+    double s = tid < n ? squares[tid] : 0.0;
     s = wave_sum_f64(s);
-    if (lane == 0) sums[tid >> 6] = s;
+    if ((tid & 63) == 0) sums[tid >> 6] = s;
     __syncthreads();
     if (tid == 0) {
-        for (int k = 1; k < kGradWG / 64; ++k) s += sums[k];
+        for (int k = 1; k < kJoinWG / 64; ++k) s += sums[k];
+        *total = (float)sqrt(s);
+    }
+}
+
+// Else a workgroup per tensor, and one for all of them.
+__global__ __launch_bounds__(kGradWG) void k_grad_norm_item(const Partial* __restrict__ partial,
+                                                            const uint32_t* __restrict__ table,
+                                                            double* __restrict__ squares, float* __restrict__ norms,
+                                                            int64_t* __restrict__ nonfinite)
+{
+    __shared__ double sums[kGradWG / 64];
+    __shared__ int64_t wrongs[kGradWG / 64];
+    const int tid = threadIdx.x, i = blockIdx.x;
+    double s = 0.0;
+    int64_t w = 0;
+    const uint32_t end = table[i + 1];
+    for (uint32_t k = table[i] + tid; k < end; k += kGradWG) {
+        s += partial[k].sum;
+        w += partial[k].wrong;
+    }
+    s = wave_sum_f64(s);
+    w = wave_sum_i64(w);
+    if ((tid & 63) == 0) {
+        sums[tid >> 6] = s;
+        wrongs[tid >> 6] = w;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kGradWG / 64; ++k) {
+            s += sums[k];
+            w += wrongs[k];
+        }
+        norms[i] = (float)sqrt(s);
+        nonfinite[i] = w;
+        squares[i] = s;
+    }
+}
+
+__global__ __launch_bounds__(kJoinWG) void k_grad_norm_total(int n, const double* __restrict__ squares,
+                                                             float* __restrict__ total)
+{
+    __shared__ double sums[kJoinWG / 64];
+    const int tid = threadIdx.x;
+    double s = 0.0;
+    for (int k = tid; k < n; k += kJoinWG) s += squares[k];
+    s = wave_sum_f64(s);
+    if ((tid & 63) == 0) sums[tid >> 6] = s;
+    __syncthreads();
+    if (tid == 0) {
+        for (int k = 1; k < kJoinWG / 64; ++k) s += sums[k];
         *total = (float)sqrt(s);
     }
 }
 
 __global__ void k_grad_norm_empty(float* total) { *total = 0.0f; }
 
+constexpr int kClipU = 4;
+#define CLIP_LOAD(p) __builtin_nontemporal_load(p)
+#define CLIP_STORE(v,p) __builtin_nontemporal_store(v,p)
 template <int DT>
-__device__ __forceinline__ void chunk_scale(const typename Elem<DT>::T* p, typename Elem<DT>::T* o, int64_t n,
-                                            float c)
+__device__ __forceinline__ void chunk_scale(uintptr_t from, uintptr_t to, int n, float c)
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
+    constexpr int U = kClipU;
     const int tid = threadIdx.x;
-    const int64_t head = head_elems<DT>(o, n);
-    const int64_t nv = (n - head) / E, tail0 = head + nv * E;
-    for (int64_t v = tid; v < nv; v += kGradWG) {
-        VecU<DT> x = *(const VecU<DT>*)(p + head + v * E);
+    const GlobalElem<DT>* p = (const GlobalElem<DT>*)from;
+    GlobalElem<DT>* o = (GlobalElem<DT>*)to;
+    const int head = (int)head_elems<DT>((const void*)to, n);
+    const int nv = (n - head) / E, tail0 = head + nv * E;
+    const GlobalVec<DT>* pv = (const GlobalVec<DT>*)(p + head);
+    GlobalVec<DT>* ov = (GlobalVec<DT>*)(o + head);
+    auto scale = [&](VecU<DT> x) {
 #pragma unroll
         for (int j = 0; j < E; ++j) x[j] = (T)((float)x[j] * c);
-        *(VecU<DT>*)(o + head + v * E) = x;
+        return x;
+    };
+    int v = tid;
+    for (; v + (U - 1) * kGradWG < nv; v += U * kGradWG) {
+        VecU<DT> x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) x[k] = CLIP_LOAD(pv + v + k * kGradWG);
+#pragma unroll
+        for (int k = 0; k < U; ++k) CLIP_STORE(scale(x[k]), ov + v + k * kGradWG);
     }
+    for (; v < nv; v += kGradWG) ov[v] = scale(pv[v]);
     if (tid < head + (n - tail0)) {
-        const int64_t j = tid < head ? tid : tail0 + (tid - head);
+        const int j = tid < head ? tid : tail0 + (tid - head);
         o[j] = (T)((float)p[j] * c);
     }
 }
 
-__global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int64_t chunk, int in_place,
+__global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int in_place,
                                                        const float* __restrict__ norms, int64_t m, float max_norm,
                                                        float eps, uint32_t* status)
 {
@@ -229,14 +308,19 @@ __global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int64_
     const uint32_t b = blockIdx.x;
     // the norm of all parts, every workgroup for itself
     double s = 0.0;
-    for (int64_t k = tid; k < m; k += kGradWG) s = fma((double)norms[k], (double)norms[k], s);
-    s = wave_sum_f64(s);
-    if ((tid & 63) == 0) sums[tid >> 6] = s;
-    __syncthreads();
-    s = 0.0;
-    for (int k = 0; k < kGradWG / 64; ++k) s += sums[k];
+    if (m == 1) {
+        s = fabs((double)norms[0]);
+    } else {
+        for (int64_t k = tid; k < m; k += kGradWG) s = fma((double)norms[k], (double)norms[k], s);
+        s = wave_sum_f64(s);
+        if ((tid & 63) == 0) sums[tid >> 6] = s;
+        __syncthreads();
+        s = 0.0;
+        for (int k = 0; k < kGradWG / 64; ++k) s += sums[k];
+        s = sqrt(s);
+    }
     const bool wrong = !(s < (double)INFINITY);
-    const double c = (double)max_norm / (sqrt(s) + (double)eps);
+    const double c = (double)max_norm / (s + (double)eps);
     const float coef = wrong || !(c < 1.0) ? 1.0f : (float)c;
     if (wrong && status && b == 0 && tid == 0) atomicOr(status, (uint32_t)SF_ERANGE);
     if (coef == 1.0f && in_place) return;
@@ -244,14 +328,14 @@ __global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int64_
     const int i = find_item<kClipBatch>(a.first, b);
     const int64_t count = a.numel[i] >> 2;
     const int dtype = (int)(a.numel[i] & 3);
-    const int64_t e0 = (int64_t)(b - a.first[i]) * chunk;
-    const int64_t len = count - e0 < chunk ? count - e0 : chunk;
+    const int64_t e0 = (int64_t)(b - a.first[i]) * kClipChunk;
+    const int len = (int)(count - e0 < kClipChunk ? count - e0 : kClipChunk);
     if (dtype == SF_F32)
-        chunk_scale<SF_F32>((const float*)a.ptr[i] + e0, (float*)a.out[i] + e0, len, coef);
+        chunk_scale<SF_F32>(a.ptr[i] + e0 * 4, a.out[i] + e0 * 4, len, coef);
     else if (dtype == SF_BF16)
-        chunk_scale<SF_BF16>((const __bf16*)a.ptr[i] + e0, (__bf16*)a.out[i] + e0, len, coef);
+        chunk_scale<SF_BF16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
     else
-        chunk_scale<SF_F16>((const _Float16*)a.ptr[i] + e0, (_Float16*)a.out[i] + e0, len, coef);
+        chunk_scale<SF_F16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
 }
 
 static inline const GradList* as_list(const void* p)
@@ -271,7 +355,7 @@ static bool clear_of(const GradList* l, const void* p, int64_t bytes)
 }
 
 struct NormLayout {
-    int64_t squares, table, done, bytes;  // offsets; the chunks' sums come first
+    int64_t squares, table, bytes;  // offsets; the chunks' sums come first
 };
 
 static NormLayout norm_layout(const GradList* l)
@@ -279,8 +363,7 @@ static NormLayout norm_layout(const GradList* l)
     NormLayout w;
     w.squares = l->chunks * (int64_t)sizeof(Partial);
     w.table = w.squares + (int64_t)l->n * 8;
-    w.done = w.table + ((int64_t)l->n + 1) * 4;
-    w.bytes = (w.done + 4 + 15) & ~(int64_t)15;
+    w.bytes = (w.table + ((int64_t)l->n + 1) * 4 + 15) & ~(int64_t)15;
     return w;
 }
 
@@ -306,26 +389,32 @@ SF_API int sf_grad_list_init(void* list, int64_t list_bytes, const void* const* 
         if (numel[i] > 0 && (!grads[i] || !aligned(grads[i], elem_size(dtype[i])))) return SF_EINVAL;
         total += numel[i];
     }
-    // Chunks of 2 K to 1 M elements, about 4096 of them: enough to fill the
-    // chip, and few enough that their sums cost little to add up.
-    int64_t chunk = 2048;
-    while (chunk < (1 << 20) && chunk * 4096 < total) chunk *= 2;
-    int64_t chunks = 0;
-    for (int32_t i = 0; i < n; ++i) chunks += (numel[i] + chunk - 1) / chunk;
+    int64_t chunk = 4096;
+    while (chunk < kChunkMax && chunk * kChunkWant < total) chunk *= 2;
+    int64_t chunks = 0, most = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const int64_t c = (numel[i] + chunk - 1) / chunk;
+        chunks += c;
+        most = c > most ? c : most;
+    }
     if (chunks > INT32_MAX) return SF_EINVAL;
     GradList* l = new (list) GradList;
     l->magic = 0;
     l->n = n;
     l->chunk = chunk;
     l->chunks = chunks;
+    l->most = most;
     GradItem* items = reinterpret_cast<GradItem*>(l + 1);
     GradSpan* spans = reinterpret_cast<GradSpan*>(items + n);
-    int64_t at = 0;
+    int64_t at = 0, clip_at = 0;
     for (int32_t i = 0; i < n; ++i) {
-        items[i] = {(uintptr_t)grads[i], numel[i], dtype[i], 0, at};
+        items[i] = {(uintptr_t)grads[i], numel[i], dtype[i], at, clip_at};
         spans[i] = {(uintptr_t)grads[i], (uintptr_t)grads[i] + (uintptr_t)(numel[i] * elem_size(dtype[i]))};
         at += (numel[i] + chunk - 1) / chunk;
+        clip_at += (numel[i] + kClipChunk - 1) / kClipChunk;
     }
+    if (clip_at > INT32_MAX) return SF_EINVAL;
+    l->clip_chunks = clip_at;
     std::sort(spans, spans + n, [](const GradSpan& x, const GradSpan& y) { return x.lo != y.lo ? x.lo < y.lo : x.hi < y.hi; });
     l->overlaps = 0;
     uintptr_t end = 0;
@@ -367,12 +456,12 @@ SF_API int sf_grad_norm(const void* list, float* out_norms, float* out_total, in
     Partial* partial = (Partial*)workspace;
     double* squares = (double*)((char*)workspace + w.squares);
     uint32_t* table = (uint32_t*)((char*)workspace + w.table);
-    uint32_t* done = (uint32_t*)((char*)workspace + w.done);
     int64_t chunk = l->chunk;
     const GradItem* items = l->items();
-    for (int64_t i0 = 0; i0 < n; i0 += kNormBatch) {
+    const int64_t batches = (n + kNormBatch - 1) / kNormBatch, each = (n + batches - 1) / batches;
+    for (int64_t i0 = 0; i0 < n; i0 += each) {
         NormArgs a;
-        int m = (int)(n - i0 < kNormBatch ? n - i0 : kNormBatch);
+        int m = (int)(n - i0 < each ? n - i0 : each);
         int64_t base = items[i0].first;
         const int64_t stop = i0 + m < n ? items[i0 + m].first : l->chunks;
         for (int k = 0; k < kNormBatch; ++k) {
@@ -383,15 +472,21 @@ SF_API int sf_grad_norm(const void* list, float* out_norms, float* out_total, in
         a.first[kNormBatch] = (uint32_t)(stop - base);
         const unsigned grid = stop > base ? (unsigned)(stop - base) : 1;
         void* args[] = {(void*)&a,  (void*)&m,       (void*)&chunk, (void*)&base,
-                        (void*)&i0, (void*)&partial, (void*)&table, (void*)&done};
+                        (void*)&i0, (void*)&partial, (void*)&table};
         const int rc = launch((const void*)&k_grad_norm, dim3(grid), dim3(kGradWG), args, 0, stream);
         if (rc != SF_OK) return rc;
     }
-    int64_t nn = n;
-    void* args[] = {(void*)&nn,   (void*)&partial,   (void*)&table,     (void*)&squares,
-                    (void*)&done, (void*)&out_norms, (void*)&out_total, (void*)&out_nonfinite};
-    return launch((const void*)&k_grad_norm_join, dim3((unsigned)((n + kGradWG / 64 - 1) / (kGradWG / 64))),
-                  dim3(kGradWG), args, 0, stream);
+    int nn = l->n;
+    if (nn <= kJoinItems && l->most <= kJoinChunks) {
+        void* args[] = {(void*)&nn,        (void*)&partial,   (void*)&table,
+                        (void*)&out_norms, (void*)&out_total, (void*)&out_nonfinite};
+        return launch((const void*)&k_grad_norm_join, dim3(1), dim3(kJoinWG), args, 0, stream);
+    }
+    void* args[] = {(void*)&partial, (void*)&table, (void*)&squares, (void*)&out_norms, (void*)&out_nonfinite};
+    const int rc = launch((const void*)&k_grad_norm_item, dim3((unsigned)n), dim3(kGradWG), args, 0, stream);
+    if (rc != SF_OK) return rc;
+    void* targs[] = {(void*)&nn, (void*)&squares, (void*)&out_total};
+    return launch((const void*)&k_grad_norm_total, dim3(1), dim3(kJoinWG), targs, 0, stream);
 }
 
 SF_API int sf_grad_clip(const void* list, const void* out_list, const float* norms, int64_t m, float max_norm,
@@ -432,21 +527,21 @@ SF_API int sf_grad_clip(const void* list, const void* out_list, const float* nor
             }
         }
     }
-    int64_t chunk = l->chunk;
-    for (int64_t i0 = 0; i0 < n; i0 += kClipBatch) {
+    const int64_t batches = (n + kClipBatch - 1) / kClipBatch, each = n > 0 ? (n + batches - 1) / batches : 1;
+    for (int64_t i0 = 0; i0 < n; i0 += each) {
         ClipArgs a;
-        int k1 = (int)(n - i0 < kClipBatch ? n - i0 : kClipBatch);
-        const int64_t base = in[i0].first;
-        const int64_t stop = i0 + k1 < n ? in[i0 + k1].first : l->chunks;
+        int k1 = (int)(n - i0 < each ? n - i0 : each);
+        const int64_t base = in[i0].clip_first;
+        const int64_t stop = i0 + k1 < n ? in[i0 + k1].clip_first : l->clip_chunks;
         for (int k = 0; k < kClipBatch; ++k) {
             a.ptr[k] = k < k1 ? in[i0 + k].ptr : 0;
             a.out[k] = k < k1 ? out[i0 + k].ptr : 0;
             a.numel[k] = k < k1 ? in[i0 + k].numel << 2 | in[i0 + k].dtype : 0;
-            a.first[k] = (uint32_t)((k < k1 ? in[i0 + k].first : stop) - base);
+            a.first[k] = (uint32_t)((k < k1 ? in[i0 + k].clip_first : stop) - base);
         }
         a.first[kClipBatch] = (uint32_t)(stop - base);
         const unsigned grid = stop > base ? (unsigned)(stop - base) : 1;
-        void* args[] = {(void*)&a,     (void*)&k1, (void*)&chunk,    (void*)&same, (void*)&norms,
+        void* args[] = {(void*)&a,     (void*)&k1, (void*)&same, (void*)&norms,
                         (void*)&m,     (void*)&max_norm, (void*)&eps, (void*)&status};
         const int rc = launch((const void*)&k_grad_clip, dim3(grid), dim3(kGradWG), args, 0, stream);
         if (rc != SF_OK) return rc;

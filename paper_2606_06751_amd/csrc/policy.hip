@@ -2,9 +2,21 @@
 // its gradient (sf_policy_loss).
 //
 // A token's terms depend on its own inputs, its sequence's advantage and the
-// reduction's weight.  The weights come first (how many tokens take part, in
-// all or per sequence), then one pass over the tokens writes the gradient and
-// a workgroup's sums, which a last workgroup adds up in their order.
+// reduction's weight, which needs to know how many tokens take part (in all or
+// per sequence) before the first gradient is written.  So the mask is counted
+// first, with one byte a token; then one pass over the tokens writes the
+// gradient and a workgroup's sums, which one workgroup adds up in their order.
+// Small inputs take one workgroup and one launch.
+//
+// What bounds it is the number of instructions as much as the bytes: some 75
+// a token, and two exponentials at a quarter of the VALU's rate.  So a lane takes
+// 4 consecutive tokens (16-byte loads) and a wave 256 a round, which are mostly
+// of one sequence: it is found once, in LDS, and followed; only in a round that
+// meets another does each lane look for its own (64 tokens a round: 31.7 us for
+// 2e6 tokens of 1024 sequences, 256: 15.6; the kernel alone).  A loop over
+// rounds, not unrolled, keeps the code short, which small inputs wait for.  The
+// sums go to a launch of their own: a counter of finished workgroups with the
+// memory fences that it needs cost 25 us more.
 
 #include "sf_device.h"
 #include "sf_host.h"
@@ -13,10 +25,21 @@
 namespace sfk {
 
 constexpr int kPolicyWG = 256;
-constexpr int kPolicyTok = 4;                          // tokens per thread
-constexpr int64_t kPolicyChunk = kPolicyWG * kPolicyTok;  // tokens per workgroup
-constexpr int kJoinWG = 1024;
+constexpr int kTok = 4;                 // consecutive tokens of a lane: 16-byte loads
+constexpr int kRoundTok = 64 * kTok;    // of a wave's round
+constexpr int kWaveTok = 2 * kRoundTok;  // of a wave
+constexpr int kPolicyChunk = kPolicyWG / 64 * kWaveTok;  // of a workgroup
+constexpr int kSliceMax = 2048;  // sequences that a workgroup keeps in LDS
+constexpr int kFewSeqs = 1024;   // sequences of which every workgroup keeps all
+constexpr int kCountMax = 2048;  // counts that every workgroup adds up by itself
+constexpr int kCountBlocks = 512;
+constexpr int kSmallWG = 1024;
+constexpr int kSmallRounds = 2;
+constexpr int kSmallN = kSmallWG * kTok * kSmallRounds;  // tokens of the one-launch path
+constexpr int kJoinWG = 512;
+constexpr int kFar = INT32_MAX;
 
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 struct Policy {
@@ -35,11 +58,10 @@ struct Policy {
 
 __device__ __forceinline__ int64_t clamp_tok(int64_t x, int64_t N) { return x < 0 ? 0 : x > N ? N : x; }
 
-// Sequence that holds token t, or -1: the last one that starts at or before t,
-// where it also ends after t.
-__device__ __forceinline__ int64_t find_seq(const int64_t* start, int64_t B, int64_t t)
+// Index of the first of n ascending starts that lies past t.
+__device__ __forceinline__ int64_t find_start(const int64_t* start, int64_t n, int64_t t)
 {
-    int64_t lo = 0, hi = B + 1;  // first index whose start lies past t
+    int64_t lo = 0, hi = n;
     while (lo < hi) {
         const int64_t mid = (lo + hi) >> 1;
         if (start[mid] <= t)
@@ -47,62 +69,82 @@ __device__ __forceinline__ int64_t find_seq(const int64_t* start, int64_t B, int
         else
             hi = mid;
     }
-    return lo >= 1 && lo <= B ? lo - 1 : -1;
+    return lo;
 }
 
-// Tokens that take part: part p of P of sequence b, by one wave.
-__global__ __launch_bounds__(kPolicyWG) void k_policy_count(Policy a, int P, int64_t* __restrict__ counts)
+// Tokens of [t0, t1) that take part, by one wave: 16 mask bytes a lane at a time.
+__device__ __forceinline__ int64_t count_mask(const uint8_t* mask, int64_t t0, int64_t t1)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t waves = (int64_t)gridDim.x * (kPolicyWG / 64);
-    for (int64_t w = (int64_t)blockIdx.x * (kPolicyWG / 64) + (threadIdx.x >> 6); w < a.B * P; w += waves) {
-        const int64_t b = w / P, p = w - b * P;
-        const int64_t s0 = clamp_tok(a.start[b], a.N), s1 = clamp_tok(a.start[b + 1], a.N);
-        const int64_t len = s1 > s0 ? s1 - s0 : 0;
-        const int64_t t0 = s0 + len * p / P, t1 = s0 + len * (p + 1) / P;
-        int64_t n = 0;
-        if (a.mask)
-            for (int64_t t = t0 + lane; t < t1; t += 64) n += a.mask[t] != 0;
-        else
-            n = lane == 0 ? t1 - t0 : 0;
-        n = wave_sum64(n);
-        if (lane == 0) counts[w] = n;
+    int64_t n = 0;
+    int64_t body = t0 + (int64_t)((0 - (uintptr_t)(mask + t0)) & 15);
+    if (body > t1) body = t1;
+    const int64_t nv = (t1 - body) >> 4, tail = body + (nv << 4);
+    const uint4* v = (const uint4*)(mask + body);
+    // one bit a byte that is not 0
+    auto bits = [](uint32_t w) { return __popc((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) & 0x80808080u); };
+    for (int64_t k = lane; k < nv; k += 64) {
+        const uint4 w = v[k];
+        n += bits(w.x) + bits(w.y) + bits(w.z) + bits(w.w);
     }
+    const int edges = (int)(body - t0 + t1 - tail);
+    if (lane < edges) n += mask[lane < body - t0 ? t0 + lane : tail + (lane - (body - t0))] != 0;
+    return wave_sum_i64(n);
 }
 
-// The weight of a token: one for all (weights[0]) or one per sequence.
-__global__ __launch_bounds__(kJoinWG) void k_policy_weight(Policy a, int P, const int64_t* __restrict__ counts,
-                                                           float* __restrict__ weights)
+__device__ __forceinline__ void seq_range(const Policy& a, int64_t b, int64_t* s0, int64_t* s1)
 {
-    __shared__ int64_t part[2][kJoinWG / 64];
-    const int tid = threadIdx.x;
-    int64_t all = 0, some = 0;
-    for (int64_t b = tid; b < a.B; b += kJoinWG) {
-        int64_t n = 0;
-        for (int p = 0; p < P; ++p) n += counts[b * P + p];
-        all += n;
-        some += n > 0;
+    *s0 = clamp_tok(a.start[b], a.N);
+    *s1 = clamp_tok(a.start[b + 1], a.N);
+    if (*s1 < *s0) *s1 = *s0;
+}
+
+// Counts of tokens that take part.  SHARES: equal shares of all tokens, one a
+// workgroup.  PARTS (few sequences): part blockIdx.y of gridDim.y of sequence
+// blockIdx.x, by a workgroup.  SEQS (many): whole sequences by one wave each, and
+// behind them a workgroup's number of those that are not empty.
+enum { COUNT_SHARES, COUNT_PARTS, COUNT_SEQS };
+
+template <int KIND>
+__global__ __launch_bounds__(kPolicyWG) void k_policy_count(Policy a, int64_t* __restrict__ counts)
+{
+    constexpr int NW = kPolicyWG / 64;
+    __shared__ int64_t part[NW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t sum = 0;
+    if (KIND == COUNT_SEQS) {
+        for (int64_t b = (int64_t)blockIdx.x * NW + wave; b < a.B; b += (int64_t)gridDim.x * NW) {
+            int64_t t0, t1;
+            seq_range(a, b, &t0, &t1);
+            const int64_t n = a.mask ? count_mask(a.mask, t0, t1) : t1 - t0;
+            if (lane == 0) counts[b] = n;
+            sum += n > 0;
+        }
+    } else {
+        int64_t t0, t1, pieces = NW, piece = wave;
+        if (KIND == COUNT_SHARES) {
+            t0 = clamp_tok(a.start[0], a.N);
+            t1 = clamp_tok(a.start[a.B], a.N);
+            pieces *= gridDim.x;
+            piece += (int64_t)blockIdx.x * NW;
+        } else {
+            seq_range(a, blockIdx.x, &t0, &t1);
+            pieces *= gridDim.y;
+            piece += (int64_t)blockIdx.y * NW;
+        }
+        // at least a round of 1 KB of mask each
+        int64_t share = t1 > t0 ? ((t1 - t0 + pieces - 1) / pieces + 1023) & ~(int64_t)1023 : 0;
+        t0 += piece * share;
+        if (t0 < t1) sum = count_mask(a.mask, t0, t0 + share < t1 ? t0 + share : t1);
     }
-    all = wave_sum64(all);
-    some = wave_sum64(some);
-    if ((tid & 63) == 0) {
-        part[0][tid >> 6] = all;
-        part[1][tid >> 6] = some;
-    }
+    if (lane == 0) part[wave] = sum;
     __syncthreads();
-    all = some = 0;
-    for (int w = 0; w < kJoinWG / 64; ++w) {
-        all += part[0][w];
-        some += part[1][w];
-    }
-    if (a.reduction == SF_MEAN_TOKENS) {
-        if (tid == 0) weights[0] = all > 0 ? (float)((double)a.scale / (double)all) : 0.0f;
-        return;
-    }
-    for (int64_t b = tid; b < a.B; b += kJoinWG) {
-        int64_t n = 0;
-        for (int p = 0; p < P; ++p) n += counts[b * P + p];
-        weights[b] = n > 0 ? (float)((double)a.scale / ((double)some * (double)n)) : 0.0f;
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < NW; ++w) sum += part[w];
+        const int64_t at = KIND == COUNT_SEQS    ? a.B + blockIdx.x
+                           : KIND == COUNT_PARTS ? (int64_t)blockIdx.x * gridDim.y + blockIdx.y
+                                                 : blockIdx.x;
+        counts[at] = sum;
     }
 }
 
@@ -110,43 +152,47 @@ struct TokenTerms {
     float surr, kl, clipped, grad;
 };
 
+// e^x, within 2 units in the last place: 2^(x log2 e) with the product's
+// rounding put right (but where 2^ of it is 0 or infinite anyway).
+__device__ __forceinline__ float exp_f32(float x)
+{
+    const float h = x * kLog2e;
+    const float l = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -h));
+    const float e = fast_exp2(h);
+    return fabsf(h) < 127.0f ? fmaf(e, l * kLn2, e) : e;
+}
+
 // e^x - x - 1 and e^x - 1.  Near 0 both differences cancel, so a series takes
 // over: x^2 (1/2 + x/6 + ... + x^8/10!), within 2^-28 of it for |x| <= 1/2.
 __device__ __forceinline__ void kl_terms(float x, float* kl, float* em1)
 {
-    if (fabsf(x) <= 0.5f) {
-        float q = 1.0f / 3628800.0f;
-        q = fmaf(q, x, 1.0f / 362880.0f);
-        q = fmaf(q, x, 1.0f / 40320.0f);
-        q = fmaf(q, x, 1.0f / 5040.0f);
-        q = fmaf(q, x, 1.0f / 720.0f);
-        q = fmaf(q, x, 1.0f / 120.0f);
-        q = fmaf(q, x, 1.0f / 24.0f);
-        q = fmaf(q, x, 1.0f / 6.0f);
-        q = fmaf(q, x, 0.5f);
-        *kl = x * x * q;
-        *em1 = *kl + x;
-        return;
-    }
-    const float e = expf(x);
-    if (e == INFINITY) {
-        *kl = *em1 = kF32Max;
-        return;
-    }
-    *em1 = e - 1.0f;
-    *kl = *em1 - x;
+    float q = 1.0f / 3628800.0f;
+    q = fmaf(q, x, 1.0f / 362880.0f);
+    q = fmaf(q, x, 1.0f / 40320.0f);
+    q = fmaf(q, x, 1.0f / 5040.0f);
+    q = fmaf(q, x, 1.0f / 720.0f);
+    q = fmaf(q, x, 1.0f / 120.0f);
+    q = fmaf(q, x, 1.0f / 24.0f);
+    q = fmaf(q, x, 1.0f / 6.0f);
+    q = fmaf(q, x, 0.5f);
+    const float near = x * x * q;
+    const float e = exp_f32(x);
+    const bool is_near = fabsf(x) <= 0.5f;
+    *em1 = is_near ? near + x : e == INFINITY ? kF32Max : e - 1.0f;
+    *kl = is_near ? near : e == INFINITY ? kF32Max : *em1 - x;
 }
 
 __device__ __forceinline__ TokenTerms token_terms(const Policy& a, float logp, float old, float ref, float adv)
 {
     TokenTerms r;
     const float d = logp - old;
-    const bool over = adv > 0.0f && d > a.log_hi, under = adv < 0.0f && d < a.log_lo;
-    float ratio = expf(d);
-    if (ratio == INFINITY) ratio = kF32Max;
-    r.clipped = over || under ? 1.0f : 0.0f;
-    r.surr = -adv * (over ? a.hi : under ? a.lo : ratio);
-    r.grad = over || under ? 0.0f : r.surr;
+    const bool up = adv > 0.0f;
+    const bool clipped = up ? d > a.log_hi : adv < 0.0f && d < a.log_lo;
+    float ratio = exp_f32(d);
+    ratio = ratio == INFINITY ? kF32Max : ratio;
+    r.clipped = clipped ? 1.0f : 0.0f;
+    r.surr = -adv * (clipped ? (up ? a.hi : a.lo) : ratio);
+    r.grad = clipped ? 0.0f : r.surr;
     r.kl = 0.0f;
     if (a.ref) {
         float em1;
@@ -156,113 +202,435 @@ __device__ __forceinline__ TokenTerms token_terms(const Policy& a, float logp, f
     return r;
 }
 
-__global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, const float* __restrict__ weights,
-                                                           float* __restrict__ out_grad,
-                                                           double* __restrict__ partial)
+// Sum over a workgroup of WG threads, in every thread.
+template <int WG>
+__device__ __forceinline__ int64_t group_sum(int64_t v, int64_t* part)
 {
-    __shared__ double part[3][kPolicyWG / 64];
-    const int tid = threadIdx.x;
-    const int64_t chunks = (a.N + kPolicyChunk - 1) / kPolicyChunk;
-    for (int64_t ch = blockIdx.x; ch < chunks; ch += gridDim.x) {
-        const int64_t t0 = ch * kPolicyChunk + (int64_t)tid * kPolicyTok;
-        double sum[3] = {0.0, 0.0, 0.0};
-        if (t0 < a.N) {
-            const int n = (int)(a.N - t0 < kPolicyTok ? a.N - t0 : kPolicyTok);
-            float lp[kPolicyTok], old[kPolicyTok], ref[kPolicyTok], adv[kPolicyTok], g[kPolicyTok];
-            bool on[kPolicyTok];
-            int64_t b = find_seq(a.start, a.B, t0);
-            int64_t end = b >= 0 ? a.start[b + 1] : 0;
-            float w = 0.0f, seq_adv = 0.0f;
-            for (int k = 0; k < kPolicyTok; ++k) {
-                const int64_t t = t0 + (k < n ? k : 0);
-                lp[k] = a.logp[t];
-                old[k] = a.old_logp[t];
-                ref[k] = a.ref ? a.ref[t] : 0.0f;
-                adv[k] = a.adv_per_token ? a.adv[t] : 0.0f;
-                on[k] = k < n && (!a.mask || a.mask[t] != 0);
-            }
-            bool fresh = true;
-            for (int k = 0; k < kPolicyTok; ++k) {
-                const int64_t t = t0 + k;
-                if (k > 0 && t >= end) {
-                    b = find_seq(a.start, a.B, t);
-                    end = b >= 0 ? a.start[b + 1] : 0;
-                    fresh = true;
-                }
-                if (fresh && b >= 0) {
-                    w = a.reduction == SF_MEAN_SEQUENCES ? weights[b]
-                        : a.reduction == SF_MEAN_TOKENS  ? weights[0]
-                                                         : a.scale;
-                    if (!a.adv_per_token) seq_adv = a.adv[b];
-                    fresh = false;
-                }
-                g[k] = 0.0f;
-                if (!on[k] || b < 0) continue;
-                const TokenTerms r = token_terms(a, lp[k], old[k], ref[k], a.adv_per_token ? adv[k] : seq_adv);
-                g[k] = w * r.grad;
-                sum[0] += (double)(w * r.surr);
-                sum[1] += (double)(w * r.kl);
-                sum[2] += (double)(w * r.clipped);
-            }
-            if (n == kPolicyTok)
-                *(v4f_a4*)(out_grad + t0) = v4f_a4{g[0], g[1], g[2], g[3]};
-            else
-                for (int k = 0; k < kPolicyTok; ++k)
-                    if (k < n) out_grad[t0 + k] = g[k];
-        }
-        for (int q = 0; q < 3; ++q) {
-            sum[q] = wave_sum_f64(sum[q]);
-            if ((tid & 63) == 0) part[q][tid >> 6] = sum[q];
-        }
-        __syncthreads();
-        if (tid < 3) {
-            double s = 0.0;
-            for (int w = 0; w < kPolicyWG / 64; ++w) s += part[tid][w];
-            partial[ch * 3 + tid] = s;
-        }
-        __syncthreads();
-    }
+    v = wave_sum_i64(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll 1
+    for (int w = 0; w < WG / 64; ++w) v += part[w];
+    return v;
 }
 
-// The workgroups' sums in their order, and the loss from them.
-__global__ __launch_bounds__(kJoinWG) void k_policy_join(int64_t chunks, float kl_coef,
-                                                         const double* __restrict__ partial,
-                                                         float* __restrict__ terms)
+// A lane's kTok consecutive tokens, as loaded.
+struct Tokens {
+    v4f lp, old, ref, adv;
+    uint32_t on;  // bit j: token j is there and its mask is not 0
+};
+
+__device__ __forceinline__ v4f load4(const float* p, int n)
 {
-    __shared__ double part[3][kJoinWG / 64];
-    const int tid = threadIdx.x;
-    double sum[3] = {0.0, 0.0, 0.0};
-    for (int64_t ch = tid; ch < chunks; ch += kJoinWG)
-        for (int q = 0; q < 3; ++q) sum[q] += partial[ch * 3 + q];
+    if (n >= kTok) return *(const v4f_a4*)p;
+    v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kTok - 1; ++j)
+        if (j < n) x[j] = p[j];
+    return x;
+}
+
+__device__ __forceinline__ uint32_t load_mask(const uint8_t* p, int n)
+{
+    if (n <= 0) return 0;
+    uint32_t on = n >= kTok ? 0xFu : (1u << n) - 1;
+    if (p) {
+        uint32_t m = 0;
+        if (n >= kTok)
+            __builtin_memcpy(&m, p, 4);
+        else
+            for (int j = 0; j < n; ++j) m |= (uint32_t)p[j] << (8 * j);
+        // a bit a byte that is not 0, gathered
+        m = (((m & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | m) & 0x80808080u;
+        on &= (m >> 7 | m >> 14 | m >> 21 | m >> 28) & 0xFu;
+    }
+    return on;
+}
+
+// The tokens from t0 + off on, of the wave's [t0, t0 + len).
+__device__ __forceinline__ Tokens load_tokens(const Policy& a, int64_t t0, int off, int len)
+{
+    Tokens x = {};
+    const int n = len - off;
+    if (n <= 0) return x;
+    x.lp = load4(a.logp + t0 + off, n);
+    x.old = load4(a.old_logp + t0 + off, n);
+    if (a.ref) x.ref = load4(a.ref + t0 + off, n);
+    if (a.adv_per_token) x.adv = load4(a.adv + t0 + off, n);
+    x.on = load_mask(a.mask ? a.mask + t0 + off : nullptr, n);
+    return x;
+}
+
+// Index of the last of `n` ascending starts at or before t, -1: none.
+__device__ __forceinline__ int last_start(const int* start, int n, int t)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= t)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    return lo - 1;
+}
+
+// The sequences of a wave's tokens, a round at a time, in the slice of n
+// sequences whose n + 1 starts lie in LDS: mostly all of one, which is followed.
+struct Walk {
+    const int* start;
+    int n, k;  // k: the sequence, or gap, of the round's first token
+
+    __device__ __forceinline__ int next() const
+    {
+        return k < n ? __builtin_amdgcn_readfirstlane(start[k + 1]) : kFar;
+    }
+    // to the round of tokens [t, t + kRoundTok); true where all are of one
+    __device__ __forceinline__ bool round(int t)
+    {
+        while (next() <= t) ++k;
+        return next() > t + kRoundTok - 1;
+    }
+    __device__ __forceinline__ bool inside(int q) const { return q >= 0 && q < n; }
+};
+
+// From token t on: the last start at or before it, found by the wave in two
+// looks (every stride-th start, then those between).
+__device__ __forceinline__ Walk walk_from(const int* start, int n, int t)
+{
+    const int lane = threadIdx.x & 63;
+    const int stride = (n + 64) >> 6;  // 64 strides hold n + 1 starts
+    int at = lane * stride;
+    int k = __popcll(__ballot(at <= n && start[at <= n ? at : 0] <= t)) - 1;
+    if (k >= 0 && stride > 1) {
+        at = k * stride + lane;
+        const bool in = lane < stride && at <= n;
+        k = k * stride + __popcll(__ballot(in && start[in ? at : 0] <= t)) - 1;
+    }
+    return {start, n, k};
+}
+
+__device__ __forceinline__ void write_terms(const double (&s)[3], float kl_coef, float* terms)
+{
+    terms[0] = (float)(kl_coef == 0.0f ? s[0] : s[0] + (double)kl_coef * s[1]);
+    terms[1] = (float)s[0];
+    terms[2] = (float)s[1];
+    terms[3] = (float)s[2];
+}
+
+// Sums over a workgroup; valid in thread 0.
+template <int WG>
+__device__ __forceinline__ void group_terms(double (&sum)[3], double (*part)[WG / 64])
+{
+#pragma unroll
     for (int q = 0; q < 3; ++q) {
         sum[q] = wave_sum_f64(sum[q]);
-        if ((tid & 63) == 0) part[q][tid >> 6] = sum[q];
+        if ((threadIdx.x & 63) == 0) part[q][threadIdx.x >> 6] = sum[q];
     }
     __syncthreads();
-    if (tid == 0) {
-        double s[3] = {0.0, 0.0, 0.0};
-        for (int q = 0; q < 3; ++q)
-            for (int w = 0; w < kJoinWG / 64; ++w) s[q] += part[q][w];
-        terms[0] = (float)(kl_coef == 0.0f ? s[0] : s[0] + (double)kl_coef * s[1]);
-        terms[1] = (float)s[0];
-        terms[2] = (float)s[1];
-        terms[3] = (float)s[2];
-    }
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            sum[q] = part[q][0];
+#pragma unroll 1
+            for (int w = 1; w < WG / 64; ++w) sum[q] += part[q][w];
+        }
 }
 
-// Parts that a sequence's count is split into: one wave each, enough for the
-// chip where there are few sequences.
-static inline int count_parts(int64_t N, int64_t B)
+// Adds a lane's tokens with their weights and advantages to its sums (of a few
+// tokens each; a workgroup's are in 64 bits); their gradients.
+__device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint32_t on, v4f w, v4f adv, float (&sum)[3])
 {
-    const int64_t want = (2048 + B - 1) / B;
-    const int64_t most = N / 4096 + 1;
-    const int64_t p = want < most ? want : most;
-    return p < 1 ? 1 : (int)p;
+    v4f g;
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) {
+        const TokenTerms r = token_terms(a, x.lp[j], x.old[j], x.ref[j], adv[j]);
+        const bool is_on = on >> j & 1;
+        g[j] = is_on ? w[j] * r.grad : 0.0f;
+        sum[0] += is_on ? w[j] * r.surr : 0.0f;
+        sum[1] += is_on ? w[j] * r.kl : 0.0f;
+        sum[2] += is_on ? w[j] * r.clipped : 0.0f;
+    }
+    return g;
 }
+
+// One round: the tokens' weights and advantages by their sequences (weight_of
+// and the slice's advantages), their terms and gradients.
+template <class WeightOf>
+__device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk& walk, int t, int off, int len,
+                                          const float* seq_adv, WeightOf weight_of, float (&sum)[3], float* out)
+{
+    v4f w = {0.0f, 0.0f, 0.0f, 0.0f}, adv = x.adv;
+    uint32_t on = x.on;
+    if (walk.round(t)) {
+        if (walk.inside(walk.k)) {
+            const float w1 = weight_of(walk.k);
+            w = v4f{w1, w1, w1, w1};
+            if (!a.adv_per_token) {
+                const float a1 = seq_adv[walk.k];
+                adv = v4f{a1, a1, a1, a1};
+            }
+        } else {
+            on = 0;
+        }
+    } else {
+        const int mine = t + (int)(threadIdx.x & 63) * kTok;
+        int k = last_start(walk.start, walk.n + 1, mine);
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+            while (k < walk.n && walk.start[k + 1] <= mine + j) ++k;
+            if (walk.inside(k)) {
+                w[j] = weight_of(k);
+                if (!a.adv_per_token) adv[j] = seq_adv[k];
+            } else {
+                on &= ~(1u << j);
+            }
+        }
+    }
+    const v4f g = add_tokens(a, x, on, w, adv, sum);
+    if (len - off >= kTok)
+        *(v4f_a4*)(out + off) = g;
+    else
+#pragma unroll
+        for (int j = 0; j < kTok - 1; ++j)
+            if (j < len - off) out[off + j] = g[j];
+}
+
+// What the count left: `n` shares' or parts' counts (P of them a sequence), or
+// a count per sequence and, behind all of them, n workgroups' numbers of
+// sequences that are not empty (P = 0), or nothing (n = 0).
+struct Weights {
+    const int64_t* counts;
+    int32_t n, shift;  // P = 1 << shift
+};
+
+// One workgroup, one chunk of tokens.  The sequences that the chunk meets (all
+// of them where they are few) lie in LDS; where even these are too many, each
+// token looks its own up in memory.
+__global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt, float* __restrict__ out_grad,
+                                                           double* __restrict__ partial)
+{
+    __shared__ int start[kSliceMax + 1];  // relative to the chunk
+    __shared__ unsigned long long count[kFewSeqs];
+    __shared__ int64_t ints[kPolicyWG / 64];
+    __shared__ double part[3][kPolicyWG / 64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t t0 = (int64_t)blockIdx.x * kPolicyChunk;
+    const int64_t t1 = t0 + kPolicyChunk < a.N ? t0 + kPolicyChunk : a.N;
+    const int first = __builtin_amdgcn_readfirstlane(tid >> 6) * kWaveTok;  // of the wave, in the chunk
+    const int64_t wave0 = t0 + first;
+    const int len = wave0 >= t1 ? 0 : t1 - wave0 < kWaveTok ? (int)(t1 - wave0) : kWaveTok;
+    Tokens next = load_tokens(a, wave0, lane * kTok, len);
+
+    // the slice of sequences [b0, b0 + slice)
+    int64_t b0 = 0, slice = a.B;
+    if (a.B > kFewSeqs) {
+        const int64_t first = find_start(a.start, a.B + 1, t0), past = find_start(a.start, a.B + 1, t1 - 1);
+        b0 = first > 0 ? first - 1 : 0;
+        const int64_t b1 = past < a.B ? past : a.B;
+        slice = b1 > b0 ? b1 - b0 : 0;
+    }
+    const bool few = a.B <= kFewSeqs, fits = slice <= kSliceMax;
+    // every load of the prologue before the first wait for one
+    constexpr int RS = kFewSeqs / kPolicyWG + 1, RC = kCountMax / kPolicyWG;
+    int64_t starts[RS], counts[RC];
+    const int64_t* from = wt.counts + (few || a.reduction == SF_MEAN_TOKENS ? 0 : a.B);
+#pragma unroll
+    for (int r = 0; r < RS; ++r) starts[r] = fits && tid + r * kPolicyWG <= slice ? a.start[b0 + tid + r * kPolicyWG] : 0;
+#pragma unroll
+    for (int r = 0; r < RC; ++r) counts[r] = tid + r * kPolicyWG < wt.n ? from[tid + r * kPolicyWG] : 0;
+    auto keep = [&](int k, int64_t v) {
+        const int64_t d = v - t0;
+        start[k] = d < -1 ? -1 : d > kPolicyChunk ? kPolicyChunk : (int)d;
+    };
+    if (fits) {
+#pragma unroll
+        for (int r = 0; r < RS; ++r)
+            if (tid + r * kPolicyWG <= slice) keep(tid + r * kPolicyWG, starts[r]);
+        for (int k = tid + RS * kPolicyWG; k <= slice; k += kPolicyWG) keep(k, a.start[b0 + k]);
+    }
+
+    // one weight for all tokens, or one per sequence
+    float scale = a.scale;
+    if (a.reduction == SF_MEAN_TOKENS) {
+        int64_t all = 0;
+#pragma unroll
+        for (int r = 0; r < RC; ++r) all += counts[r];
+        if (wt.n == 0 && tid == 0) all = clamp_tok(a.start[a.B], a.N) - clamp_tok(a.start[0], a.N);
+        all = group_sum<kPolicyWG>(all, ints);
+        scale = all > 0 ? scale / (float)all : 0.0f;
+    } else if (a.reduction == SF_MEAN_SEQUENCES) {
+        int64_t some = 0;
+        if (!few) {
+#pragma unroll
+            for (int r = 0; r < RC; ++r) some += counts[r];
+        } else {
+            if (wt.n == 0) {  // no mask: their lengths
+                for (int k = tid; k < slice; k += kPolicyWG) {
+                    int64_t s0, s1;
+                    seq_range(a, k, &s0, &s1);
+                    count[k] = (unsigned long long)(s1 - s0);
+                }
+            } else if (wt.shift == 0) {
+#pragma unroll
+                for (int r = 0; r < RC; ++r)
+                    if (tid + r * kPolicyWG < wt.n) count[tid + r * kPolicyWG] = (unsigned long long)counts[r];
+            } else {
+                for (int k = tid; k < slice; k += kPolicyWG) count[k] = 0;
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < RC; ++r)
+                    if (tid + r * kPolicyWG < wt.n)
+                        atomicAdd(&count[(tid + r * kPolicyWG) >> wt.shift], (unsigned long long)counts[r]);
+                __syncthreads();
+            }
+            for (int k = tid; k < slice; k += kPolicyWG) some += count[k] > 0;
+        }
+        some = group_sum<kPolicyWG>(some, ints);
+        scale = some > 0 ? scale / (float)some : 0.0f;
+    }
+    __syncthreads();
+    auto weight_of = [&](int k) {
+        if (a.reduction != SF_MEAN_SEQUENCES) return scale;
+        const float n = few ? (float)count[k] : (float)wt.counts[b0 + k];
+        return n > 0.0f ? scale / n : 0.0f;
+    };
+    float sums[3] = {0.0f, 0.0f, 0.0f};
+    float* grad = out_grad + wave0;
+    if (fits) {
+        Walk walk = walk_from(start, (int)slice, first);
+#pragma unroll 1
+        for (int q = 0; q < len; q += kRoundTok) {
+            const Tokens x = next;
+            next = load_tokens(a, wave0, q + kRoundTok + lane * kTok, len);
+            add_round(a, x, walk, first + q, q + lane * kTok, len, a.adv + b0, weight_of, sums, grad);
+        }
+    } else {
+#pragma unroll 1
+        for (int off = lane; off < len; off += 64) {
+            const int64_t k = find_start(a.start, a.B + 1, wave0 + off);
+            const bool on = k >= 1 && k <= a.B && (!a.mask || a.mask[wave0 + off] != 0);
+            float g = 0.0f;
+            if (on) {
+                const TokenTerms r = token_terms(a, a.logp[wave0 + off], a.old_logp[wave0 + off],
+                                                 a.ref ? a.ref[wave0 + off] : 0.0f,
+                                                 a.adv_per_token ? a.adv[wave0 + off] : a.adv[k - 1]);
+                const float w = weight_of((int)(k - 1 - b0));
+                g = w * r.grad;
+                sums[0] += w * r.surr;
+                sums[1] += w * r.kl;
+                sums[2] += w * r.clipped;
+            }
+            grad[off] = g;
+        }
+    }
+    double sum[3] = {(double)sums[0], (double)sums[1], (double)sums[2]};
+    group_terms<kPolicyWG>(sum, part);
+    if (tid == 0)
+        for (int q = 0; q < 3; ++q) partial[(int64_t)blockIdx.x * 3 + q] = sum[q];
+}
+
+// The whole loss by one workgroup: up to kSmallN tokens in kFewSeqs sequences.
+__global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __restrict__ out_grad,
+                                                           float* __restrict__ out_terms)
+{
+    __shared__ int start[kFewSeqs + 1];
+    __shared__ int count[kFewSeqs];
+    __shared__ int64_t ints[kSmallWG / 64];
+    __shared__ double part[3][kSmallWG / 64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int B = (int)a.B;
+    const int N = (int)a.N, rounds = N <= kSmallWG * kTok ? 1 : kSmallRounds;
+    const int each = rounds * kRoundTok;  // consecutive tokens of a wave
+    const int first = __builtin_amdgcn_readfirstlane(tid >> 6) * each;
+    const int len = first >= N ? 0 : N - first < each ? N - first : each;
+    Tokens next = load_tokens(a, first, lane * kTok, len);
+    uint32_t ons = next.on;  // kTok bits a round
+#pragma unroll
+    for (int q = 1; q < kSmallRounds; ++q) {
+        const int off = q * kRoundTok + lane * kTok;
+        ons |= load_mask(a.mask ? a.mask + first + off : nullptr, len - off) << (q * kTok);
+    }
+    for (int k = tid; k <= B; k += kSmallWG) {
+        start[k] = (int)clamp_tok(a.start[k], a.N);
+        if (k < B) count[k] = 0;
+    }
+    __syncthreads();
+    float scale = a.scale;
+    if (a.reduction == SF_MEAN_TOKENS) {
+        int64_t n = 0;
+#pragma unroll
+        for (int q = 0; q < kSmallRounds * kTok; ++q) {
+            const int t = first + (q / kTok) * kRoundTok + lane * kTok + q % kTok;
+            n += (ons >> q & 1) && t >= start[0] && t < start[B];
+        }
+        n = group_sum<kSmallWG>(n, ints);
+        scale = n > 0 ? scale / (float)n : 0.0f;
+    } else if (a.reduction == SF_MEAN_SEQUENCES) {
+        Walk walk = walk_from(start, B, first);
+        uint32_t left = ons;
+#pragma unroll 1
+        for (int q = 0; q < len; q += kRoundTok, left >>= kTok) {
+            // a wave whose tokens are all of one sequence adds once
+            if (walk.round(first + q)) {
+                const int n = (int)wave_sum_i64(__popc(left & ((1u << kTok) - 1)));
+                if (lane == 0 && walk.inside(walk.k) && n > 0) atomicAdd(&count[walk.k], n);
+            } else {
+                for (int j = 0; j < kTok; ++j) {
+                    const int k = last_start(start, B + 1, first + q + lane * kTok + j);
+                    if ((left >> j & 1) && walk.inside(k)) atomicAdd(&count[k], 1);
+                }
+            }
+        }
+        __syncthreads();
+        const int64_t n = group_sum<kSmallWG>(tid < B && count[tid] > 0, ints);
+        scale = n > 0 ? scale / (float)n : 0.0f;
+    }
+    auto weight_of = [&](int k) {
+        if (a.reduction != SF_MEAN_SEQUENCES) return scale;
+        return count[k] > 0 ? scale / (float)count[k] : 0.0f;
+    };
+    float sums[3] = {0.0f, 0.0f, 0.0f};
+    Walk walk = walk_from(start, B, first);
+#pragma unroll 1
+    for (int q = 0; q < len; q += kRoundTok) {
+        const Tokens x = next;
+        next = load_tokens(a, first, q + kRoundTok + lane * kTok, len);
+        add_round(a, x, walk, first + q, q + lane * kTok, len, a.adv, weight_of, sums, out_grad + first);
+    }
+    double sum[3] = {(double)sums[0], (double)sums[1], (double)sums[2]};
+    group_terms<kSmallWG>(sum, part);
+    if (tid == 0) write_terms(sum, a.kl_coef, out_terms);
+}
+
+// The workgroups' sums in their order.
+__global__ __launch_bounds__(kJoinWG) void k_policy_join(int64_t chunks, float kl_coef,
+                                                           const double* __restrict__ partial,
+                                                           float* __restrict__ terms)
+{
+    __shared__ double part[3][kJoinWG / 64];
+    double sum[3] = {0.0, 0.0, 0.0};
+    for (int64_t k = threadIdx.x; k < chunks; k += kJoinWG)
+        for (int q = 0; q < 3; ++q) sum[q] += partial[k * 3 + q];
+    group_terms<kJoinWG>(sum, part);
+    if (threadIdx.x == 0) write_terms(sum, kl_coef, terms);
+}
+
+// log2 of the workgroups that count a sequence, where there are few: each has
+// about four rounds of 4 KB of mask.
+static inline int count_shift(int64_t N, int64_t B)
+{
+    int shift = 0;
+    while ((B << (shift + 1)) <= kCountMax && (N >> shift) > 16384 * B) ++shift;
+    return shift;
+}
+
+static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kFewSeqs; }
 
 struct PolicyLayout {
-    int P;
-    int64_t counts, weights, partial, bytes;  // offsets
+    int64_t partial, bytes;  // offsets; the counts come first
 };
 
 static inline int64_t up16(int64_t n) { return (n + 15) & ~(int64_t)15; }
@@ -270,11 +638,8 @@ static inline int64_t up16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 static inline PolicyLayout policy_layout(int64_t N, int64_t B)
 {
     PolicyLayout l;
-    l.P = B > 0 ? count_parts(N, B) : 1;
-    l.counts = 0;
-    l.weights = up16(B * l.P * 8);
-    l.partial = l.weights + up16((B > 0 ? B : 1) * 4);
-    l.bytes = l.partial + up16((N + kPolicyChunk - 1) / kPolicyChunk * 3 * 8) + 16;
+    l.partial = up16((B + kCountBlocks > kCountMax ? B + kCountBlocks : kCountMax) * 8);
+    l.bytes = l.partial + up16((N + kPolicyChunk - 1) / kPolicyChunk * 3 * 8);
     return l;
 }
 
@@ -289,7 +654,8 @@ using namespace sfk;
 
 SF_API int64_t sf_policy_loss_workspace(int64_t N, int64_t B)
 {
-    return policy_sizes_ok(N, B) ? policy_layout(N, B).bytes : -1;
+    if (!policy_sizes_ok(N, B)) return -1;
+    return small_policy(N, B) ? 0 : policy_layout(N, B).bytes;
 }
 
 SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantage,
@@ -303,8 +669,9 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
         !(clip_high >= 0.0f && clip_high <= kF32Max) || !(fabsf(kl_coef) <= kF32Max))
         return SF_EINVAL;
     const PolicyLayout l = policy_layout(N, B);
-    if (!out_terms || !workspace || workspace_bytes < l.bytes || !aligned(workspace, 16) || !seq_start)
-        return SF_EINVAL;
+    const int64_t need = small_policy(N, B) ? 0 : l.bytes;
+    if (!out_terms || !seq_start) return SF_EINVAL;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SF_EINVAL;
     const int64_t n_adv = advantage_per_token ? N : B;
     if (N > 0 && (!logp || !old_logp || !out_grad)) return SF_EINVAL;
     if (n_adv > 0 && !advantage) return SF_EINVAL;
@@ -314,7 +681,7 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
     const void* ins[6] = {logp, old_logp, ref_logp, advantage, mask, seq_start};
     const int64_t in_bytes[6] = {N * 4, N * 4, N * 4, n_adv * 4, N, (B + 1) * 8};
     const void* outs[3] = {out_terms, out_grad, workspace};
-    const int64_t out_bytes[3] = {16, N * 4, l.bytes};
+    const int64_t out_bytes[3] = {16, N * 4, need};
     for (int o = 0; o < 3; ++o) {
         if (!outs[o] || out_bytes[o] == 0) continue;
         for (int i = 0; i < 6; ++i)
@@ -340,25 +707,42 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
     a.scale = scale;
     a.adv_per_token = advantage_per_token != 0;
     a.reduction = reduction;
-    int64_t* counts = (int64_t*)((char*)workspace + l.counts);
-    float* weights = (float*)((char*)workspace + l.weights);
+    if (small_policy(N, B)) {
+        void* args[] = {(void*)&a, (void*)&out_grad, (void*)&out_terms};
+        return launch((const void*)&k_policy_small, dim3(1), dim3(kSmallWG), args, 0, stream);
+    }
+    int64_t* counts = (int64_t*)workspace;
     double* partial = (double*)((char*)workspace + l.partial);
     int64_t chunks = (N + kPolicyChunk - 1) / kPolicyChunk;
-    int P = l.P;
-    if (N > 0 && B > 0 && reduction != SF_SUM_TOKENS) {
-        const int64_t nw = (B * P + kPolicyWG / 64 - 1) / (kPolicyWG / 64);
-        void* cargs[] = {(void*)&a, (void*)&P, (void*)&counts};
-        int rc = launch((const void*)&k_policy_count, dim3((unsigned)(nw < (1 << 20) ? nw : (1 << 20))),
-                        dim3(kPolicyWG), cargs, 0, stream);
-        if (rc != SF_OK) return rc;
-        void* wargs[] = {(void*)&a, (void*)&P, (void*)&counts, (void*)&weights};
-        rc = launch((const void*)&k_policy_weight, dim3(1), dim3(kJoinWG), wargs, 0, stream);
+    if (chunks > INT32_MAX) return SF_EINVAL;
+    Weights wt = {counts, 0, 0};
+    if (N > 0 && B > 0 && reduction != SF_SUM_TOKENS && (mask || (reduction == SF_MEAN_SEQUENCES && B > kFewSeqs))) {
+        const void* fn;
+        dim3 grid;
+        if (reduction == SF_MEAN_TOKENS) {
+            // shares of at least four rounds
+            const int64_t want = N / 16384 + 1;
+            wt.n = (int)(want < kCountBlocks ? want : kCountBlocks);
+            fn = (const void*)&k_policy_count<COUNT_SHARES>;
+            grid = dim3((unsigned)wt.n);
+        } else if (B <= kFewSeqs) {
+            wt.shift = count_shift(N, B);
+            wt.n = (int)B << wt.shift;
+            fn = (const void*)&k_policy_count<COUNT_PARTS>;
+            grid = dim3((unsigned)B, 1u << wt.shift);
+        } else {
+            const int64_t want = (B + kPolicyWG / 64 - 1) / (kPolicyWG / 64);
+            wt.n = (int)(want < kCountBlocks ? want : kCountBlocks);
+            fn = (const void*)&k_policy_count<COUNT_SEQS>;
+            grid = dim3((unsigned)wt.n);
+        }
+        void* args[] = {(void*)&a, (void*)&counts};
+        const int rc = launch(fn, grid, dim3(kPolicyWG), args, 0, stream);
         if (rc != SF_OK) return rc;
     }
-    if (N > 0) {
-        void* args[] = {(void*)&a, (void*)&weights, (void*)&out_grad, (void*)&partial};
-        const int rc = launch((const void*)&k_policy_loss, dim3((unsigned)(chunks < (1 << 20) ? chunks : (1 << 20))),
-                              dim3(kPolicyWG), args, 0, stream);
+    if (chunks > 0) {
+        void* args[] = {(void*)&a, (void*)&wt, (void*)&out_grad, (void*)&partial};
+        const int rc = launch((const void*)&k_policy_loss, dim3((unsigned)chunks), dim3(kPolicyWG), args, 0, stream);
         if (rc != SF_OK) return rc;
     }
     void* jargs[] = {(void*)&chunks, (void*)&kl_coef, (void*)&partial, (void*)&out_terms};

@@ -34,6 +34,12 @@ using VecU = typename Elem<DT>::T __attribute__((ext_vector_type(kVec<DT>), alig
 template <int DT>
 using VecF = float __attribute__((ext_vector_type(kVec<DT>)));
 
+// The same in global memory, for addresses that reach a kernel as numbers.
+template <int DT>
+using GlobalVec = __attribute__((address_space(1))) VecU<DT>;
+template <int DT>
+using GlobalElem = __attribute__((address_space(1))) typename Elem<DT>::T;
+
 static inline int elem_size(int dtype) { return dtype == SF_F32 ? 4 : 2; }
 
 // Elements from p up to the next 16-byte boundary, at most n.
@@ -45,6 +51,7 @@ __device__ __forceinline__ int64_t head_elems(const void* p, int64_t n)
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2eLow = 1.92596299112661746887e-8f;  // log2 e - kLog2e
 constexpr double kLog2eD = 1.44269504088896340736;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLn2Low = -1.90465429995776804525e-9f;  // ln 2 - kLn2
@@ -88,10 +95,46 @@ __device__ __forceinline__ float wave_max_f32(float v)
     return last_lane(v);
 }
 
+// Sums of 64-bit values over a wave, wave-uniform, by the same moves of their
+// halves: short code, which a kernel of a few microseconds waits for.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ uint64_t dpp_u64(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROW_MASK, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROW_MASK, 0xF, false);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t last_lane_u64(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+    return (uint64_t)hi << 32 | lo;
+}
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double dpp_f64(double v)
+{
+    return __longlong_as_double((long long)dpp_u64<CTRL, ROW_MASK>((uint64_t)__double_as_longlong(v)));
+}
 __device__ __forceinline__ double wave_sum_f64(double v)
 {
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    v += dpp_f64<0xB1, 0xF>(v);
+    v += dpp_f64<0x4E, 0xF>(v);
+    v += dpp_f64<0x141, 0xF>(v);
+    v += dpp_f64<0x140, 0xF>(v);
+    v += dpp_f64<0x142, 0xA>(v);
+    v += dpp_f64<0x143, 0xC>(v);
+    return __longlong_as_double((long long)last_lane_u64((uint64_t)__double_as_longlong(v)));
+}
+__device__ __forceinline__ int64_t wave_sum_i64(int64_t x)
+{
+    uint64_t v = (uint64_t)x;
+    v += dpp_u64<0xB1, 0xF>(v);
+    v += dpp_u64<0x4E, 0xF>(v);
+    v += dpp_u64<0x141, 0xF>(v);
+    v += dpp_u64<0x140, 0xF>(v);
+    v += dpp_u64<0x142, 0xA>(v);
+    v += dpp_u64<0x143, 0xC>(v);
+    return (int64_t)last_lane_u64(v);
 }
 
 }  // namespace sfk

@@ -366,15 +366,11 @@ static inline unsigned grid_of(int64_t n) { return (unsigned)(n < (1 << 30) ? n 
 
 using namespace sfk;
 
-SF_API int64_t sf_token_logp_workspace(int64_t N, int64_t V)
+SF_API int64_t sf_token_logp_workspace(int32_t dtype, int64_t N, int64_t V)
 {
-    if (N < 0 || V < 1 || V > ((int64_t)1 << 30) || N > ((int64_t)1 << 56)) return -1;
+    if (!rows_ok(dtype, N, V, V, 1.0f)) return -1;
     if (N == 0) return 0;
-    int P = 1;
-    for (int b = 2; b <= 4; b += 2) {
-        const int p = row_shape(N, V, b).P;
-        P = p > P ? p : P;
-    }
+    const int P = row_shape(N, V, elem_size(dtype)).P;
     return P == 1 ? 0 : N * P * (int64_t)sizeof(RowState);
 }
 
@@ -384,7 +380,7 @@ SF_API int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V
 {
     if (!rows_ok(dtype, N, V, row_stride, inv_temperature)) return SF_EINVAL;
     if (N == 0) return SF_OK;
-    const int64_t need = sf_token_logp_workspace(N, V);
+    const int64_t need = sf_token_logp_workspace(dtype, N, V);
     if (!logits || !targets || !out_logp || !out_lse || (need > 0 && !workspace) || workspace_bytes < need)
         return SF_EINVAL;
     const int64_t in_bytes = ((N - 1) * row_stride + V) * elem_size(dtype);

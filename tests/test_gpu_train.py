@@ -202,7 +202,8 @@ def run_policy(tr, lp, old, r, adv, per, mask, start, red, scale, lo, hi, beta, 
 
 @pytest.mark.parametrize("reduction", [0, 1, 2])
 @pytest.mark.parametrize("N,B", [(1, 1), (2, 5), (3, 1), (65, 3), (257, 257), (1023, 7), (1025, 1), (4099, 300),
-                                 (9000, 2), (20000, 5000), (70001, 11)])
+                                 (9000, 2), (20000, 5000), (70001, 11),
+                                 (8192, 1024), (8193, 1024), (8191, 1025), (30000, 1023), (40000, 1025), (33, 3000)])
 def test_policy(tr, N, B, reduction):
     lp, old, r, start, rng = policy_inputs(N, B, N + B)
     for per, masked, with_ref in ((False, True, True), (True, False, False), (True, True, True), (False, False, True)):
@@ -237,7 +238,8 @@ def test_policy_masked_garbage_and_tokens_of_no_sequence(tr):
     np.testing.assert_array_equal(ggrad, grad)
 
 
-@pytest.mark.parametrize("N,B,masked", [(0, 0, False), (0, 3, False), (50, 0, False), (50, 3, True), (5000, 40, True)])
+@pytest.mark.parametrize("N,B,masked", [(0, 0, False), (0, 3, False), (50, 0, False), (50, 3, True), (5000, 40, True),
+                                        (0, 2000, False), (20000, 0, False), (20000, 0, True), (20000, 2000, True)])
 @pytest.mark.parametrize("reduction", [0, 1, 2])
 def test_policy_with_nothing_taking_part(tr, N, B, masked, reduction):
     z = np.zeros(N, np.float32)
@@ -459,7 +461,7 @@ def test_captured_chain_replays(tr):
     f = lambda *s: torch.empty(s, device=DEV)  # noqa: E731
     o = dict(logp=f(N), lse=f(N), ent=f(N), terms=f(4), gl=f(N), gx=torch.empty_like(x), norms=f(3), total=f(1),
              wrong=torch.empty(3, dtype=torch.int64, device=DEV), out=[torch.empty_like(q) for q in g],
-             w1=torch.empty(tr.sf_token_logp_workspace(N, V), dtype=torch.uint8, device=DEV),
+             w1=torch.empty(tr.sf_token_logp_workspace(torch.bfloat16, N, V), dtype=torch.uint8, device=DEV),
              w2=torch.empty(tr.sf_policy_loss_workspace(N, 4), dtype=torch.uint8, device=DEV),
              w3=torch.empty(grads.workspace_bytes, dtype=torch.uint8, device=DEV))
     outset = tr.GradSet(o["out"])
@@ -502,6 +504,7 @@ def test_binding_refusals(tr):
     x = torch.zeros(4, 10, device=DEV)
     t = torch.zeros(4, dtype=torch.int64, device=DEV)
     f = torch.zeros(4, device=DEV)
+    big = torch.zeros(20000, device=DEV)
     bad = [
         (TypeError, lambda: tr.sf_token_logp(x.double(), t)),
         (ValueError, lambda: tr.sf_token_logp(x.cpu(), t)),
@@ -522,7 +525,7 @@ def test_binding_refusals(tr):
         (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, clip_low=1.0)),
         (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, reduction=3)),
         (tr.StageFrontierError, lambda: tr.sf_policy_loss(f, f, f[:3], t, out_grad=f)),
-        (ValueError, lambda: tr.sf_policy_loss(f, f, f[:3], t, workspace=torch.zeros(8, dtype=torch.uint8, device=DEV))),
+        (ValueError, lambda: tr.sf_policy_loss(big, big, f[:3], t, workspace=torch.zeros(8, dtype=torch.uint8, device=DEV))),
         (TypeError, lambda: tr.GradSet([x.double()])),
         (ValueError, lambda: tr.GradSet([x, x.cpu()])),
         (ValueError, lambda: tr.GradSet([x[:, :5]])),

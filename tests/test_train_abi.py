@@ -72,12 +72,14 @@ def test_token_logp_refusals(tr, lib):
                 dict(h=E + 2), dict(lp=D + 8), dict(lp=A + 8), dict(h=B + 16), dict(N=1 << 50, ld=1 << 20)):
         assert call(**bad) == tr.SF_EINVAL, bad
     # one row of many logits is split, and needs its workspace
-    need = lib.sf_token_logp_workspace(1, 131072)
+    V = 1 << 20
+    need = lib.sf_token_logp_workspace(1, 1, V)
     assert need > 0 and need % 4 == 0
     for bad in (dict(ws=None), dict(wb=need - 1), dict(ws=W + 4), dict(ws=A + 64)):
-        assert call(N=1, V=131072, ld=131072, **bad) == tr.SF_EINVAL, bad
-    assert lib.sf_token_logp_workspace(1, 0) == -1 and lib.sf_token_logp_workspace(-1, 5) == -1
-    assert lib.sf_token_logp_workspace(0, 5) == 0 and lib.sf_token_logp_workspace(100000, 32000) == 0
+        assert call(N=1, V=V, ld=V, **bad) == tr.SF_EINVAL, bad
+    for bad in ((1, 1, 0), (1, -1, 5), (3, 1, 5), (0, 1, 1 << 31)):
+        assert lib.sf_token_logp_workspace(*bad) == -1, bad
+    assert lib.sf_token_logp_workspace(0, 0, 5) == 0 and lib.sf_token_logp_workspace(2, 100000, 32000) == 0
 
 
 def test_token_logp_grad_refusals(tr, lib):
@@ -97,21 +99,21 @@ def test_policy_refusals(tr, lib):
     nan, inf = float("nan"), float("inf")
 
     def call(**k):
-        a = dict(dict(lp=A, old=B, ref=C, adv=D, per=0, mask=E, start=F, N=1000, B=10, red=0, sc=1.0, lo=0.2, hi=0.2,
-                      kl=0.1, terms=G, grad=G + 4096, ws=W, wb=1 << 30), **k)
+        a = dict(dict(lp=A, old=B, ref=C, adv=D, per=0, mask=E, start=F, N=100000, B=10, red=0, sc=1.0, lo=0.2, hi=0.2,
+                      kl=0.1, terms=G, grad=G + (1 << 30), ws=W, wb=1 << 30), **k)
         return lib.sf_policy_loss(a["lp"], a["old"], a["ref"], a["adv"], a["per"], a["mask"], a["start"], a["N"], a["B"],
                                   a["red"], a["sc"], a["lo"], a["hi"], a["kl"], a["terms"], a["grad"], a["ws"], a["wb"],
                                   None)
 
-    need = lib.sf_policy_loss_workspace(1000, 10)
+    need = lib.sf_policy_loss_workspace(100000, 10)
     assert need > 0
     for bad in (dict(N=-1), dict(B=-1), dict(N=1 << 40), dict(B=1 << 31), dict(red=-1), dict(red=3), dict(sc=nan),
                 dict(sc=inf), dict(lo=1.0), dict(lo=-0.1), dict(lo=nan), dict(hi=-0.1), dict(hi=inf), dict(kl=nan),
                 dict(lp=None), dict(old=None), dict(adv=None), dict(start=None), dict(terms=None), dict(grad=None),
                 dict(ws=None), dict(wb=need - 1), dict(ws=W + 8), dict(lp=A + 2), dict(start=F + 4), dict(terms=G + 2),
-                dict(grad=A), dict(grad=G + 8), dict(terms=D), dict(ws=F), dict(ws=E), dict(grad=C + 400)):
+                dict(grad=A), dict(grad=G + 8), dict(N=20, terms=A + 40, ws=None), dict(terms=D), dict(ws=F), dict(ws=E), dict(grad=C + 400)):
         assert call(**bad) == tr.SF_EINVAL, bad
-    assert lib.sf_policy_loss_workspace(-1, 0) == -1 and lib.sf_policy_loss_workspace(0, 0) > 0
+    assert lib.sf_policy_loss_workspace(-1, 0) == -1 and lib.sf_policy_loss_workspace(0, 0) == 0
 
 
 def make_list(lib, items):
