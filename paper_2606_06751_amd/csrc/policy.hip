@@ -13,8 +13,7 @@
 // 4 consecutive tokens (16-byte loads) and a wave 256 a round, which are mostly
 // of one sequence: it is found once, in LDS, and followed; only in a round that
 // meets another does each lane look for its own (64 tokens a round: 31.7 us for
-// 2e6 tokens of 1024 sequences, 256: 15.6; the kernel alone).  A loop over
-// rounds, not unrolled, keeps the code short, which small inputs wait for.  The
+// 2e6 tokens of 1024 sequences, 256: 15.6; the kernel alone).  The
 // sums go to a launch of their own: a counter of finished workgroups with the
 // memory fences that it needs cost 25 us more.
 
@@ -24,11 +23,10 @@
 
 namespace sfk {
 
-constexpr int kPolicyWG = 256;
+constexpr int kPolicyWG = 512;
 constexpr int kTok = 4;                 // consecutive tokens of a lane: 16-byte loads
 constexpr int kRoundTok = 64 * kTok;    // of a wave's round
-constexpr int kWaveTok = 2 * kRoundTok;  // of a wave
-constexpr int kPolicyChunk = kPolicyWG / 64 * kWaveTok;  // of a workgroup
+constexpr int kPolicyChunk = kPolicyWG / 64 * kRoundTok;  // of a workgroup: a round a wave
 constexpr int kSliceMax = 2048;  // sequences that a workgroup keeps in LDS
 constexpr int kFewSeqs = 1024;   // sequences of which every workgroup keeps all
 constexpr int kCountMax = 2048;  // counts that every workgroup adds up by itself
@@ -58,7 +56,8 @@ struct Policy {
 
 __device__ __forceinline__ int64_t clamp_tok(int64_t x, int64_t N) { return x < 0 ? 0 : x > N ? N : x; }
 
-// Index of the first of n ascending starts that lies past t.
+// Index of the first of n ascending starts that lies past t: by a lane for
+// itself, or by a wave in looks at 64 starts.
 __device__ __forceinline__ int64_t find_start(const int64_t* start, int64_t n, int64_t t)
 {
     int64_t lo = 0, hi = n;
@@ -68,6 +67,19 @@ __device__ __forceinline__ int64_t find_start(const int64_t* start, int64_t n, i
             lo = mid + 1;
         else
             hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ int64_t find_start_wave(const int64_t* start, int64_t n, int64_t t)
+{
+    int64_t lo = 0;
+    while (n > 0) {
+        const int64_t stride = (n + 63) >> 6, at = (int64_t)(threadIdx.x & 63) * stride;
+        const int c = __popcll(__ballot(at < n && start[lo + (at < n ? at : 0)] <= t));
+        if (c == 0) break;
+        const int64_t from = (c - 1) * stride + 1, to = from - 1 + stride < n ? from - 1 + stride : n;
+        lo += from;
+        n = to - from;
     }
     return lo;
 }
@@ -356,17 +368,16 @@ __device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint
     return g;
 }
 
-// One round: the tokens' weights and advantages by their sequences (weight_of
-// and the slice's advantages), their terms and gradients.
-template <class WeightOf>
+// One round: the tokens' weights and advantages by their sequences (the slice's,
+// in LDS), their terms and gradients.
 __device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk& walk, int t, int off, int len,
-                                          const float* seq_adv, WeightOf weight_of, float (&sum)[3], float* out)
+                                          const float* seq_adv, const float* weight, float (&sum)[3], float* out)
 {
     v4f w = {0.0f, 0.0f, 0.0f, 0.0f}, adv = x.adv;
     uint32_t on = x.on;
     if (walk.round(t)) {
         if (walk.inside(walk.k)) {
-            const float w1 = weight_of(walk.k);
+            const float w1 = weight[walk.k];
             w = v4f{w1, w1, w1, w1};
             if (!a.adv_per_token) {
                 const float a1 = seq_adv[walk.k];
@@ -382,7 +393,7 @@ __device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk
         for (int j = 0; j < kTok; ++j) {
             while (k < walk.n && walk.start[k + 1] <= mine + j) ++k;
             if (walk.inside(k)) {
-                w[j] = weight_of(k);
+                w[j] = weight[k];
                 if (!a.adv_per_token) adv[j] = seq_adv[k];
             } else {
                 on &= ~(1u << j);
@@ -414,22 +425,28 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
 {
     __shared__ int start[kSliceMax + 1];  // relative to the chunk
     __shared__ unsigned long long count[kFewSeqs];
+    __shared__ float weight[kSliceMax], seq_adv[kSliceMax];
     __shared__ int64_t ints[kPolicyWG / 64];
     __shared__ double part[3][kPolicyWG / 64];
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t t0 = (int64_t)blockIdx.x * kPolicyChunk;
     const int64_t t1 = t0 + kPolicyChunk < a.N ? t0 + kPolicyChunk : a.N;
-    const int first = __builtin_amdgcn_readfirstlane(tid >> 6) * kWaveTok;  // of the wave, in the chunk
+    const int first = __builtin_amdgcn_readfirstlane(tid >> 6) * kRoundTok;  // of the wave, in the chunk
     const int64_t wave0 = t0 + first;
-    const int len = wave0 >= t1 ? 0 : t1 - wave0 < kWaveTok ? (int)(t1 - wave0) : kWaveTok;
-    Tokens next = load_tokens(a, wave0, lane * kTok, len);
+    const int len = wave0 >= t1 ? 0 : t1 - wave0 < kRoundTok ? (int)(t1 - wave0) : kRoundTok;
+    const Tokens x = load_tokens(a, wave0, lane * kTok, len);
 
     // the slice of sequences [b0, b0 + slice)
     int64_t b0 = 0, slice = a.B;
     if (a.B > kFewSeqs) {
-        const int64_t first = find_start(a.start, a.B + 1, t0), past = find_start(a.start, a.B + 1, t1 - 1);
-        b0 = first > 0 ? first - 1 : 0;
-        const int64_t b1 = past < a.B ? past : a.B;
+        const int wave = tid >> 6;
+        if (wave < 2) {
+            const int64_t k = find_start_wave(a.start, a.B + 1, wave == 0 ? t0 : t1 - 1);
+            if (lane == 0) ints[wave] = k;
+        }
+        __syncthreads();
+        b0 = ints[0] > 0 ? ints[0] - 1 : 0;
+        const int64_t b1 = ints[1] < a.B ? ints[1] : a.B;
         slice = b1 > b0 ? b1 - b0 : 0;
     }
     const bool few = a.B <= kFewSeqs, fits = slice <= kSliceMax;
@@ -492,21 +509,23 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
         scale = some > 0 ? scale / (float)some : 0.0f;
     }
     __syncthreads();
-    auto weight_of = [&](int k) {
+    auto weight_of = [&](int64_t k) {
         if (a.reduction != SF_MEAN_SEQUENCES) return scale;
         const float n = few ? (float)count[k] : (float)wt.counts[b0 + k];
         return n > 0.0f ? scale / n : 0.0f;
     };
+    if (fits) {
+        for (int k = tid; k < slice; k += kPolicyWG) {
+            weight[k] = weight_of(k);
+            if (!a.adv_per_token) seq_adv[k] = a.adv[b0 + k];
+        }
+        __syncthreads();
+    }
     float sums[3] = {0.0f, 0.0f, 0.0f};
     float* grad = out_grad + wave0;
     if (fits) {
         Walk walk = walk_from(start, (int)slice, first);
-#pragma unroll 1
-        for (int q = 0; q < len; q += kRoundTok) {
-            const Tokens x = next;
-            next = load_tokens(a, wave0, q + kRoundTok + lane * kTok, len);
-            add_round(a, x, walk, first + q, q + lane * kTok, len, a.adv + b0, weight_of, sums, grad);
-        }
+        if (len > 0) add_round(a, x, walk, first, lane * kTok, len, seq_adv, weight, sums, grad);
     } else {
 #pragma unroll 1
         for (int off = lane; off < len; off += 64) {
@@ -517,7 +536,7 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
                 const TokenTerms r = token_terms(a, a.logp[wave0 + off], a.old_logp[wave0 + off],
                                                  a.ref ? a.ref[wave0 + off] : 0.0f,
                                                  a.adv_per_token ? a.adv[wave0 + off] : a.adv[k - 1]);
-                const float w = weight_of((int)(k - 1 - b0));
+                const float w = weight_of(k - 1 - b0);
                 g = w * r.grad;
                 sums[0] += w * r.surr;
                 sums[1] += w * r.kl;
@@ -538,6 +557,7 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
 {
     __shared__ int start[kFewSeqs + 1];
     __shared__ int count[kFewSeqs];
+    __shared__ float weight[kFewSeqs], seq_adv[kFewSeqs];
     __shared__ int64_t ints[kSmallWG / 64];
     __shared__ double part[3][kSmallWG / 64];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -553,6 +573,7 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
         const int off = q * kRoundTok + lane * kTok;
         ons |= load_mask(a.mask ? a.mask + first + off : nullptr, len - off) << (q * kTok);
     }
+    const float adv = !a.adv_per_token && tid < B ? a.adv[tid] : 0.0f;
     for (int k = tid; k <= B; k += kSmallWG) {
         start[k] = (int)clamp_tok(a.start[k], a.N);
         if (k < B) count[k] = 0;
@@ -588,17 +609,18 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
         const int64_t n = group_sum<kSmallWG>(tid < B && count[tid] > 0, ints);
         scale = n > 0 ? scale / (float)n : 0.0f;
     }
-    auto weight_of = [&](int k) {
-        if (a.reduction != SF_MEAN_SEQUENCES) return scale;
-        return count[k] > 0 ? scale / (float)count[k] : 0.0f;
-    };
+    if (tid < B) {
+        weight[tid] = a.reduction != SF_MEAN_SEQUENCES ? scale : count[tid] > 0 ? scale / (float)count[tid] : 0.0f;
+        if (!a.adv_per_token) seq_adv[tid] = adv;
+    }
+    __syncthreads();
     float sums[3] = {0.0f, 0.0f, 0.0f};
     Walk walk = walk_from(start, B, first);
 #pragma unroll 1
     for (int q = 0; q < len; q += kRoundTok) {
         const Tokens x = next;
         next = load_tokens(a, first, q + kRoundTok + lane * kTok, len);
-        add_round(a, x, walk, first + q, q + lane * kTok, len, a.adv, weight_of, sums, out_grad + first);
+        add_round(a, x, walk, first + q, q + lane * kTok, len, seq_adv, weight, sums, out_grad + first);
     }
     double sum[3] = {(double)sums[0], (double)sums[1], (double)sums[2]};
     group_terms<kSmallWG>(sum, part);

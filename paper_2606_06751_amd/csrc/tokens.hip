@@ -267,65 +267,79 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<
 }
 
 // out = inv_t (g ([j = t] - p) - h p (log p + H)): element by element from the
-// row's lse; one workgroup per (row, kGradVecs vectors).
-constexpr int kGradU = 4;
-constexpr int kGradVecs = kRowWG * kGradU;
+// row's lse, bound by HBM.  LANES lanes take chunk blockIdx.x of a row, kGradU
+// vectors each, aligned by the output: a workgroup of 256 one chunk, or a wave
+// each of 4 short rows (16000 x 515 f16: 8.4 us, by workgroups 14).  Measured at
+// 16411 x 131072 bf16, vectors a lane / loads and stores past the caches or not:
+// 1 / both 1212, 2 / loads 1210, 2 / both 1298, 2 / none 1237, 4 / both 1362 us;
+// at 512 x 100003 41.5, 37.1, 37.8, 41.3, 39.1.
+constexpr int kGradU = 2;
 
-template <int DT>
-__global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<DT>::T* logits, int64_t N,
-                                                            int64_t V, int64_t stride,
-                                                            const int64_t* __restrict__ targets, float inv_t,
-                                                            const float* __restrict__ lse,
+template <int DT, int LANES>
+__global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<DT>::T* logits, int64_t N, int V,
+                                                            int64_t stride, const int64_t* __restrict__ targets,
+                                                            float inv_t, const float* __restrict__ lse,
                                                             const float* __restrict__ grad_logp,
                                                             const float* __restrict__ entropy,
                                                             const float* __restrict__ grad_entropy,
-                                                            typename Elem<DT>::T* out, int64_t out_stride,
-                                                            int64_t chunks)
+                                                            typename Elem<DT>::T* out, int64_t out_stride)
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
-    const int tid = threadIdx.x;
-    for (int64_t blk = blockIdx.x; blk < N * chunks; blk += gridDim.x) {
-        const int64_t i = blk / chunks;
-        const int64_t ch = blk - i * chunks;
+    constexpr int ROWS = kRowWG / LANES;
+    const int tid = threadIdx.x & (LANES - 1);
+    const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+    for (int64_t i = (int64_t)blockIdx.y * ROWS + sub; i < N; i += (int64_t)gridDim.y * ROWS) {
         const int64_t t = targets[i];
+        const float l = lse[i];
         T* o = out + i * out_stride;
         const T* row = logits + i * stride;
-        const int64_t head = head_elems<DT>(o, V);
-        const int64_t nv = (V - head) / E, tail0 = head + nv * E;
-        const float l = lse[i];
-        const bool none = t < 0 || t >= V || l == -INFINITY;
-        const float g = none ? 0.0f : grad_logp[i] * inv_t;
-        const float h = none || !grad_entropy ? 0.0f : grad_entropy[i] * inv_t;
-        // -(g + h (log p + H)) = -(k0 + h log p)
-        const float k0 = h != 0.0f ? fmaf(h, entropy[i], g) : g;
-        auto value = [&](float x, int64_t j) {
-            const float q = fmaf(x, inv_t, -l);  // log p
-            const float p = fast_exp2(q * kLog2e);
-            const float y = -p * fmaf(h, fmaxf(q, -1000.0f), k0);
-            return j == t ? y + g : y;
+        const int head = (int)head_elems<DT>(o, V);
+        const int nv = (V - head) / E, tail0 = head + nv * E;
+        const int v0 = (int)blockIdx.x * (kGradU * LANES) + tid;
+        VecU<DT>* ov = (VecU<DT>*)(o + head);
+        const VecU<DT>* xv = (const VecU<DT>*)(row + head);
+        const bool edge = blockIdx.x == 0 && tid < head + V - tail0;
+        const int je = tid < head ? tid : tail0 + (tid - head);
+        if (t < 0 || t >= V || l == -INFINITY) {
+#pragma unroll
+            for (int k = 0; k < kGradU; ++k)
+                if (v0 + k * LANES < nv) ov[v0 + k * LANES] = (VecU<DT>)(T)0.0f;
+            if (edge) o[je] = (T)0.0f;
+            continue;
+        }
+        VecU<DT> x[kGradU];
+#pragma unroll
+        for (int k = 0; k < kGradU; ++k)
+            if (v0 + k * LANES < nv) x[k] = __builtin_nontemporal_load(xv + v0 + k * LANES);
+        const T xe = row[edge ? je : 0];
+        const float g = grad_logp[i] * inv_t;
+        const float h = grad_entropy ? grad_entropy[i] * inv_t : 0.0f;
+        // -(g + h (log p + H)) = -(k0 + h log p); the bound keeps 0 * -inf out
+        const float k0 = grad_entropy ? fmaf(h, entropy[i], g) : g;
+        const int at = (int)t;
+        auto value = [&](float z) {
+            const float q = fmaf(z, inv_t, -l);  // log p
+            return -fast_exp2(q * kLog2e) * fmaf(h, fmaxf(q, -1000.0f), k0);
         };
-        const int64_t v0 = ch * kGradVecs;
 #pragma unroll
         for (int k = 0; k < kGradU; ++k) {
-            const int64_t v = v0 + k * kRowWG + tid;
-            if (v >= nv) break;
-            const int64_t j0 = head + v * E;
-            VecU<DT> y;
-            if (none) {
+            const int v = v0 + k * LANES;
+            if (v < nv) {
+                float y[E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) y[j] = (T)0.0f;
-            } else {
-                const VecU<DT> x = *(const VecU<DT>*)(row + j0);
+                for (int j = 0; j < E; ++j) y[j] = value((float)x[k][j]);
+                const int hit = at - (head + v * E);  // the taken token's place, if here
+                if ((unsigned)hit < (unsigned)E)
 #pragma unroll
-                for (int j = 0; j < E; ++j) y[j] = (T)value((float)x[j], j0 + j);
+                    for (int j = 0; j < E; ++j) y[j] += j == hit ? g : 0.0f;
+                VecU<DT> r;
+#pragma unroll
+                for (int j = 0; j < E; ++j) r[j] = (T)y[j];
+                ov[v] = r;
             }
-            *(VecU<DT>*)(o + j0) = y;
         }
-        if (ch == 0 && tid < (int)(head + V - tail0)) {
-            const int64_t j = tid < head ? tid : tail0 + (tid - head);
-            o[j] = none ? (T)0.0f : (T)value((float)row[j], j);
-        }
+        if (edge) o[je] = (T)(value((float)xe) + (je == at ? g : 0.0f));
     }
 }
 
@@ -440,13 +454,18 @@ SF_API int sf_token_logp_grad(const void* logits, int32_t dtype, int64_t N, int6
     const void* ins[5] = {targets, lse, grad_logp, entropy, grad_entropy};
     for (int a = 0; a < 5; ++a)
         if (ins[a] && !disjoint(ins[a], N * (a == 0 ? 8 : 4), out_grad, out_bytes)) return SF_EINVAL;
-    const int64_t e = 16 / b;
-    int64_t chunks = (V / e + kGradVecs - 1) / kGradVecs;
-    if (chunks < 1) chunks = 1;
-    void* args[] = {(void*)&logits,  (void*)&N,         (void*)&V,       (void*)&row_stride,   (void*)&targets,
+    int Vi = (int)V;
+    const int64_t vecs = V / (16 / b);
+    const int lanes = vecs <= 64 * kGradU ? 64 : 256;
+    const int64_t chunks = (vecs + kGradU * lanes - 1) / (kGradU * lanes);
+    const int64_t groups = (N + kRowWG / lanes - 1) / (kRowWG / lanes);
+    void* args[] = {(void*)&logits,  (void*)&N,         (void*)&Vi,      (void*)&row_stride,   (void*)&targets,
                     (void*)&inv_temperature, (void*)&lse, (void*)&grad_logp, (void*)&entropy,
-                    (void*)&grad_entropy, (void*)&out_grad, (void*)&out_row_stride, (void*)&chunks};
-    const void* fn[3] = {(const void*)&k_token_logp_grad<SF_F32>, (const void*)&k_token_logp_grad<SF_BF16>,
-                         (const void*)&k_token_logp_grad<SF_F16>};
-    return launch(fn[dtype], dim3(grid_of(N * chunks)), dim3(kRowWG), args, 0, stream);
+                    (void*)&grad_entropy, (void*)&out_grad, (void*)&out_row_stride};
+    const void* fn[2][3] = {{(const void*)&k_token_logp_grad<SF_F32, 256>, (const void*)&k_token_logp_grad<SF_BF16, 256>,
+                             (const void*)&k_token_logp_grad<SF_F16, 256>},
+                            {(const void*)&k_token_logp_grad<SF_F32, 64>, (const void*)&k_token_logp_grad<SF_BF16, 64>,
+                             (const void*)&k_token_logp_grad<SF_F16, 64>}};
+    return launch(fn[lanes == 64][dtype], dim3((unsigned)(chunks < 1 ? 1 : chunks), (unsigned)(groups < 65535 ? groups : 65535)),
+                  dim3(kRowWG), args, 0, stream);
 }
