@@ -129,6 +129,32 @@ def test_logp_masked_and_extreme_logits(tr, kind):
         torch.testing.assert_close(many.view(120, -1), one.expand(120, -1), rtol=1e-5, atol=1e-5, equal_nan=True)
 
 
+@pytest.mark.parametrize("inv_t", [1e-20, 1e-3, 37.0, 1e4, 1e6, 1e12])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_logp_far_temperatures(tr, kind, inv_t):
+    """From a flat to a certain distribution; the exponents' scale passes every
+    range that the kernel tells apart."""
+    logits = matrix(5, 3001, kind, 21, 1, 1)
+    targets = torch.tensor([0, 7, 3000, -1, 55], device=DEV)
+    targets[4] = logits[4].float().argmax()
+    _, lse, ent = check_logp(tr, logits, targets, inv_t)
+    keep = torch.tensor([0, 1, 2, 4], device=DEV)
+    if inv_t <= 37.0:  # past this the lse's own rounding is more than a probability
+        check_grad(tr, logits[keep], targets[keep], inv_t, lse[keep], ent[keep], True)
+
+
+@pytest.mark.parametrize("share", [0.01, 0.5, 0.999])
+def test_logp_masked_vocabulary(tr, share):
+    """The same entries of -inf in every row, as a constrained decoder has."""
+    logits = matrix(40, 20011, "bf16", 31)
+    drop = torch.rand(20011, generator=torch.Generator().manual_seed(3)) < share
+    drop[[17, 19999]] = False
+    logits[:, drop.to(DEV)] = -math.inf
+    targets = torch.where(torch.arange(40) % 2 == 0, 17, 19999).to(DEV)
+    _, lse, ent = check_logp(tr, logits, targets, 1.0)
+    check_grad(tr, logits, targets, 1.0, lse, ent, True)
+
+
 def test_logp_rows_out_of_reach(tr):
     """Rows that take no part are 0, whatever they hold, and give no gradient."""
     logits = torch.full((4, 700), float("nan"), dtype=torch.bfloat16, device=DEV)
@@ -282,6 +308,29 @@ def test_policy_bool_mask_and_unaligned_views(tr):
                             out_grad=torch.zeros(N + 1, device=DEV)[1:])
     np.testing.assert_array_equal(got[0].cpu().numpy(), want[0])
     np.testing.assert_array_equal(got[1].cpu().numpy(), want[1])
+
+
+def test_policy_past_32_bit_tokens(tr):
+    """More tokens than 2^31, in three sequences; the last begins past them."""
+    N, cut = (1 << 31) + 4099, (1 << 31) + 7
+    lp = torch.full((N,), -1.0, device=DEV)
+    mask = torch.ones(N, dtype=torch.uint8, device=DEV)
+    mask[cut - 3:cut] = 0
+    old = lp.clone()
+    old[5], old[cut + 1] = -2.0, 0.0   # ratios e and 1/e
+    start = torch.tensor([0, 0, cut, N], device=DEV)
+    adv = torch.tensor([9.0, 0.5, -2.0], device=DEV)
+    terms, grad = tr.sf_policy_loss(lp, old, adv, start, mask=mask, reduction=tr.SF_MEAN_SEQUENCES)
+    w1, w2 = 0.5 / (cut - 3), 0.5 / (N - cut)
+    for at, want in ((0, -0.5 * w1), (5, 0.0), (cut - 4, -0.5 * w1), (cut - 1, 0.0), (cut, 2.0 * w2), (cut + 1, 0.0),
+                     (N - 1, 2.0 * w2)):
+        assert abs(grad[at].item() - want) <= 16 * ref.U * abs(want), at
+    # surr: 0.5 everywhere but for the two clipped tokens (1.2 and 0.8 times)
+    want = -0.5 * (cut - 4 + 1.2) * w1 + 2.0 * (N - cut - 1 + 0.8) * w2
+    assert abs(terms[0].item() - want) <= 32 * ref.U * 1.5
+    assert abs(terms[3].item() - (w1 + w2)) <= 16 * ref.U * (w1 + w2)
+    terms, grad = tr.sf_policy_loss(lp, old, adv, start, mask=mask)
+    assert abs(grad[N - 1].item() - 2.0 / (N - 3)) <= 16 * ref.U * 2.0 / (N - 3)
 
 
 # -- gradient norm and clipping --------------------------------------------
