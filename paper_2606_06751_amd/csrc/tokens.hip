@@ -53,7 +53,6 @@ __device__ __forceinline__ void row_rebase(RowState& a, float b, float R, float 
     a.R = R;
 }
 
-constexpr int kRowU = 4;  // vectors of a chunk per lane
 
 // Adds `live` vectors a lane and an edge logit (-inf: none) after taking their
 // maximum.  Lanes without a logit hold -inf, whose e is 0; the bound keeps
@@ -61,13 +60,13 @@ constexpr int kRowU = 4;  // vectors of a chunk per lane
 // its rounding is no longer small beside 1, the reference is the maximum
 // itself, taken off before the product: a row of very low logits, all masked
 // alike, keeps its distribution.
-template <int DT>
-__device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU], int live, float edge, float c)
+template <int DT, int U>
+__device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[U], int live, float edge, float c)
 {
     constexpr int E = kVec<DT>;
     float m = edge;
 #pragma unroll
-    for (int k = 0; k < kRowU; ++k)
+    for (int k = 0; k < U; ++k)
         if (k < live)
 #pragma unroll
             for (int j = 0; j < E; ++j) m = fmaxf(m, (float)y[k][j]);
@@ -76,7 +75,12 @@ __device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU],
         const float top = m * c;
         const bool huge = !(fabsf(top) < 4194304.0f);
         const float b = huge ? m : 0.0f, R = huge ? 0.0f : rintf(top);
-        if (row_height(b, R, c) > row_height(a.b, a.R, c)) row_rebase(a, b, R, c);
+        if (a.R == -INFINITY) {  // the first: nothing to scale
+            a.b = b;
+            a.R = R;
+        } else if (row_height(b, R, c) > row_height(a.b, a.R, c)) {
+            row_rebase(a, b, R, c);
+        }
     }
     const float R = a.R == -INFINITY ? 0.0f : a.R;
     auto add = [&](float v) {
@@ -87,7 +91,7 @@ __device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU],
     };
     add(edge);
 #pragma unroll
-    for (int k = 0; k < kRowU; ++k)
+    for (int k = 0; k < U; ++k)
         if (k < live)
 #pragma unroll
             for (int j = 0; j < E; ++j) add((float)y[k][j]);
@@ -95,13 +99,13 @@ __device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU],
 
 // Adds a full chunk relative to the reference as it is; false where that would
 // lose digits (a term far above 1).
-template <int DT>
-__device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[kRowU], float c)
+template <int DT, int U>
+__device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[U], float c)
 {
-    constexpr int E = kVec<DT>, K = kRowU * E;
+    constexpr int E = kVec<DT>, K = U * E;
     float s = 0.0f, u = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kRowU; ++k)
+    for (int k = 0; k < U; ++k)
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const float t = fmaf((float)y[k][j], c, -a.R);
@@ -109,8 +113,10 @@ __device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[kRowU],
             s += e;
             u = fmaf(e, fmaxf(t, -1000.0f), u);
         }
-    // no term above 2^(1/2) gives K * 1.42 at most
-    if (__any(!(s < 2.0f * K))) return false;
+    // no term above 2^(1/2) gives K * 1.42 at most.  (u is not a number only
+    // where s is not; asked for here, it is summed beside s.  Else the compiler
+    // sums it after the branch, from values that take 105 registers, not 66.)
+    if (__any(!(s < 2.0f * K) || u != u)) return false;
     a.s += s;
     a.u += u;
     return true;
@@ -136,11 +142,22 @@ __device__ __forceinline__ RowState row_merge(RowState a, RowState o, float c)
     return a;
 }
 
-// Joins the states of aligned groups of LANES lanes, in every lane of them.
-template <int LANES>
+// Joins the states that a wave's lanes hold, in every lane.  Without references
+// of huge logits that is a maximum and powers of two.
 __device__ __forceinline__ RowState row_join(RowState a, float c)
 {
-    for (int off = LANES / 2; off > 0; off >>= 1)
+    if (__all(a.b == 0.0f)) {
+        const float top = wave_max_f32(a.R);
+        if (top != -INFINITY) {
+            const float t = a.R - top, e = fast_exp2(t);
+            a.u = e * fmaf(fmaxf(t, -1000.0f), a.s, a.u);
+            a.s *= e;
+            a.R = top;
+        }
+        return row_wave(a);
+    }
+#pragma unroll 1
+    for (int off = 32; off > 0; off >>= 1)
         a = row_merge(a, {__shfl_xor(a.b, off, 64), __shfl_xor(a.R, off, 64), __shfl_xor(a.s, off, 64),
                           __shfl_xor(a.u, off, 64)}, c);
     return a;
@@ -173,7 +190,7 @@ __device__ __forceinline__ void row_write(RowState a, float xt, RowScale z, int6
 // after the last whole vector join the last chunk, one a lane.  Every chunk
 // that needs its maximum goes through one piece of code: where few rows give a
 // compute unit little work, fetching the code is a good part of the time.
-template <int DT, int WG, int WAVES>
+template <int DT, int WG, int WAVES, int U>
 __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* __restrict__ logits, int64_t N, int V,
                                                    int64_t stride, const int64_t* __restrict__ targets, RowScale z,
                                                    int share, float* __restrict__ logp, float* __restrict__ lse,
@@ -181,7 +198,6 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
-    constexpr int U = kRowU;
     constexpr int LANES = WAVES * 64;
     constexpr int ROWS = WG / LANES;
     static_assert(ROWS == 1 || WAVES == 1, "rows of one wave, or one row");
@@ -217,7 +233,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
             if (!last) {
 #pragma unroll
                 for (int k = 0; k < U; ++k) y[k] = __builtin_nontemporal_load((const VecU<DT>*)(body + (int64_t)(v + k * LANES) * E));
-                if (a.b == 0.0f && a.R != -INFINITY && row_try<DT>(a, y, z.c)) continue;
+                if (a.b == 0.0f && a.R != -INFINITY && row_try<DT, U>(a, y, z.c)) continue;
             } else {
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
@@ -226,7 +242,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
                 }
             }
             const int live = last ? (v1 - w + LANES - 1) / LANES : U;
-            row_add<DT>(a, y, live, last && has_edge ? (float)edge : -INFINITY, z.c);
+            row_add<DT, U>(a, y, live, last && has_edge ? (float)edge : -INFINITY, z.c);
             if (last) break;
         }
         a = row_wave(a);
@@ -238,7 +254,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
         __syncthreads();
         if (tid < 64) {
             a = tid < WAVES ? wave_state[tid] : RowState{0.0f, -INFINITY, 0.0f, 0.0f};
-            a = row_join<WAVES>(a, z.c);
+            a = row_join(a, z.c);
             if (tid == 0) {
                 if (P == 1)
                     row_write(a, (float)xt, z, i, logp, lse, entropy);
@@ -267,7 +283,7 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<
         const float xt = (float)logits[i * stride + t];
         RowState a = {0.0f, -INFINITY, 0.0f, 0.0f};
         for (int p = lane; p < P; p += 64) a = row_merge(a, parts[i * P + p], c);
-        a = row_join<64>(a, c);
+        a = row_join(a, c);
         if (lane == 0) row_write(a, xt, z, i, logp, lse, entropy);
     }
 }
@@ -426,12 +442,12 @@ SF_API int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V
     z.eps = (float)(((double)inv_temperature * kLog2eD - (double)z.c) / (double)z.c);
     void* args[] = {(void*)&logits, (void*)&N,     (void*)&Vi,       (void*)&row_stride, (void*)&targets,    (void*)&z,
                     (void*)&share,  (void*)&out_logp, (void*)&out_lse, (void*)&out_entropy, (void*)&workspace};
-    const void* fn[3][3] = {{(const void*)&k_token_logp<SF_F32, 256, 1>, (const void*)&k_token_logp<SF_BF16, 256, 1>,
-                             (const void*)&k_token_logp<SF_F16, 256, 1>},
-                            {(const void*)&k_token_logp<SF_F32, 256, 4>, (const void*)&k_token_logp<SF_BF16, 256, 4>,
-                             (const void*)&k_token_logp<SF_F16, 256, 4>},
-                            {(const void*)&k_token_logp<SF_F32, 1024, 16>, (const void*)&k_token_logp<SF_BF16, 1024, 16>,
-                             (const void*)&k_token_logp<SF_F16, 1024, 16>}};
+    const void* fn[3][3] = {{(const void*)&k_token_logp<SF_F32, 256, 1, 4>, (const void*)&k_token_logp<SF_BF16, 256, 1, 4>,
+                             (const void*)&k_token_logp<SF_F16, 256, 1, 4>},
+                            {(const void*)&k_token_logp<SF_F32, 256, 4, 4>, (const void*)&k_token_logp<SF_BF16, 256, 4, 4>,
+                             (const void*)&k_token_logp<SF_F16, 256, 4, 4>},
+                            {(const void*)&k_token_logp<SF_F32, 1024, 16, 4>, (const void*)&k_token_logp<SF_BF16, 1024, 16, 4>,
+                             (const void*)&k_token_logp<SF_F16, 1024, 16, 4>}};
     const int rows = shape.wg == 64 ? 4 : 1;
     const int rc = launch(fn[shape.wg == 64 ? 0 : shape.wg == 256 ? 1 : 2][dtype], dim3(grid_of((N + rows - 1) / rows), P),
                           dim3(shape.wg == 64 ? 256 : shape.wg), args, 0, stream);
