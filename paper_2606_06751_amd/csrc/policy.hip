@@ -13,9 +13,9 @@
 // 4 consecutive tokens (16-byte loads) and a wave 256 a round, which are mostly
 // of one sequence: it is found once, in LDS, and followed; only in a round that
 // meets another does each lane look for its own (64 tokens a round: 31.7 us for
-// 2e6 tokens of 1024 sequences, 256: 15.6; the kernel alone).  The
-// sums go to a launch of their own: a counter of finished workgroups with the
-// memory fences that it needs cost 25 us more.
+// 2e6 tokens of 1024 sequences, 256: 15.9; the kernel alone).  The sums go to a
+// launch of their own: a counter of finished workgroups with the memory fences
+// that it needs cost 25 us more, since each fence writes back an L2.
 
 #include "sf_device.h"
 #include "sf_host.h"
@@ -409,12 +409,13 @@ __device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk
             if (j < len - off) out[off + j] = g[j];
 }
 
-// What the count left: `n` shares' or parts' counts (P of them a sequence), or
-// a count per sequence and, behind all of them, n workgroups' numbers of
-// sequences that are not empty (P = 0), or nothing (n = 0).
+// What the count left: n counts, of shares of all tokens, or of parts of
+// sequences (1 << shift a sequence); or (many sequences) a count per sequence
+// and, behind all of them, n workgroups' numbers of sequences that are not
+// empty; or nothing (n = 0).
 struct Weights {
     const int64_t* counts;
-    int32_t n, shift;  // P = 1 << shift
+    int32_t n, shift;
 };
 
 // One workgroup, one chunk of tokens.  The sequences that the chunk meets (all
@@ -640,6 +641,10 @@ __global__ __launch_bounds__(kJoinWG) void k_policy_join(int64_t chunks, float k
     if (threadIdx.x == 0) write_terms(sum, kl_coef, terms);
 }
 
+// One workgroup for all of it takes 10.8 us for 5003 tokens, where two or three
+// launches take the host 6 to 10 us more than one.
+static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kFewSeqs; }
+
 // log2 of the workgroups that count a sequence, where there are few: each has
 // about four rounds of 4 KB of mask.
 static inline int count_shift(int64_t N, int64_t B)
@@ -648,8 +653,6 @@ static inline int count_shift(int64_t N, int64_t B)
     while ((B << (shift + 1)) <= kCountMax && (N >> shift) > 16384 * B) ++shift;
     return shift;
 }
-
-static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kFewSeqs; }
 
 struct PolicyLayout {
     int64_t partial, bytes;  // offsets; the counts come first
