@@ -54,16 +54,20 @@ __device__ __forceinline__ void row_rebase(RowState& a, float b, float R, float 
 }
 
 
+// Vectors of a chunk per lane (2 or 8: within 2% at 3072 x 65536; 2 is slower by
+// a third at 2048 x 32000, 8 spills with 1024 threads).
+constexpr int kRowU = 4;
+
 // Adds `live` vectors a lane and an edge logit (-inf: none) after taking their
 // maximum.  Lanes without a logit hold -inf, whose e is 0; the bound keeps
 // 0 * -inf out of u; NaN passes through e.  Where |m c| reaches 2^22, and
 // its rounding is no longer small beside 1, the reference is the maximum
 // itself, taken off before the product: a row of very low logits, all masked
 // alike, keeps its distribution.
-template <int DT, int U>
-__device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[U], int live, float edge, float c)
+template <int DT>
+__device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[kRowU], int live, float edge, float c)
 {
-    constexpr int E = kVec<DT>;
+    constexpr int E = kVec<DT>, U = kRowU;
     float m = edge;
 #pragma unroll
     for (int k = 0; k < U; ++k)
@@ -99,10 +103,10 @@ __device__ __forceinline__ void row_add(RowState& a, const VecU<DT> (&y)[U], int
 
 // Adds a full chunk relative to the reference as it is; false where that would
 // lose digits (a term far above 1).
-template <int DT, int U>
-__device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[U], float c)
+template <int DT>
+__device__ __forceinline__ bool row_try(RowState& a, const VecU<DT> (&y)[kRowU], float c)
 {
-    constexpr int E = kVec<DT>, K = U * E;
+    constexpr int E = kVec<DT>, U = kRowU, K = U * E;
     float s = 0.0f, u = 0.0f;
 #pragma unroll
     for (int k = 0; k < U; ++k)
@@ -190,7 +194,7 @@ __device__ __forceinline__ void row_write(RowState a, float xt, RowScale z, int6
 // after the last whole vector join the last chunk, one a lane.  Every chunk
 // that needs its maximum goes through one piece of code: where few rows give a
 // compute unit little work, fetching the code is a good part of the time.
-template <int DT, int WG, int WAVES, int U>
+template <int DT, int WG, int WAVES>
 __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* __restrict__ logits, int64_t N, int V,
                                                    int64_t stride, const int64_t* __restrict__ targets, RowScale z,
                                                    int share, float* __restrict__ logp, float* __restrict__ lse,
@@ -198,6 +202,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
+    constexpr int U = kRowU;
     constexpr int LANES = WAVES * 64;
     constexpr int ROWS = WG / LANES;
     static_assert(ROWS == 1 || WAVES == 1, "rows of one wave, or one row");
@@ -233,7 +238,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
             if (!last) {
 #pragma unroll
                 for (int k = 0; k < U; ++k) y[k] = __builtin_nontemporal_load((const VecU<DT>*)(body + (int64_t)(v + k * LANES) * E));
-                if (a.b == 0.0f && a.R != -INFINITY && row_try<DT, U>(a, y, z.c)) continue;
+                if (a.b == 0.0f && a.R != -INFINITY && row_try<DT>(a, y, z.c)) continue;
             } else {
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
@@ -242,7 +247,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
                 }
             }
             const int live = last ? (v1 - w + LANES - 1) / LANES : U;
-            row_add<DT, U>(a, y, live, last && has_edge ? (float)edge : -INFINITY, z.c);
+            row_add<DT>(a, y, live, last && has_edge ? (float)edge : -INFINITY, z.c);
             if (last) break;
         }
         a = row_wave(a);
@@ -442,12 +447,12 @@ SF_API int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V
     z.eps = (float)(((double)inv_temperature * kLog2eD - (double)z.c) / (double)z.c);
     void* args[] = {(void*)&logits, (void*)&N,     (void*)&Vi,       (void*)&row_stride, (void*)&targets,    (void*)&z,
                     (void*)&share,  (void*)&out_logp, (void*)&out_lse, (void*)&out_entropy, (void*)&workspace};
-    const void* fn[3][3] = {{(const void*)&k_token_logp<SF_F32, 256, 1, 4>, (const void*)&k_token_logp<SF_BF16, 256, 1, 4>,
-                             (const void*)&k_token_logp<SF_F16, 256, 1, 4>},
-                            {(const void*)&k_token_logp<SF_F32, 256, 4, 4>, (const void*)&k_token_logp<SF_BF16, 256, 4, 4>,
-                             (const void*)&k_token_logp<SF_F16, 256, 4, 4>},
-                            {(const void*)&k_token_logp<SF_F32, 1024, 16, 4>, (const void*)&k_token_logp<SF_BF16, 1024, 16, 4>,
-                             (const void*)&k_token_logp<SF_F16, 1024, 16, 4>}};
+    const void* fn[3][3] = {{(const void*)&k_token_logp<SF_F32, 256, 1>, (const void*)&k_token_logp<SF_BF16, 256, 1>,
+                             (const void*)&k_token_logp<SF_F16, 256, 1>},
+                            {(const void*)&k_token_logp<SF_F32, 256, 4>, (const void*)&k_token_logp<SF_BF16, 256, 4>,
+                             (const void*)&k_token_logp<SF_F16, 256, 4>},
+                            {(const void*)&k_token_logp<SF_F32, 1024, 16>, (const void*)&k_token_logp<SF_BF16, 1024, 16>,
+                             (const void*)&k_token_logp<SF_F16, 1024, 16>}};
     const int rows = shape.wg == 64 ? 4 : 1;
     const int rc = launch(fn[shape.wg == 64 ? 0 : shape.wg == 256 ? 1 : 2][dtype], dim3(grid_of((N + rows - 1) / rows), P),
                           dim3(shape.wg == 64 ? 256 : shape.wg), args, 0, stream);
