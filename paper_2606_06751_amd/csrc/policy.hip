@@ -28,12 +28,15 @@ constexpr int kTok = 4;                 // consecutive tokens of a lane: 16-byte
 constexpr int kRoundTok = 64 * kTok;    // of a wave's round
 constexpr int kPolicyChunk = kPolicyWG / 64 * kRoundTok;  // of a workgroup: a round a wave
 constexpr int kSliceMax = 2048;  // sequences that a workgroup keeps in LDS
-constexpr int kFewSeqs = 1024;   // sequences of which every workgroup keeps all
+// Sequences of which every workgroup keeps all; with more, a chunk's are looked
+// up first (2e6 tokens of 1024: 14.0 us, all of them kept 15.9).
+constexpr int kFewSeqs = 256;
 constexpr int kCountMax = 2048;  // counts that every workgroup adds up by itself
 constexpr int kCountBlocks = 512;
 constexpr int kSmallWG = 1024;
 constexpr int kSmallRounds = 2;
 constexpr int kSmallN = kSmallWG * kTok * kSmallRounds;  // tokens of the one-launch path
+constexpr int kSmallSeqs = kSmallWG;                     // and its sequences
 constexpr int kJoinWG = 512;
 constexpr int kFar = INT32_MAX;
 
@@ -112,8 +115,8 @@ __device__ __forceinline__ void seq_range(const Policy& a, int64_t b, int64_t* s
 }
 
 // Counts of tokens that take part.  SHARES: equal shares of all tokens, one a
-// workgroup.  PARTS (few sequences): part blockIdx.y of gridDim.y of sequence
-// blockIdx.x, by a workgroup.  SEQS (many): whole sequences by one wave each, and
+// workgroup.  PARTS (up to kCountMax): part blockIdx.y of gridDim.y of sequence
+// blockIdx.x, by a workgroup.  SEQS (more): whole sequences by one wave each, and
 // behind them a workgroup's number of those that are not empty.
 enum { COUNT_SHARES, COUNT_PARTS, COUNT_SEQS };
 
@@ -147,7 +150,8 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_count(Policy a, int64_t* _
         // at least a round of 1 KB of mask each
         int64_t share = t1 > t0 ? ((t1 - t0 + pieces - 1) / pieces + 1023) & ~(int64_t)1023 : 0;
         t0 += piece * share;
-        if (t0 < t1) sum = count_mask(a.mask, t0, t0 + share < t1 ? t0 + share : t1);
+        if (t0 + share < t1) t1 = t0 + share;
+        if (t0 < t1) sum = a.mask ? count_mask(a.mask, t0, t1) : t1 - t0;
     }
     if (lane == 0) part[wave] = sum;
     __syncthreads();
@@ -410,12 +414,12 @@ __device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk
 }
 
 // What the count left: n counts, of shares of all tokens, or of parts of
-// sequences (1 << shift a sequence); or (many sequences) a count per sequence
-// and, behind all of them, n workgroups' numbers of sequences that are not
-// empty; or nothing (n = 0).
+// sequences (1 << shift a sequence); or (numbers) a count per sequence and,
+// behind all of them, n workgroups' numbers of sequences that are not empty; or
+// nothing (n = 0).
 struct Weights {
     const int64_t* counts;
-    int32_t n, shift;
+    int32_t n, shift, numbers;
 };
 
 // One workgroup, one chunk of tokens.  The sequences that the chunk meets (all
@@ -454,7 +458,7 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
     // every load of the prologue before the first wait for one
     constexpr int RS = kFewSeqs / kPolicyWG + 1, RC = kCountMax / kPolicyWG;
     int64_t starts[RS], counts[RC];
-    const int64_t* from = wt.counts + (few || a.reduction == SF_MEAN_TOKENS ? 0 : a.B);
+    const int64_t* from = wt.counts + (wt.numbers ? a.B : 0);
 #pragma unroll
     for (int r = 0; r < RS; ++r) starts[r] = fits && tid + r * kPolicyWG <= slice ? a.start[b0 + tid + r * kPolicyWG] : 0;
 #pragma unroll
@@ -483,7 +487,7 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
         int64_t some = 0;
         if (!few) {
 #pragma unroll
-            for (int r = 0; r < RC; ++r) some += counts[r];
+            for (int r = 0; r < RC; ++r) some += wt.numbers ? counts[r] : counts[r] > 0;
         } else {
             if (wt.n == 0) {  // no mask: their lengths
                 for (int k = tid; k < slice; k += kPolicyWG) {
@@ -552,13 +556,13 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
         for (int q = 0; q < 3; ++q) partial[(int64_t)blockIdx.x * 3 + q] = sum[q];
 }
 
-// The whole loss by one workgroup: up to kSmallN tokens in kFewSeqs sequences.
+// The whole loss by one workgroup: up to kSmallN tokens in kSmallSeqs sequences.
 __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __restrict__ out_grad,
                                                            float* __restrict__ out_terms)
 {
-    __shared__ int start[kFewSeqs + 1];
-    __shared__ int count[kFewSeqs];
-    __shared__ float weight[kFewSeqs], seq_adv[kFewSeqs];
+    __shared__ int start[kSmallSeqs + 1];
+    __shared__ int count[kSmallSeqs];
+    __shared__ float weight[kSmallSeqs], seq_adv[kSmallSeqs];
     __shared__ int64_t ints[kSmallWG / 64];
     __shared__ double part[3][kSmallWG / 64];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -643,7 +647,7 @@ __global__ __launch_bounds__(kJoinWG) void k_policy_join(int64_t chunks, float k
 
 // One workgroup for all of it takes 10.8 us for 5003 tokens, where two or three
 // launches take the host 6 to 10 us more than one.
-static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kFewSeqs; }
+static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kSmallSeqs; }
 
 // log2 of the workgroups that count a sequence, where there are few: each has
 // about four rounds of 4 KB of mask.
@@ -663,7 +667,7 @@ static inline int64_t up16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 static inline PolicyLayout policy_layout(int64_t N, int64_t B)
 {
     PolicyLayout l;
-    l.partial = up16((B + kCountBlocks > kCountMax ? B + kCountBlocks : kCountMax) * 8);
+    l.partial = up16((B > kCountMax ? B + kCountBlocks : kCountMax) * 8);
     l.bytes = l.partial + up16((N + kPolicyChunk - 1) / kPolicyChunk * 3 * 8);
     return l;
 }
@@ -740,7 +744,7 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
     double* partial = (double*)((char*)workspace + l.partial);
     int64_t chunks = (N + kPolicyChunk - 1) / kPolicyChunk;
     if (chunks > INT32_MAX) return SF_EINVAL;
-    Weights wt = {counts, 0, 0};
+    Weights wt = {counts, 0, 0, 0};
     if (N > 0 && B > 0 && reduction != SF_SUM_TOKENS && (mask || (reduction == SF_MEAN_SEQUENCES && B > kFewSeqs))) {
         const void* fn;
         dim3 grid;
@@ -750,14 +754,15 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
             wt.n = (int)(want < kCountBlocks ? want : kCountBlocks);
             fn = (const void*)&k_policy_count<COUNT_SHARES>;
             grid = dim3((unsigned)wt.n);
-        } else if (B <= kFewSeqs) {
-            wt.shift = count_shift(N, B);
+        } else if (B <= kCountMax) {
+            wt.shift = B <= kFewSeqs ? count_shift(N, B) : 0;
             wt.n = (int)B << wt.shift;
             fn = (const void*)&k_policy_count<COUNT_PARTS>;
             grid = dim3((unsigned)B, 1u << wt.shift);
         } else {
             const int64_t want = (B + kPolicyWG / 64 - 1) / (kPolicyWG / 64);
             wt.n = (int)(want < kCountBlocks ? want : kCountBlocks);
+            wt.numbers = 1;
             fn = (const void*)&k_policy_count<COUNT_SEQS>;
             grid = dim3((unsigned)wt.n);
         }

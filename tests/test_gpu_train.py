@@ -229,7 +229,8 @@ def run_policy(tr, lp, old, r, adv, per, mask, start, red, scale, lo, hi, beta, 
 @pytest.mark.parametrize("reduction", [0, 1, 2])
 @pytest.mark.parametrize("N,B", [(1, 1), (2, 5), (3, 1), (65, 3), (257, 257), (1023, 7), (1025, 1), (4099, 300),
                                  (9000, 2), (20000, 5000), (70001, 11),
-                                 (8192, 1024), (8193, 1024), (8191, 1025), (30000, 1023), (40000, 1025), (33, 3000)])
+                                 (8192, 1024), (8193, 1024), (8191, 1025), (30000, 1023), (40000, 1025), (33, 3000),
+                                 (9000, 256), (9000, 257), (30000, 2048), (30000, 2049)])
 def test_policy(tr, N, B, reduction):
     lp, old, r, start, rng = policy_inputs(N, B, N + B)
     for per, masked, with_ref in ((False, True, True), (True, False, False), (True, True, True), (False, False, True)):

@@ -61,8 +61,10 @@ def policy(N, B, reduction, mask):
 @pytest.mark.parametrize("N,B,reduction,mask,kernels", [
     (8192, 1024, 1, True, ["small"]), (0, 0, 0, False, ["small"]),
     (8193, 1024, 2, True, ["loss", "join"]), (8193, 1024, 0, False, ["loss", "join"]),
-    (8193, 1024, 1, False, ["loss", "join"]), (8193, 1024, 0, True, ["count<0>", "loss", "join"]),
-    (8193, 1024, 1, True, ["count<1>", "loss", "join"]), (8192, 1025, 1, False, ["count<2>", "loss", "join"]),
+    (8193, 1024, 0, True, ["count<0>", "loss", "join"]),
+    (8193, 1024, 1, True, ["count<1>", "loss", "join"]), (8192, 1025, 1, False, ["count<1>", "loss", "join"]), (8193, 256, 1, False, ["loss", "join"]),
+    (8193, 257, 1, False, ["count<1>", "loss", "join"]), (8193, 2048, 1, True, ["count<1>", "loss", "join"]),
+    (8193, 2049, 1, True, ["count<2>", "loss", "join"]),
     (100000, 5000, 1, True, ["count<2>", "loss", "join"]), (100000, 5000, 0, False, ["loss", "join"]),
     (100000, 0, 1, True, ["loss", "join"]), (0, 2000, 0, True, ["join"])])
 def test_policy_launches(run, N, B, reduction, mask, kernels):
