@@ -101,7 +101,7 @@ __device__ __forceinline__ void chunk_norm(uintptr_t at, int n, double* sum, int
     constexpr int U = kNormU;
     const int tid = threadIdx.x;
     const GlobalElem<DT>* p = (const GlobalElem<DT>*)at;
-    const int head = (int)head_elems<DT>((const void*)at, n);
+    const int head = (int)head_elems<DT, 128>((const void*)at, n);
     const int nv = (n - head) / E, tail0 = head + nv * E;
     const GlobalVec<DT>* body = (const GlobalVec<DT>*)(p + head);
     double s = 0.0;
@@ -289,7 +289,7 @@ __device__ __forceinline__ void chunk_scale(uintptr_t from, uintptr_t to, int n,
     const int tid = threadIdx.x;
     const GlobalElem<DT>* p = (const GlobalElem<DT>*)from;
     GlobalElem<DT>* o = (GlobalElem<DT>*)to;
-    const int head = (int)head_elems<DT>((const void*)to, n);
+    const int head = (int)head_elems<DT, 128>((const void*)to, n);
     const int nv = (n - head) / E, tail0 = head + nv * E;
     const GlobalVec<DT>* pv = (const GlobalVec<DT>*)(p + head);
     GlobalVec<DT>* ov = (GlobalVec<DT>*)(o + head);

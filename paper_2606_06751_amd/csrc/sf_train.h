@@ -42,11 +42,11 @@ using GlobalElem = __attribute__((address_space(1))) typename Elem<DT>::T;
 
 static inline int elem_size(int dtype) { return dtype == SF_F32 ? 4 : 2; }
 
-// Elements from p up to the next 16-byte boundary, at most n.
-template <int DT>
+// Elements from p up to the next ALIGN-byte boundary, at most n.
+template <int DT, int ALIGN>
 __device__ __forceinline__ int64_t head_elems(const void* p, int64_t n)
 {
-    const int64_t h = (int64_t)((0 - (uintptr_t)p) & 15) / (int64_t)sizeof(typename Elem<DT>::T);
+    const int64_t h = (int64_t)((0 - (uintptr_t)p) & (ALIGN - 1)) / (int64_t)sizeof(typename Elem<DT>::T);
     return h < n ? h : n;
 }
 

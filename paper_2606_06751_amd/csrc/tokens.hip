@@ -222,7 +222,7 @@ __global__ __launch_bounds__(WG) void k_token_logp(const typename Elem<DT>::T* _
             continue;
         }
         const T* row = logits + i * stride;
-        const int head = (int)head_elems<DT>(row, V);
+        const int head = (int)head_elems<DT, WAVES == 1 ? 64 : 128>(row, V);
         const int nv = (V - head) / E, tail0 = head + nv * E;
         const T* body = row + head;
         const int v0 = min(nv, p * share), v1 = min(nv, v0 + share);
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
         const float l = lse[i];
         T* o = out + i * out_stride;
         const T* row = logits + i * stride;
-        const int head = (int)head_elems<DT>(o, V);
+        const int head = (int)head_elems<DT, LANES == 64 ? 64 : 128>(o, V);
         const int nv = (V - head) / E, tail0 = head + nv * E;
         const int v0 = (int)blockIdx.x * (kGradU * LANES) + tid;
         VecU<DT>* ov = (VecU<DT>*)(o + head);
@@ -379,7 +379,7 @@ struct RowShape {
 
 // Measured (bf16, us, a wave / 256 / 1024 threads a row / 256 threads in parts):
 //   300 x 1000: 3.4 / 4.0 / 6.4;  4096 x 16000: 27 / 30 / 64;  2048 x 32000:
-//   26.5 / 28.3 / 46;  3072 x 65536: 78 / 70 / 103;  1024 x 16000: 13.0 / 11.7 / 18;
+//   26.5 / 28.3 / 46;  8192 x 8000: 27.5 / 28.5;  8192 x 32003: 96 / 89;  3072 x 65536: 78 / 70 / 103;  1024 x 16000: 13.0 / 11.7 / 18;
 //   512 x 16000: 11.5 / 7.8 / 9.5;  256 x 32000: 17.8 / 8.7 / 7.5;  128 x 65536:
 //   32 / 11.8 / 9.1 / 9.9;  64 x 131072: 59 / 19 / 12.5 / 9.9;  1 x 65536: 25 / 10 /
 //   7.8 / 5.2;  1 x 262144: 105 / 31 / 18 / 6.3.
@@ -387,7 +387,7 @@ struct RowShape {
 static inline RowShape row_shape(int64_t N, int64_t V, int bytes)
 {
     const int64_t row = V * bytes;
-    if (row <= 4096 || (N >= 2048 && row <= 65536)) return {64, 1};
+    if (row <= 4096 || (N >= 2048 && row <= (N < 8192 ? 65536 : 20480))) return {64, 1};
     if (row > 131072 && N <= 64) {
         const int64_t want = 1024 / N, most = row / 8192;
         return {256, (int)(want < most ? want : most)};

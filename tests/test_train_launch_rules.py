@@ -29,6 +29,7 @@ def logp(N, V, dtype=BF16):
     (1, 65537, BF16, ["<1, 256, 4>", "join<1>"]), (64, 65537, BF16, ["<1, 256, 4>", "join<1>"]),
     (65, 65537, BF16, ["<1, 1024, 16>"]), (256, 65537, BF16, ["<1, 1024, 16>"]), (257, 65537, BF16, ["<1, 256, 4>"]),
     (2047, 32768, BF16, ["<1, 256, 4>"]), (2048, 32768, BF16, ["<1, 256, 1>"]), (2048, 32769, BF16, ["<1, 256, 4>"]),
+    (8191, 32768, BF16, ["<1, 256, 1>"]), (8192, 10240, BF16, ["<1, 256, 1>"]), (8192, 10241, BF16, ["<1, 256, 4>"]),
     (2048, 16384, F32, ["<0, 256, 1>"]), (2048, 16385, F32, ["<0, 256, 4>"]), (1, 32769, F32, ["<0, 256, 4>", "join<0>"])])
 def test_rows(run, N, V, dtype, kernels):
     got = run([logp(N, V, dtype)])[0]
