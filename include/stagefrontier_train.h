@@ -128,7 +128,7 @@ enum {
  *                    the tokens [seq_start[b], seq_start[b+1]).  Tokens
  *                    outside every sequence take no part.  (On the device,
  *                    so not checked; other values give unspecified results.)
- *   N, B             0 <= N < 2^40, 0 <= B < 2^31; N == 0 or B == 0 gives
+ *   N, B             0 <= N < 2^34, 0 <= B < 2^31; N == 0 or B == 0 gives
  *                    zeros.
  *   reduction        SF_MEAN_TOKENS, SF_MEAN_SEQUENCES or SF_SUM_TOKENS.
  *   scale            finite factor of every weight.
@@ -162,7 +162,8 @@ int64_t sf_policy_loss_workspace(int64_t N, int64_t B);
  *   grads        host array of n device pointers, each aligned to its element
  *                size; dense tensors in any order of dimensions.  A pointer may
  *                be NULL where numel is 0.
- *   numel        host array of n element counts, 0 <= numel < 2^40.
+ *   numel        host array of n element counts, >= 0, below 2^40 each and in
+ *                all.
  *   dtype        host array of n types (SF_F32, SF_BF16, SF_F16; a list may
  *                mix them).
  *   n            0 <= n <= 2^20.

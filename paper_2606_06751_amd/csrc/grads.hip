@@ -319,7 +319,6 @@ __global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int in
 {
     __shared__ double sums[kGradWG / 64];
     const int tid = threadIdx.x;
-    const uint32_t b = blockIdx.x;
     // the norm of all parts, every workgroup for itself
     double s = 0.0;
     if (m == 1) {
@@ -336,20 +335,21 @@ __global__ __launch_bounds__(kGradWG) void k_grad_clip(ClipArgs a, int n, int in
     const bool wrong = !(s < (double)INFINITY);
     const double c = (double)max_norm / (s + (double)eps);
     const float coef = wrong || !(c < 1.0) ? 1.0f : (float)c;
-    if (wrong && status && b == 0 && tid == 0) atomicOr(status, (uint32_t)SF_ERANGE);
+    if (wrong && status && blockIdx.x == 0 && tid == 0) atomicOr(status, (uint32_t)SF_ERANGE);
     if (coef == 1.0f && in_place) return;
-    if (b >= a.first[n]) return;
-    const int i = find_item<kClipBatch>(a.first, b);
-    const int64_t count = a.numel[i] >> 2;
-    const int dtype = (int)(a.numel[i] & 3);
-    const int64_t e0 = (int64_t)(b - a.first[i]) * kClipChunk;
-    const int len = (int)(count - e0 < kClipChunk ? count - e0 : kClipChunk);
-    if (dtype == SF_F32)
-        chunk_scale<SF_F32>(a.ptr[i] + e0 * 4, a.out[i] + e0 * 4, len, coef);
-    else if (dtype == SF_BF16)
-        chunk_scale<SF_BF16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
-    else
-        chunk_scale<SF_F16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
+    for (uint32_t b = blockIdx.x; b < a.first[n]; b += gridDim.x) {
+        const int i = find_item<kClipBatch>(a.first, b);
+        const int64_t count = a.numel[i] >> 2;
+        const int dtype = (int)(a.numel[i] & 3);
+        const int64_t e0 = (int64_t)(b - a.first[i]) * kClipChunk;
+        const int len = (int)(count - e0 < kClipChunk ? count - e0 : kClipChunk);
+        if (dtype == SF_F32)
+            chunk_scale<SF_F32>(a.ptr[i] + e0 * 4, a.out[i] + e0 * 4, len, coef);
+        else if (dtype == SF_BF16)
+            chunk_scale<SF_BF16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
+        else
+            chunk_scale<SF_F16>(a.ptr[i] + e0 * 2, a.out[i] + e0 * 2, len, coef);
+    }
 }
 
 static inline const GradList* as_list(const void* p)
@@ -411,7 +411,7 @@ SF_API int sf_grad_list_init(void* list, int64_t list_bytes, const void* const* 
         chunks += c;
         most = c > most ? c : most;
     }
-    if (chunks > INT32_MAX) return SF_EINVAL;
+    if (total >= kGradMax) return SF_EINVAL;  // (so fewer than 2^24 chunks and n more)
     GradList* l = new (list) GradList;
     l->magic = 0;
     l->n = n;
@@ -554,7 +554,9 @@ SF_API int sf_grad_clip(const void* list, const void* out_list, const float* nor
             a.first[k] = (uint32_t)((k < k1 ? in[i0 + k].clip_first : stop) - base);
         }
         a.first[kClipBatch] = (uint32_t)(stop - base);
-        const unsigned grid = stop > base ? (unsigned)(stop - base) : 1;
+        // a workgroup a chunk, but fewer than 2^32 threads
+        const int64_t want = stop - base < 1 ? 1 : stop - base;
+        const unsigned grid = (unsigned)(want < (1 << 23) ? want : (1 << 23));
         void* args[] = {(void*)&a,     (void*)&k1, (void*)&same, (void*)&norms,
                         (void*)&m,     (void*)&max_norm, (void*)&eps, (void*)&status};
         const int rc = launch((const void*)&k_grad_clip, dim3(grid), dim3(kGradWG), args, 0, stream);

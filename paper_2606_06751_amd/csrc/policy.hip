@@ -674,7 +674,7 @@ static inline PolicyLayout policy_layout(int64_t N, int64_t B)
 
 static inline bool policy_sizes_ok(int64_t N, int64_t B)
 {
-    return N >= 0 && N < ((int64_t)1 << 40) && B >= 0 && B < ((int64_t)1 << 31);
+    return N >= 0 && N < ((int64_t)1 << 34) && B >= 0 && B < ((int64_t)1 << 31);
 }
 
 }  // namespace sfk
@@ -743,7 +743,6 @@ SF_API int sf_policy_loss(const float* logp, const float* old_logp, const float*
     int64_t* counts = (int64_t*)workspace;
     double* partial = (double*)((char*)workspace + l.partial);
     int64_t chunks = (N + kPolicyChunk - 1) / kPolicyChunk;
-    if (chunks > INT32_MAX) return SF_EINVAL;
     Weights wt = {counts, 0, 0, 0};
     if (N > 0 && B > 0 && reduction != SF_SUM_TOKENS && (mask || (reduction == SF_MEAN_SEQUENCES && B > kFewSeqs))) {
         const void* fn;

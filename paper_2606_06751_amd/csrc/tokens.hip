@@ -402,7 +402,9 @@ static inline bool rows_ok(int32_t dtype, int64_t N, int64_t V, int64_t stride, 
            (N == 0 || stride <= (((int64_t)1 << 56) / N));
 }
 
-static inline unsigned grid_of(int64_t n) { return (unsigned)(n < (1 << 30) ? n : (1 << 30)); }
+// Workgroups for n units; the kernels take the rest in turns.  (A launch has
+// fewer than 2^32 threads a dimension.)
+static inline unsigned grid_of(int64_t n) { return (unsigned)(n < (1 << 21) ? n : (1 << 21)); }
 
 }  // namespace sfk
 

@@ -107,7 +107,7 @@ def test_policy_refusals(tr, lib):
 
     need = lib.sf_policy_loss_workspace(100000, 10)
     assert need > 0
-    for bad in (dict(N=-1), dict(B=-1), dict(N=1 << 40), dict(B=1 << 31), dict(red=-1), dict(red=3), dict(sc=nan),
+    for bad in (dict(N=-1), dict(B=-1), dict(N=1 << 34), dict(B=1 << 31), dict(red=-1), dict(red=3), dict(sc=nan),
                 dict(sc=inf), dict(lo=1.0), dict(lo=-0.1), dict(lo=nan), dict(hi=-0.1), dict(hi=inf), dict(kl=nan),
                 dict(lp=None), dict(old=None), dict(adv=None), dict(start=None), dict(terms=None), dict(grad=None),
                 dict(ws=None), dict(wb=need - 1), dict(ws=W + 8), dict(lp=A + 2), dict(start=F + 4), dict(terms=G + 2),
