@@ -13,7 +13,7 @@
 // 4 consecutive tokens (16-byte loads) and a wave 256 a round, which are mostly
 // of one sequence: it is found once, in LDS, and followed; only in a round that
 // meets another does each lane look for its own (64 tokens a round: 31.7 us for
-// 2e6 tokens of 1024 sequences, 256: 15.9; the kernel alone).  The sums go to a
+// 2e6 tokens of 1024 sequences, 256: 14.4; the kernel alone).  The sums go to a
 // launch of their own: a counter of finished workgroups with the memory fences
 // that it needs cost 25 us more, since each fence writes back an L2.
 
