@@ -58,8 +58,9 @@ enum {
  *                    may be NULL where that is 0.
  *
  * Logits of -inf have probability 0.  A row of nothing else has no
- * distribution: logp = lse = -inf, H = 0.  A row that holds +inf or NaN gives
- * NaN.  Returns SF_OK, SF_EINVAL or SF_EHIP.
+ * distribution: logp = lse = -inf, H = 0.  In any other row lse is held within
+ * the largest floats, so that -inf says this alone.  A row that holds +inf or
+ * NaN gives NaN.  Returns SF_OK, SF_EINVAL or SF_EHIP.
  */
 int sf_token_logp(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t row_stride,
                   const int64_t* targets, float inv_temperature, float* out_logp, float* out_lse,
@@ -75,6 +76,10 @@ int64_t sf_token_logp_workspace(int32_t dtype, int64_t N, int64_t V);
  * sf_token_logp_grad -- the gradient of sf_token_logp's outputs back to the
  * logits.  With g = grad_logp[i] and h = grad_entropy[i] (0 where NULL),
  *     out[j] = inv_temperature * (g ([j = t] - p_j) - h p_j (log p_j + H)).
+ * log p_j = z_j - lse with lse as given while |lse| < 2^16, where its rounding is
+ * a relative error of p of 2^-24 |lse|, up to 2^-9.  In a row with lse
+ * beyond, whose logits lie far from 0, the kernel takes log p_j relative to the
+ * row's maximum, with a sum of its own over the row; lse then only says so.
  *
  *   logits, dtype, N, V, row_stride, targets, inv_temperature: as for
  *                    sf_token_logp.

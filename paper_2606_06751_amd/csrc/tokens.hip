@@ -181,7 +181,9 @@ __device__ __forceinline__ void row_write(RowState a, float xt, RowScale z, int6
     // the exponents are off by c's own rounding, which turns log p by their
     // distance from the mean and lse by the mean
     logp[i] = fmaf(t, kLn2, -ls) + (t > -1000.0f ? turn * (t - mean) : 0.0f);
-    lse[i] = a.b == 0.0f ? fmaf(a.R, kLn2, fmaf(a.R, kLn2Low, ls)) + turn * (a.R + mean) : fmaf(a.b, z.inv_t, ls);
+    // held within the floats: -inf is for rows that have no distribution
+    const float l = a.b == 0.0f ? fmaf(a.R, kLn2, fmaf(a.R, kLn2Low, ls)) + turn * (a.R + mean) : fmaf(a.b, z.inv_t, ls);
+    lse[i] = fabsf(l) == INFINITY ? copysignf(kF32Max, l) : l;
     if (entropy) {
         const float h = ls - kLn2 * mean;
         entropy[i] = h < 0.0f ? 0.0f : h;
@@ -301,6 +303,50 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<
 // 1 / both 1212, 2 / loads 1210, 2 / both 1298, 2 / none 1237, 4 / both 1362 us;
 // at 512 x 100003 41.5, 37.1, 37.8, 41.3, 39.1.
 constexpr int kGradU = 2;
+// From this |lse| on (2^16) its own rounding, up to 2^-24 of it and with that
+// an error of log p, passes that of a bfloat16, 2^-9 of p, and from 2^24 on
+// nothing is left of p.  Such a row takes its normaliser from its logits again.
+constexpr float kFarLse = 65536.0f;
+
+// -p (g + h (log p + H)) = -p (k0 + h q), q = log p; the bound keeps 0 * -inf out.
+// exp2f keeps probabilities below 2^-126, which h and T may raise again.
+__device__ __forceinline__ float grad_term(float q, float h, float k0)
+{
+    return -exp2f(q * kLog2e) * fmaf(h, fmaxf(q, -1000.0f), k0);
+}
+
+// Such a row by LANES lanes, each of which reads the elements that it writes:
+// log p = (x - m) / T - log s with the row's maximum m, s = sum e^((x - m) / T).
+template <int DT, int LANES>
+__device__ __forceinline__ void far_row(const typename Elem<DT>::T* row, int V, float inv_t, int tid, float* part, int at,
+                                        float g, float h, float entropy, typename Elem<DT>::T* o)
+{
+    typedef typename Elem<DT>::T T;
+    constexpr int NW = LANES / 64;
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll 1
+    for (int j = tid; j < V; j += LANES) m = fmaxf(m, (float)row[j]);
+    m = wave_max_f32(m);
+    if (NW > 1) {
+        __syncthreads();  // a former row's sums are read
+        if ((tid & 63) == 0) part[tid >> 6] = m;
+        __syncthreads();
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, part[w]);
+    }
+#pragma unroll 1
+    for (int j = tid; j < V; j += LANES) s += exp2f(((float)row[j] - m) * inv_t * kLog2e);
+    s = wave_sum_f32(s);
+    if (NW > 1) {
+        if ((tid & 63) == 0) part[NW + (tid >> 6)] = s;
+        __syncthreads();
+        s = 0.0f;
+        for (int w = 0; w < NW; ++w) s += part[NW + w];
+    }
+    const float ls = logf(s), k0 = fmaf(h, entropy, g);
+#pragma unroll 1
+    for (int j = tid; j < V; j += LANES)
+        o[j] = (T)(grad_term(fmaf((float)row[j] - m, inv_t, -ls), h, k0) + (j == at ? g : 0.0f));
+}
 
 template <int DT, int LANES>
 __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<DT>::T* logits, int64_t N, int V,
@@ -314,6 +360,7 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
     constexpr int ROWS = kRowWG / LANES;
+    __shared__ float part[2 * LANES / 64];
     const int tid = threadIdx.x & (LANES - 1);
     const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
     for (int64_t i = (int64_t)blockIdx.y * ROWS + sub; i < N; i += (int64_t)gridDim.y * ROWS) {
@@ -335,6 +382,13 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
             if (edge) o[je] = (T)0.0f;
             continue;
         }
+        if (fabsf(l) >= kFarLse) {
+            // the whole row by the lanes of its first chunk, so that none reads what another wrote in place
+            if (blockIdx.x == 0)
+                far_row<DT, LANES>(row, V, inv_t, tid, part, (int)t, grad_logp[i] * inv_t,
+                                   grad_entropy ? grad_entropy[i] * inv_t : 0.0f, grad_entropy ? entropy[i] : 0.0f, o);
+            continue;
+        }
         VecU<DT> x[kGradU];
 #pragma unroll
         for (int k = 0; k < kGradU; ++k)
@@ -342,14 +396,9 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
         const T xe = row[edge ? je : 0];
         const float g = grad_logp[i] * inv_t;
         const float h = grad_entropy ? grad_entropy[i] * inv_t : 0.0f;
-        // -(g + h (log p + H)) = -(k0 + h log p); the bound keeps 0 * -inf out
         const float k0 = grad_entropy ? fmaf(h, entropy[i], g) : g;
         const int at = (int)t;
-        auto value = [&](float z) {
-            const float q = fmaf(z, inv_t, -l);  // log p
-            // exp2f keeps probabilities below 2^-126, which h and T may raise again
-            return -exp2f(q * kLog2e) * fmaf(h, fmaxf(q, -1000.0f), k0);
-        };
+        auto value = [&](float z) { return grad_term(fmaf(z, inv_t, -l), h, k0); };
 #pragma unroll
         for (int k = 0; k < kGradU; ++k) {
             const int v = v0 + k * LANES;
