@@ -121,8 +121,8 @@ enum {
  *     out_grad  = d out_terms[0] / d logp.
  * A token is clipped (and passes no gradient through r) where A > 0 and
  * d > log(1 + clip_high), or A < 0 and d < log(1 - clip_low).  r and e^x are
- * held at the largest float, so an advantage of 0 stays 0.  Tokens are summed
- * in 64 bits, in a fixed order.
+ * held at the largest float, so an advantage of 0 stays 0.  Tokens are weighed
+ * and summed in 64 bits, in a fixed order.
  *
  *   logp, old_logp   [N] float.
  *   ref_logp         [N] float or NULL.

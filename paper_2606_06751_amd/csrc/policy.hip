@@ -165,7 +165,8 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_count(Policy a, int64_t* _
 }
 
 struct TokenTerms {
-    float surr, kl, clipped, grad;
+    float surr, kl, grad;
+    bool clipped;
 };
 
 // e^x, within 2 units in the last place: 2^(x log2 e) with the product's
@@ -206,7 +207,7 @@ __device__ __forceinline__ TokenTerms token_terms(const Policy& a, float logp, f
     const bool clipped = up ? d > a.log_hi : adv < 0.0f && d < a.log_lo;
     float ratio = exp_f32(d);
     ratio = ratio == INFINITY ? kF32Max : ratio;
-    r.clipped = clipped ? 1.0f : 0.0f;
+    r.clipped = clipped;
     r.surr = -adv * (clipped ? (up ? a.hi : a.lo) : ratio);
     r.grad = clipped ? 0.0f : r.surr;
     r.kl = 0.0f;
@@ -355,9 +356,19 @@ __device__ __forceinline__ void group_terms(double (&sum)[3], double (*part)[WG 
         }
 }
 
-// Adds a lane's tokens with their weights and advantages to its sums (of a few
-// tokens each; a workgroup's are in 64 bits); their gradients.
-__device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint32_t on, v4f w, v4f adv, float (&sum)[3])
+// Adds a token with its weight to the sums, in 64 bits, where no product of two
+// floats overflows or rounds.
+__device__ __forceinline__ void add_terms(const TokenTerms& r, float w, bool on, double (&sum)[3])
+{
+    const double d = on ? (double)w : 0.0;
+    sum[0] = fma(d, on ? (double)r.surr : 0.0, sum[0]);
+    sum[1] = fma(d, on ? (double)r.kl : 0.0, sum[1]);
+    sum[2] += r.clipped ? d : 0.0;
+}
+
+// Adds a lane's tokens with their weights and advantages to its sums; their
+// gradients.
+__device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint32_t on, v4f w, v4f adv, double (&sum)[3])
 {
     v4f g;
 #pragma unroll
@@ -365,9 +376,7 @@ __device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint
         const TokenTerms r = token_terms(a, x.lp[j], x.old[j], x.ref[j], adv[j]);
         const bool is_on = on >> j & 1;
         g[j] = is_on ? w[j] * r.grad : 0.0f;
-        sum[0] += is_on ? w[j] * r.surr : 0.0f;
-        sum[1] += is_on ? w[j] * r.kl : 0.0f;
-        sum[2] += is_on ? w[j] * r.clipped : 0.0f;
+        add_terms(r, w[j], is_on, sum);
     }
     return g;
 }
@@ -375,7 +384,7 @@ __device__ __forceinline__ v4f add_tokens(const Policy& a, const Tokens& x, uint
 // One round: the tokens' weights and advantages by their sequences (the slice's,
 // in LDS), their terms and gradients.
 __device__ __forceinline__ void add_round(const Policy& a, const Tokens& x, Walk& walk, int t, int off, int len,
-                                          const float* seq_adv, const float* weight, float (&sum)[3], float* out)
+                                          const float* seq_adv, const float* weight, double (&sum)[3], float* out)
 {
     v4f w = {0.0f, 0.0f, 0.0f, 0.0f}, adv = x.adv;
     uint32_t on = x.on;
@@ -526,11 +535,11 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
         }
         __syncthreads();
     }
-    float sums[3] = {0.0f, 0.0f, 0.0f};
+    double sum[3] = {0.0, 0.0, 0.0};
     float* grad = out_grad + wave0;
     if (fits) {
         Walk walk = walk_from(start, (int)slice, first);
-        if (len > 0) add_round(a, x, walk, first, lane * kTok, len, seq_adv, weight, sums, grad);
+        if (len > 0) add_round(a, x, walk, first, lane * kTok, len, seq_adv, weight, sum, grad);
     } else {
 #pragma unroll 1
         for (int off = lane; off < len; off += 64) {
@@ -543,14 +552,11 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
                                                  a.adv_per_token ? a.adv[wave0 + off] : a.adv[k - 1]);
                 const float w = weight_of(k - 1 - b0);
                 g = w * r.grad;
-                sums[0] += w * r.surr;
-                sums[1] += w * r.kl;
-                sums[2] += w * r.clipped;
+                add_terms(r, w, true, sum);
             }
             grad[off] = g;
         }
     }
-    double sum[3] = {(double)sums[0], (double)sums[1], (double)sums[2]};
     group_terms<kPolicyWG>(sum, part);
     if (tid == 0)
         for (int q = 0; q < 3; ++q) partial[(int64_t)blockIdx.x * 3 + q] = sum[q];
@@ -619,15 +625,14 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
         if (!a.adv_per_token) seq_adv[tid] = adv;
     }
     __syncthreads();
-    float sums[3] = {0.0f, 0.0f, 0.0f};
+    double sum[3] = {0.0, 0.0, 0.0};
     Walk walk = walk_from(start, B, first);
 #pragma unroll 1
     for (int q = 0; q < len; q += kRoundTok) {
         const Tokens x = next;
         next = load_tokens(a, first, q + kRoundTok + lane * kTok, len);
-        add_round(a, x, walk, first + q, q + lane * kTok, len, seq_adv, weight, sums, out_grad + first);
+        add_round(a, x, walk, first + q, q + lane * kTok, len, seq_adv, weight, sum, out_grad + first);
     }
-    double sum[3] = {(double)sums[0], (double)sums[1], (double)sums[2]};
     group_terms<kSmallWG>(sum, part);
     if (tid == 0) write_terms(sum, a.kl_coef, out_terms);
 }
