@@ -116,7 +116,7 @@ enum {
  *     surr = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
  *     x = ref_logp - logp,  kl = e^x - x - 1            (0 without ref_logp)
  *     loss = surr + kl_coef * kl
- * and over tokens, with w the reduction's weight times scale,
+ * and over tokens, with w the reduction's weight times scale, rounded once,
  *     out_terms = { sum w loss, sum w surr, sum w kl, sum w [clipped] }
  *     out_grad  = d out_terms[0] / d logp.
  * A token is clipped (and passes no gradient through r) where A > 0 and

@@ -219,6 +219,9 @@ __device__ __forceinline__ TokenTerms token_terms(const Policy& a, float logp, f
     return r;
 }
 
+// scale / n for a count n, and 0 where nothing takes part; one rounding.
+__device__ __forceinline__ float share_of(float scale, double n) { return n > 0.0 ? (float)((double)scale / n) : 0.0f; }
+
 // Sum over a workgroup of WG threads, in every thread.
 template <int WG>
 __device__ __forceinline__ int64_t group_sum(int64_t v, int64_t* part)
@@ -485,18 +488,19 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
 
     // one weight for all tokens, or one per sequence
     float scale = a.scale;
+    double some = 0.0;  // sequences that are not empty
     if (a.reduction == SF_MEAN_TOKENS) {
         int64_t all = 0;
 #pragma unroll
         for (int r = 0; r < RC; ++r) all += counts[r];
         if (wt.n == 0 && tid == 0) all = clamp_tok(a.start[a.B], a.N) - clamp_tok(a.start[0], a.N);
         all = group_sum<kPolicyWG>(all, ints);
-        scale = all > 0 ? scale / (float)all : 0.0f;
+        scale = share_of(scale, (double)all);
     } else if (a.reduction == SF_MEAN_SEQUENCES) {
-        int64_t some = 0;
+        int64_t mine = 0;
         if (!few) {
 #pragma unroll
-            for (int r = 0; r < RC; ++r) some += wt.numbers ? counts[r] : counts[r] > 0;
+            for (int r = 0; r < RC; ++r) mine += wt.numbers ? counts[r] : counts[r] > 0;
         } else {
             if (wt.n == 0) {  // no mask: their lengths
                 for (int k = tid; k < slice; k += kPolicyWG) {
@@ -517,16 +521,14 @@ __global__ __launch_bounds__(kPolicyWG) void k_policy_loss(Policy a, Weights wt,
                         atomicAdd(&count[(tid + r * kPolicyWG) >> wt.shift], (unsigned long long)counts[r]);
                 __syncthreads();
             }
-            for (int k = tid; k < slice; k += kPolicyWG) some += count[k] > 0;
+            for (int k = tid; k < slice; k += kPolicyWG) mine += count[k] > 0;
         }
-        some = group_sum<kPolicyWG>(some, ints);
-        scale = some > 0 ? scale / (float)some : 0.0f;
+        some = (double)group_sum<kPolicyWG>(mine, ints);
     }
     __syncthreads();
     auto weight_of = [&](int64_t k) {
         if (a.reduction != SF_MEAN_SEQUENCES) return scale;
-        const float n = few ? (float)count[k] : (float)wt.counts[b0 + k];
-        return n > 0.0f ? scale / n : 0.0f;
+        return share_of(scale, some * (few ? (double)count[k] : (double)wt.counts[b0 + k]));
     };
     if (fits) {
         for (int k = tid; k < slice; k += kPolicyWG) {
@@ -591,6 +593,7 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
     }
     __syncthreads();
     float scale = a.scale;
+    double some = 0.0;  // sequences that are not empty
     if (a.reduction == SF_MEAN_TOKENS) {
         int64_t n = 0;
 #pragma unroll
@@ -599,7 +602,7 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
             n += (ons >> q & 1) && t >= start[0] && t < start[B];
         }
         n = group_sum<kSmallWG>(n, ints);
-        scale = n > 0 ? scale / (float)n : 0.0f;
+        scale = share_of(scale, (double)n);
     } else if (a.reduction == SF_MEAN_SEQUENCES) {
         Walk walk = walk_from(start, B, first);
         uint32_t left = ons;
@@ -617,11 +620,10 @@ __global__ __launch_bounds__(kSmallWG) void k_policy_small(Policy a, float* __re
             }
         }
         __syncthreads();
-        const int64_t n = group_sum<kSmallWG>(tid < B && count[tid] > 0, ints);
-        scale = n > 0 ? scale / (float)n : 0.0f;
+        some = (double)group_sum<kSmallWG>(tid < B && count[tid] > 0, ints);
     }
     if (tid < B) {
-        weight[tid] = a.reduction != SF_MEAN_SEQUENCES ? scale : count[tid] > 0 ? scale / (float)count[tid] : 0.0f;
+        weight[tid] = a.reduction != SF_MEAN_SEQUENCES ? scale : share_of(scale, some * count[tid]);
         if (!a.adv_per_token) seq_adv[tid] = adv;
     }
     __syncthreads();

@@ -1,4 +1,5 @@
-"""What the policy loss promises of its numbers: tokens summed in 64 bits."""
+"""What the policy loss promises of its numbers: tokens summed in 64 bits,
+weights rounded once."""
 import numpy as np
 import pytest
 
@@ -57,3 +58,22 @@ def test_large_terms_do_not_overflow(tr, N, B):
     # of the term, and the loss's own rounding
     assert abs(terms[0] - beta * N * each) <= 8 * 2.0 ** -24 * beta * N * each
     assert terms[2] == np.inf and terms[1] == 0
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("reduction", [0, 1])
+@pytest.mark.parametrize("N,B", PATHS + [(30000, 200), (30000, 3000), (8191, 77)])
+def test_weights_round_once(tr, N, B, reduction, masked):
+    """On-policy tokens with advantage -1 have their weight as gradient."""
+    rng = np.random.default_rng(N + B)
+    start = np.concatenate([[0], np.sort(rng.integers(0, N + 1, B - 1)), [N]]).astype(np.int64)
+    mask = (rng.random(N) < 0.7).astype(np.uint8) if masked else None
+    on = np.ones(N, bool) if mask is None else mask != 0
+    zero = np.zeros(N, np.float32)
+    _, grad = loss(tr, zero, zero, np.full(B, -1.0, np.float32), start, mask=mask, reduction=reduction, scale=0.7)
+    scale = float(np.float32(0.7))
+    seq = np.searchsorted(start, np.arange(N), side="right") - 1
+    count = np.bincount(seq[on], minlength=B)
+    share = on.sum() if reduction == 0 else (count > 0).sum() * count[seq]
+    want = np.where(on, scale / np.maximum(share, 1), 0.0).astype(np.float32)
+    np.testing.assert_array_equal(grad, want)
