@@ -169,14 +169,18 @@ struct TokenTerms {
     bool clipped;
 };
 
-// e^x, within 2 units in the last place: 2^(x log2 e) with the product's
-// rounding put right (but where 2^ of it is 0 or infinite anyway).
+// e^x, within 2 units in the last place wherever it is a float: 2^(x log2 e)
+// with the product's rounding put right.  The instruction gives 0 where its
+// result is below the normal range, so there it runs 2^64 higher.
 __device__ __forceinline__ float exp_f32(float x)
 {
+#pragma clang fp contract(off)  // h + 64 is the rounded h's, exactly
     const float h = x * kLog2e;
     const float l = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -h));
-    const float e = fast_exp2(h);
-    return fabsf(h) < 127.0f ? fmaf(e, l * kLn2, e) : e;
+    const bool low = h < -126.0f;
+    const float e = fast_exp2(low ? h + 64.0f : h);
+    const float r = fabsf(h) < 128.0f + 64.0f && e != INFINITY ? fmaf(e, l * kLn2, e) : e;
+    return low ? r * 0x1p-64f : r;
 }
 
 // e^x - x - 1 and e^x - 1.  Near 0 both differences cancel, so a series takes

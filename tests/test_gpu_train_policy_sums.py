@@ -1,5 +1,5 @@
 """What the policy loss promises of its numbers: tokens summed in 64 bits,
-weights rounded once."""
+weights rounded once, e^x right over the whole range of floats."""
 import numpy as np
 import pytest
 
@@ -77,3 +77,30 @@ def test_weights_round_once(tr, N, B, reduction, masked):
     share = on.sum() if reduction == 0 else (count > 0).sum() * count[seq]
     want = np.where(on, scale / np.maximum(share, 1), 0.0).astype(np.float32)
     np.testing.assert_array_equal(grad, want)
+
+
+def within_ulps(got, want, n, what):
+    off = np.abs(got.astype(np.float64) - want) / np.spacing(np.abs(want).astype(np.float32)).astype(np.float64)
+    assert (off <= n).all(), "%s: %.1f units in the last place at %d" % (what, off.max(), np.argmax(off))
+
+
+@pytest.mark.parametrize("N,B", PATHS[2:4])
+def test_ratio_over_the_whole_range(tr, N, B):
+    """r = e^d within 2 units in the last place wherever it is a float."""
+    d = np.concatenate([np.linspace(-103.0, 88.72, N - 2000), np.linspace(88.0, 88.7228, 1000),
+                        np.linspace(-103.2, -87.0, 1000)]).astype(np.float32)
+    adv = np.where(d <= 0, 1.0, -1.0).astype(np.float32)  # never clipped
+    _, grad = loss(tr, d, np.zeros(N, np.float32), adv, starts(N, B), advantage_per_token=True, reduction=2)
+    within_ulps(-grad * adv, np.exp(d.astype(np.float64)), 2.0, "ratio")
+    far = np.array([-1e30, -np.inf, -200.0, 88.73, 100.0, 1e30, np.inf] + [0.0] * (N - 7), np.float32)
+    adv = np.where(far <= 0, 1.0, -1.0).astype(np.float32)
+    _, grad = loss(tr, far, np.zeros(N, np.float32), adv, starts(N, B), advantage_per_token=True, reduction=2)
+    assert not grad[:3].any() and (grad[3:7] == np.finfo(np.float32).max).all()
+
+
+def test_kl_near_the_largest_float(tr):
+    N = 4000
+    x = np.linspace(85.0, 88.7228, N).astype(np.float32)
+    zero = np.zeros(N, np.float32)
+    _, grad = loss(tr, zero, zero, zero[:1], starts(N, 1), ref=x, reduction=2, kl_coef=1.0)
+    within_ulps(-grad, np.expm1(x.astype(np.float64)), 3.0, "e^x - 1")  # and the difference's own rounding
