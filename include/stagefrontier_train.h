@@ -219,8 +219,10 @@ int64_t sf_grad_norm_workspace(const void* list);
  *               gradients are left (copied) as they are and SF_ERANGE is
  *               OR-ed into *status; the library never clears it.
  *
- * In place with c = 1 the gradients are neither read nor written.  Returns
- * SF_OK, SF_EINVAL or SF_EHIP.
+ * In place with c = 1 the gradients are neither read nor written.  A list of
+ * n == 0 tensors is a no-op that launches nothing and leaves *status; a rank
+ * without gradients that wants the status of the others lists one tensor of 0
+ * entries.  Returns SF_OK, SF_EINVAL or SF_EHIP.
  */
 int sf_grad_clip(const void* list, const void* out_list, const float* norms, int64_t m,
                  float max_norm, float eps, uint32_t* status, sf_stream_t stream);

@@ -214,6 +214,22 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+def _lay_out(tensors):
+    """The C list of tensors (``sf_grad_list_init``)."""
+    n = len(tensors)
+    size = _lib.sf_grad_list_bytes(n)
+    if size < 0:
+        raise StageFrontierError(SF_EINVAL, "sf_grad_list_init")
+    made = (ctypes.c_int64 * ((size + 7) // 8))()
+    ptrs = (ctypes.c_void_p * n)(*(t.data_ptr() for t in tensors))
+    numel = (ctypes.c_int64 * n)(*(t.numel() for t in tensors))
+    dtype = (ctypes.c_int32 * n)(*(_DTYPES[t.dtype] for t in tensors))
+    rc = _lib.sf_grad_list_init(made, size, ptrs, numel, dtype, n)
+    if rc != SF_OK:
+        raise StageFrontierError(rc, "sf_grad_list_init")
+    return made
+
+
 class GradSet:
     """A list of gradient tensors laid out for ``sf_grad_norm`` and
     ``sf_grad_clip`` (``sf_grad_list_init``), checked once.
@@ -225,7 +241,6 @@ class GradSet:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        n = len(self.tensors)
         self.device = None
         for k, t in enumerate(self.tensors):
             if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
@@ -238,16 +253,9 @@ class GradSet:
                 raise ValueError("gradient %d is on %s, the others on %s" % (k, t.device, self.device))
             if not _dense(t):
                 raise ValueError("gradient %d must fill its memory without gaps" % k)
-        size = _lib.sf_grad_list_bytes(n)
-        if size < 0:
-            raise StageFrontierError(SF_EINVAL, "sf_grad_list_init")
-        self._list = (ctypes.c_int64 * ((size + 7) // 8))()
-        ptrs = (ctypes.c_void_p * n)(*(t.data_ptr() for t in self.tensors))
-        numel = (ctypes.c_int64 * n)(*(t.numel() for t in self.tensors))
-        dtype = (ctypes.c_int32 * n)(*(_DTYPES[t.dtype] for t in self.tensors))
-        rc = _lib.sf_grad_list_init(self._list, size, ptrs, numel, dtype, n)
-        if rc != SF_OK:
-            raise StageFrontierError(rc, "sf_grad_list_init")
+        self._list = _lay_out(self.tensors)
+        # a list of no tensors launches nothing: one without entries has a clip's status set
+        self._clip_list = self._list if self.tensors else _lay_out([torch.empty(0, dtype=torch.float32)])
         self._order = [None if t.is_contiguous() else t.stride() for t in self.tensors]
         self.workspace_bytes = int(_lib.sf_grad_norm_workspace(self._list))
 
@@ -294,7 +302,7 @@ def sf_grad_clip(grads, norms: torch.Tensor, max_norm: float, eps: float = 1e-6,
     gradients go (a ``GradSet`` or tensors of the same types and layouts), by
     default in place.  ``status``, a one-element int32 tensor, takes
     ``SF_ERANGE`` where the norm is not finite and the gradients are left as
-    they are.  Returns the set of scaled gradients.
+    they are, also on a rank that has none.  Returns the set of scaled gradients.
     """
     if not isinstance(grads, GradSet):
         grads = GradSet(grads)
@@ -315,7 +323,7 @@ def sf_grad_clip(grads, norms: torch.Tensor, max_norm: float, eps: float = 1e-6,
     _check(norms, "norms", torch.float32, norms.shape, like)
     if status is not None:
         _check(status, "status", torch.int32, (1,), like)
-    rc = _lib.sf_grad_clip(grads._list, out._list, norms.data_ptr(), norms.shape[0], max_norm, eps,
+    rc = _lib.sf_grad_clip(grads._clip_list, out._clip_list, norms.data_ptr(), norms.shape[0], max_norm, eps,
                            None if status is None else status.data_ptr(), _stream_handle(stream, like.device))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_grad_clip")
