@@ -36,6 +36,7 @@ constexpr int64_t kGradMax = (int64_t)1 << 40;
 // Entries of a chunk: the norm's from 4 K up to 64 K, about 4096 chunks where
 // that is enough; the clip's.
 constexpr int64_t kChunkMax = 1 << 16, kChunkWant = 4096;
+constexpr int64_t kChunkMost = 1 << 23;  // and n more, of 256 threads each
 constexpr int64_t kClipChunk = 8192;
 
 struct GradItem {
@@ -403,15 +404,16 @@ SF_API int sf_grad_list_init(void* list, int64_t list_bytes, const void* const* 
         if (numel[i] > 0 && (!grads[i] || !aligned(grads[i], elem_size(dtype[i])))) return SF_EINVAL;
         total += numel[i];
     }
+    if (total >= kGradMax) return SF_EINVAL;
+    // (past 2^39 entries longer ones: a launch has fewer than 2^32 threads)
     int64_t chunk = 4096;
-    while (chunk < kChunkMax && chunk * kChunkWant < total) chunk *= 2;
+    while ((chunk < kChunkMax && chunk * kChunkWant < total) || total / chunk >= kChunkMost) chunk *= 2;
     int64_t chunks = 0, most = 0;
     for (int32_t i = 0; i < n; ++i) {
         const int64_t c = (numel[i] + chunk - 1) / chunk;
         chunks += c;
         most = c > most ? c : most;
     }
-    if (total >= kGradMax) return SF_EINVAL;  // (so fewer than 2^24 chunks and n more)
     GradList* l = new (list) GradList;
     l->magic = 0;
     l->n = n;
