@@ -133,7 +133,7 @@ enum {
  *                    the tokens [seq_start[b], seq_start[b+1]).  Tokens
  *                    outside every sequence take no part.  (On the device,
  *                    so not checked; other values give unspecified results.)
- *   N, B             0 <= N < 2^34, 0 <= B < 2^31; N == 0 or B == 0 gives
+ *   N, B             0 <= N <= 2^34 - 2^11, 0 <= B < 2^31; N == 0 or B == 0 gives
  *                    zeros.
  *   reduction        SF_MEAN_TOKENS, SF_MEAN_SEQUENCES or SF_SUM_TOKENS.
  *   scale            finite factor of every weight.

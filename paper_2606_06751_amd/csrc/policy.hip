@@ -27,6 +27,9 @@ constexpr int kPolicyWG = 512;
 constexpr int kTok = 4;                 // consecutive tokens of a lane: 16-byte loads
 constexpr int kRoundTok = 64 * kTok;    // of a wave's round
 constexpr int kPolicyChunk = kPolicyWG / 64 * kRoundTok;  // of a workgroup: a round a wave
+// Tokens at most: a launch has fewer than 2^32 threads.
+constexpr int64_t kPolicyMax = ((((int64_t)1 << 32) / kPolicyWG) - 1) * kPolicyChunk;
+static_assert(kPolicyMax == ((int64_t)1 << 34) - (1 << 11), "as the header says");
 constexpr int kSliceMax = 2048;  // sequences that a workgroup keeps in LDS
 // Sequences of which every workgroup keeps all; with more, a chunk's are looked
 // up first (2e6 tokens of 1024: 14.0 us, all of them kept 15.9).
@@ -685,7 +688,7 @@ static inline PolicyLayout policy_layout(int64_t N, int64_t B)
 
 static inline bool policy_sizes_ok(int64_t N, int64_t B)
 {
-    return N >= 0 && N < ((int64_t)1 << 34) && B >= 0 && B < ((int64_t)1 << 31);
+    return N >= 0 && N <= kPolicyMax && B >= 0 && B < ((int64_t)1 << 31);
 }
 
 }  // namespace sfk
