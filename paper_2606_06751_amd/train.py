@@ -214,6 +214,12 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+def _order(t: torch.Tensor):
+    """What a dense tensor's dimensions order its entries by: None where that is
+    theirs, else the strides of those with more than one entry."""
+    return None if t.is_contiguous() else tuple(st if sz != 1 else 0 for st, sz in zip(t.stride(), t.shape))
+
+
 def _lay_out(tensors):
     """The C list of tensors (``sf_grad_list_init``)."""
     n = len(tensors)
@@ -256,7 +262,7 @@ class GradSet:
         self._list = _lay_out(self.tensors)
         # a list of no tensors launches nothing: one without entries has a clip's status set
         self._clip_list = self._list if self.tensors else _lay_out([torch.empty(0, dtype=torch.float32)])
-        self._order = [None if t.is_contiguous() else t.stride() for t in self.tensors]
+        self._order = [_order(t) for t in self.tensors]
         self.workspace_bytes = int(_lib.sf_grad_norm_workspace(self._list))
 
     def __len__(self):

@@ -1,4 +1,5 @@
-"""Sets of gradients: what their calls owe a rank that has none."""
+"""Sets of gradients: what their calls owe a rank that has none, and layouts
+that are alike."""
 import math
 
 import pytest
@@ -30,3 +31,15 @@ def test_status_without_gradients(tr, norms, wrong):
                         status=status)
         assert status.item() == (tr.SF_ERANGE if wrong else 0)
     tr.sf_grad_clip([], torch.tensor(norms, device=DEV), 1.0)
+
+
+def test_dimensions_of_one_entry_have_any_stride(tr):
+    """Layouts that differ in the stride of a dimension of size 1 alone are one."""
+    base = torch.randn(4, 6, device=DEV)
+    g = torch.as_strided(base, (6, 1, 4), (1, 77, 6))
+    o = torch.as_strided(torch.zeros(4, 6, device=DEV), (6, 1, 4), (1, 1, 6))
+    assert not g.is_contiguous() and g.stride() != o.stride()
+    tr.sf_grad_clip([g], torch.tensor([4.0], device=DEV), 1.0, eps=0.0, out=[o])
+    assert torch.equal(o, g * 0.25)
+    with pytest.raises(ValueError):
+        tr.sf_grad_clip([g], torch.tensor([4.0], device=DEV), 1.0, out=[torch.zeros(6, 1, 4, device=DEV)])
