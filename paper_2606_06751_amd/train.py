@@ -10,6 +10,7 @@ kernels.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import torch
 
@@ -214,6 +215,9 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+_data_ptr, _nbytes, _stride = torch.Tensor.data_ptr, operator.attrgetter("nbytes"), torch.Tensor.stride
+
+
 def _order(t: torch.Tensor):
     """What a dense tensor's dimensions order its entries by: None where that is
     theirs, else the strides of those with more than one entry."""
@@ -241,8 +245,10 @@ class GradSet:
     ``sf_grad_clip`` (``sf_grad_list_init``), checked once.
 
     Tensors are dense float32, bfloat16 or float16 ones on one GPU, mixed as
-    they come.  The set keeps them: it stands for these tensors, so a program
-    that gives its parameters new gradient tensors makes a new set of them.
+    they come.  The set stands for these tensors in the memory that they have
+    now: a program that gives its parameters new gradient tensors
+    (``zero_grad(set_to_none=True)``, torch's default) makes a new set of those,
+    and one whose tensors have other memory since is refused by the calls.
     """
 
     def __init__(self, tensors):
@@ -259,11 +265,26 @@ class GradSet:
                 raise ValueError("gradient %d is on %s, the others on %s" % (k, t.device, self.device))
             if not _dense(t):
                 raise ValueError("gradient %d must fill its memory without gaps" % k)
+        self._held = tuple(list(map(f, self.tensors)) for f in (_data_ptr, _nbytes, _stride))
         self._list = _lay_out(self.tensors)
         # a list of no tensors launches nothing: one without entries has a clip's status set
         self._clip_list = self._list if self.tensors else _lay_out([torch.empty(0, dtype=torch.float32)])
         self._order = [_order(t) for t in self.tensors]
         self.workspace_bytes = int(_lib.sf_grad_norm_workspace(self._list))
+
+    def check(self, order: bool = False):
+        """Raises where a tensor no longer has the memory that was laid out (its
+        ``data`` set, its storage resized), or, with ``order``, its layout.
+        (0.2 us a tensor: the kernels would read and write the former memory,
+        which may be another tensor's by now.)"""
+        for held, of in zip(self._held, (_data_ptr, _nbytes, _stride) if order else (_data_ptr, _nbytes)):
+            now = list(map(of, self.tensors))
+            if now != held:
+                if len(now) != len(held):
+                    raise ValueError("the set has %d tensors of the %d laid out" % (len(now), len(held)))
+                k = next(k for k in range(len(now)) if now[k] != held[k])
+                raise ValueError("gradient %d is not as it was laid out (%s %s, then %s): make a new set"
+                                 % (k, "stride" if of is _stride else "bytes" if of is _nbytes else "address", now[k], held[k]))
 
     def __len__(self):
         return len(self.tensors)
@@ -283,6 +304,8 @@ def sf_grad_norm(grads, out_norms: torch.Tensor | None = None, out_total: torch.
     """
     if not isinstance(grads, GradSet):
         grads = GradSet(grads)
+    else:
+        grads.check()
     n = len(grads)
     if n == 0 and out_total is None:
         raise ValueError("out_total is needed where there are no gradients")
@@ -312,10 +335,14 @@ def sf_grad_clip(grads, norms: torch.Tensor, max_norm: float, eps: float = 1e-6,
     """
     if not isinstance(grads, GradSet):
         grads = GradSet(grads)
+    else:
+        grads.check(order=out is not None and out is not grads)
     if out is None:
         out = grads
     elif not isinstance(out, GradSet):
         out = GradSet(out)
+    elif out is not grads:
+        out.check(order=True)
     if norms.dim() != 1:
         raise ValueError("norms must be [m]")
     if len(out) != len(grads):
