@@ -6,6 +6,12 @@ Every function has the name of the C entry point it wraps (declared in
 tensors on the GPU, outputs and workspaces that are not given are allocated on
 the call's stream, and every step of the computation runs in the library's HIP
 kernels.
+
+Autograd does not see through the calls: their outputs require no gradient, also
+where the inputs do, and a loss made of them passes none back.
+``sf_policy_loss`` and ``sf_token_logp_grad`` compute the gradients themselves;
+the program hands the last to autograd (``logits.backward(grad)``).  What a call
+writes into a caller's tensor counts there as an operation in place.
 """
 from __future__ import annotations
 
@@ -60,6 +66,14 @@ def _out(t, name: str, dtype, shape, like: torch.Tensor, stream):
     return t
 
 
+def _wrote(*outs):
+    """Tells autograd that the caller's tensors were written, as an operation of
+    torch's does: a backward pass that saved one of them refuses it."""
+    outs = [t for t in outs if t is not None]
+    if outs:
+        torch.autograd.graph.increment_version(outs)
+
+
 def _space(workspace, need: int, where: str, like: torch.Tensor, stream):
     """The call's workspace: the caller's uint8 tensor, or a new one."""
     if need < 0:
@@ -103,6 +117,7 @@ def sf_token_logp(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: 
     N, V = logits.shape
     dev = logits.device
     _check(targets, "targets", torch.int64, (N,), logits)
+    given = (out_logp, out_lse, out_entropy)
     if out_logp is None and out_lse is None and out_entropy is None and entropy:
         # one allocation for the three costs 2 us less than one each
         out_logp, out_lse, out_entropy = _new((3, N), torch.float32, dev, stream).unbind(0)
@@ -121,6 +136,7 @@ def sf_token_logp(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: 
                             None if need == 0 else workspace.data_ptr(), need, _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_token_logp")
+    _wrote(*given)
     return out_logp, out_lse, out_entropy
 
 
@@ -146,6 +162,7 @@ def sf_token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.T
             raise ValueError("entropy is needed with grad_entropy")
     if entropy is not None:
         _check(entropy, "entropy", torch.float32, (N,), logits)
+    given = out_grad
     if out_grad is None:
         out_grad = _new((N, V), logits.dtype, dev, stream)
     out_stride = _rows(out_grad, "out_grad")
@@ -158,6 +175,7 @@ def sf_token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.T
                                  out_stride, _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_token_logp_grad")
+    _wrote(given)
     return out_grad
 
 
@@ -188,6 +206,7 @@ def sf_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.
     if mask is not None:
         _check(mask, "mask", torch.bool if mask.dtype is torch.bool else torch.uint8, (N,), logp)
     dev = logp.device
+    given = (out_terms, out_grad)
     out_terms = _out(out_terms, "out_terms", f32, (4,), logp, stream)
     out_grad = _out(out_grad, "out_grad", f32, (N,), logp, stream)
     need = _lib.sf_policy_loss_workspace(N, B)
@@ -200,6 +219,7 @@ def sf_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.
                              None if need == 0 else workspace.data_ptr(), need, _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_policy_loss")
+    _wrote(*given)
     return out_terms, out_grad
 
 
@@ -277,7 +297,7 @@ class GradSet:
         ``data`` set, its storage resized), or, with ``order``, its layout.
         (0.2 us a tensor: the kernels would read and write the former memory,
         which may be another tensor's by now.)"""
-        for held, of in zip(self._held, (_data_ptr, _nbytes, _stride) if order else (_data_ptr, _nbytes)):
+        for of, held in zip((_data_ptr, _nbytes, _stride) if order else (_data_ptr, _nbytes), self._held):
             now = list(map(of, self.tensors))
             if now != held:
                 if len(now) != len(held):
@@ -311,6 +331,7 @@ def sf_grad_norm(grads, out_norms: torch.Tensor | None = None, out_total: torch.
         raise ValueError("out_total is needed where there are no gradients")
     like = grads.tensors[0] if n else out_total
     dev = like.device
+    given = (out_norms, out_total, out_nonfinite)
     out_norms = _out(out_norms, "out_norms", torch.float32, (n,), like, stream)
     out_total = _out(out_total, "out_total", torch.float32, (1,), like, stream)
     out_nonfinite = _out(out_nonfinite, "out_nonfinite", torch.int64, (n,), like, stream)
@@ -319,6 +340,7 @@ def sf_grad_norm(grads, out_norms: torch.Tensor | None = None, out_total: torch.
                            workspace.data_ptr(), workspace.numel(), _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_grad_norm")
+    _wrote(*given)
     return out_norms, out_total, out_nonfinite
 
 
@@ -360,4 +382,6 @@ def sf_grad_clip(grads, norms: torch.Tensor, max_norm: float, eps: float = 1e-6,
                            None if status is None else status.data_ptr(), _stream_handle(stream, like.device))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_grad_clip")
+    torch.autograd.graph.increment_version(out.tensors)
+    _wrote(status)
     return out
