@@ -8,7 +8,12 @@
  * and entropy, the gradient norm, entries that are not finite) are taken here
  * in the same manner: on the step's stream, without a host synchronisation
  * (which the accounting would show as exposed time of every rank) and in a
- * fixed order of summation, so equal inputs give equal bits on every rank.
+ * fixed order of summation.  Vectors are read from 128-byte boundaries, so that
+ * order depends on where logits and gradients begin: equal inputs with equal
+ * strides give equal bits on every rank where their addresses are equal modulo
+ * 128, and may differ in the rounding of 32-bit sums (of 64-bit sums: in the
+ * last rounding) elsewhere.  sf_token_logp_grad and sf_policy_loss do not depend
+ * on the address.
  *
  * Conventions are those of stagefrontier.h: device pointers, asynchronous on
  * the caller's stream, buffers and workspaces allocated by the caller, no
