@@ -27,9 +27,10 @@ namespace sfk {
 
 constexpr int kRowWG = 256;
 
-// Terms relative to (m, lo): s = sum 2^((x - m) c + lo), u = sum 2^t t with t
-// that exponent.  lo is the rounding of m c, so that t is one multiply-add of
-// x whose only error is its own rounding, and the largest term is 2^lo.
+// Terms relative to (b, R): s = sum 2^t, u = sum 2^t t with t = (x - b) c - R.
+// Either b is 0 and R a whole number near the largest x c, so that t is one
+// multiply-add of x whose only error is its own rounding, or, for huge logits, R
+// is 0 and b the largest x.
 struct RowState {
     float b, R, s, u;  // R = -inf: nothing but -inf so far
 };
@@ -301,7 +302,8 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_join(const typename Elem<
 // each of 4 short rows (16000 x 515 f16: 8.4 us, by workgroups 14).  Measured at
 // 16411 x 131072 bf16, vectors a lane / loads and stores past the caches or not:
 // 1 / both 1212, 2 / loads 1210, 2 / both 1298, 2 / none 1237, 4 / both 1362 us;
-// at 512 x 100003 41.5, 37.1, 37.8, 41.3, 39.1.
+// at 512 x 100003 41.5, 37.1, 37.8, 41.3, 39.1.  (8 waves a SIMD are asked for:
+// the code of far rows would take registers that leave 6.)
 constexpr int kGradU = 2;
 // From this |lse| on (2^16) its own rounding, up to 2^-24 of it and with that
 // an error of log p, passes that of a bfloat16, 2^-9 of p, and from 2^24 on
@@ -317,15 +319,30 @@ __device__ __forceinline__ float grad_term(float q, float h, float k0)
 
 // Such a row by LANES lanes, each of which reads the elements that it writes:
 // log p = (x - m) / T - log s with the row's maximum m, s = sum e^((x - m) / T).
+// The row is its `nv` vectors from `head` on and the elements around them.  (All
+// rows of 1024 x 65536 bf16 far: 120 us, none 44; two vectors a lane in flight
+// take more registers than leave 8 waves.)
 template <int DT, int LANES>
-__device__ __forceinline__ void far_row(const typename Elem<DT>::T* row, int V, float inv_t, int tid, float* part, int at,
-                                        float g, float h, float entropy, typename Elem<DT>::T* o)
+__device__ __forceinline__ void far_row(const typename Elem<DT>::T* row, int V, int head, int nv, float inv_t, int tid,
+                                        float* part, int at, float g, float h, float entropy, typename Elem<DT>::T* o)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int NW = LANES / 64;
-    float m = -INFINITY, s = 0.0f;
+    constexpr int E = kVec<DT>, NW = LANES / 64;
+    const VecU<DT>* xv = (const VecU<DT>*)(row + head);
+    VecU<DT>* ov = (VecU<DT>*)(o + head);
+    const int tail0 = head + nv * E;
+    const bool edge = tid < head + V - tail0;
+    const int je = edge ? (tid < head ? tid : tail0 + (tid - head)) : 0;
+    const float xe = edge ? (float)row[je] : -INFINITY;
+    auto vectors = [&](auto f) {
 #pragma unroll 1
-    for (int j = tid; j < V; j += LANES) m = fmaxf(m, (float)row[j]);
+        for (int v = tid; v < nv; v += LANES) f(xv[v], v);
+    };
+    float m = xe, s = 0.0f;
+    vectors([&](const VecU<DT>& x, int) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) m = fmaxf(m, (float)x[j]);
+    });
     m = wave_max_f32(m);
     if (NW > 1) {
         __syncthreads();  // a former row's sums are read
@@ -333,8 +350,12 @@ __device__ __forceinline__ void far_row(const typename Elem<DT>::T* row, int V, 
         __syncthreads();
         for (int w = 0; w < NW; ++w) m = fmaxf(m, part[w]);
     }
-#pragma unroll 1
-    for (int j = tid; j < V; j += LANES) s += exp2f(((float)row[j] - m) * inv_t * kLog2e);
+    auto add = [&](float x) { s += fast_exp2((x - m) * inv_t * kLog2e); };
+    vectors([&](const VecU<DT>& x, int) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) add((float)x[j]);
+    });
+    add(xe);
     s = wave_sum_f32(s);
     if (NW > 1) {
         if ((tid & 63) == 0) part[NW + (tid >> 6)] = s;
@@ -343,19 +364,24 @@ __device__ __forceinline__ void far_row(const typename Elem<DT>::T* row, int V, 
         for (int w = 0; w < NW; ++w) s += part[NW + w];
     }
     const float ls = logf(s), k0 = fmaf(h, entropy, g);
-#pragma unroll 1
-    for (int j = tid; j < V; j += LANES)
-        o[j] = (T)(grad_term(fmaf((float)row[j] - m, inv_t, -ls), h, k0) + (j == at ? g : 0.0f));
+    auto value = [&](float x, int j) { return (T)(grad_term(fmaf(x - m, inv_t, -ls), h, k0) + (j == at ? g : 0.0f)); };
+    vectors([&](const VecU<DT>& x, int v) {
+        VecU<DT> r;
+#pragma unroll
+        for (int j = 0; j < E; ++j) r[j] = value((float)x[j], head + v * E + j);
+        ov[v] = r;
+    });
+    if (edge) o[je] = value(xe, je);
 }
 
 template <int DT, int LANES>
-__global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<DT>::T* logits, int64_t N, int V,
-                                                            int64_t stride, const int64_t* __restrict__ targets,
-                                                            float inv_t, const float* __restrict__ lse,
-                                                            const float* __restrict__ grad_logp,
-                                                            const float* __restrict__ entropy,
-                                                            const float* __restrict__ grad_entropy,
-                                                            typename Elem<DT>::T* out, int64_t out_stride)
+__global__ __launch_bounds__(kRowWG, 8) void k_token_logp_grad(const typename Elem<DT>::T* logits, int64_t N, int V,
+                                                               int64_t stride, const int64_t* __restrict__ targets,
+                                                               float inv_t, const float* __restrict__ lse,
+                                                               const float* __restrict__ grad_logp,
+                                                               const float* __restrict__ entropy,
+                                                               const float* __restrict__ grad_entropy,
+                                                               typename Elem<DT>::T* out, int64_t out_stride)
 {
     typedef typename Elem<DT>::T T;
     constexpr int E = kVec<DT>;
@@ -383,9 +409,11 @@ __global__ __launch_bounds__(kRowWG) void k_token_logp_grad(const typename Elem<
             continue;
         }
         if (fabsf(l) >= kFarLse) {
-            // the whole row by the lanes of its first chunk, so that none reads what another wrote in place
-            if (blockIdx.x == 0)
-                far_row<DT, LANES>(row, V, inv_t, tid, part, (int)t, grad_logp[i] * inv_t,
+            // the whole row by the lanes of one chunk, so that none reads what another wrote in
+            // place; of another chunk row by row, as workgroups go to the XCDs in turn (the
+            // first of each: 599 us in place of 120)
+            if (blockIdx.x == (unsigned)i % gridDim.x)
+                far_row<DT, LANES>(row, V, head, nv, inv_t, tid, part, (int)t, grad_logp[i] * inv_t,
                                    grad_entropy ? grad_entropy[i] * inv_t : 0.0f, grad_entropy ? entropy[i] : 0.0f, o);
             continue;
         }
