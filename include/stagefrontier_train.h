@@ -12,8 +12,8 @@
  * order depends on where logits and gradients begin: equal inputs with equal
  * strides give equal bits on every rank where their addresses are equal modulo
  * 128, and may differ in the rounding of 32-bit sums (of 64-bit sums: in the
- * last rounding) elsewhere.  sf_token_logp_grad and sf_policy_loss do not depend
- * on the address.
+ * last rounding) elsewhere.  sf_policy_loss does not depend on the address, nor
+ * sf_token_logp_grad but in rows that it sums itself.
  *
  * Conventions are those of stagefrontier.h: device pointers, asynchronous on
  * the caller's stream, buffers and workspaces allocated by the caller, no
@@ -45,8 +45,9 @@ enum {
  *     lse  = log sum_j e^(z_j)
  *     logp = z_t - lse
  *     H    = - sum_j p_j log p_j,   p_j = e^(z_j - lse).
- * All arithmetic and sums are in 32 bits; the running maximum is subtracted
- * before each exponential.
+ * Arithmetic and sums are in 32 bits.  Exponents are taken relative to a
+ * reference that no term of a sum passes by more than a few powers of two, and
+ * that follows the row's maximum.
  *
  *   logits           [N][row_stride], the first V entries of each row used.
  *                    Aligned to the element size.
@@ -208,8 +209,11 @@ int64_t sf_grad_norm_workspace(const void* list);
 /*
  * sf_grad_clip -- scales the gradients of a list to a largest norm:
  *     norm = sqrt(sum_i norms[i]^2),  c = min(1, max_norm / (norm + eps))
- *     out = c * grad, rounded once to nearest even.
- * The norm stays on the device: the host need not wait for it.
+ *     out = c * grad.
+ * The norm and the quotient are in 64 bits, c is rounded to a float once.  The
+ * product is a float, rounded, and for SF_BF16 and SF_F16 rounded again to the
+ * type, each to nearest even.  The norm stays on the device: the host need not
+ * wait for it.
  *
  *   list        the gradients.
  *   out_list    where the scaled gradients go: the same list (in place) or
