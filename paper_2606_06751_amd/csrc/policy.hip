@@ -13,9 +13,11 @@
 // 4 consecutive tokens (16-byte loads) and a wave 256 a round, which are mostly
 // of one sequence: it is found once, in LDS, and followed; only in a round that
 // meets another does each lane look for its own (64 tokens a round: 31.7 us for
-// 2e6 tokens of 1024 sequences, 256: 14.4; the kernel alone).  The sums go to a
-// launch of their own: a counter of finished workgroups with the memory fences
-// that it needs cost 25 us more, since each fence writes back an L2.
+// 2e6 tokens of 1024 sequences, 256: 14.4; the kernel alone).  Terms are weighed
+// and summed in 64 bits and weights are 64-bit quotients, which costs 0.5 us there
+// (14.9).  The sums go to a launch of their own: a counter of finished workgroups
+// with the memory fences that it needs cost 25 us more, since each fence writes
+// back an L2.
 
 #include "sf_device.h"
 #include "sf_host.h"
@@ -659,7 +661,7 @@ __global__ __launch_bounds__(kJoinWG) void k_policy_join(int64_t chunks, float k
     if (threadIdx.x == 0) write_terms(sum, kl_coef, terms);
 }
 
-// One workgroup for all of it takes 10.8 us for 5003 tokens, where two or three
+// One workgroup for all of it takes 11.2 us for 5003 tokens, where two or three
 // launches take the host 6 to 10 us more than one.
 static inline bool small_policy(int64_t N, int64_t B) { return N <= kSmallN && B <= kSmallSeqs; }
 

@@ -14,10 +14,10 @@
 // relative to the wave's reference as it stands, and only where its sum shows
 // that a logit lies far above is the chunk done again with its maximum.  The
 // reference is a wave's, not a lane's, so that this is rare.  (Without the bound,
-// -inf logits sent every chunk the second way: 94 against 70 us at 3072 x 65536
-// bf16 with a hundredth of them masked; with it 69.6 us, without masks 69.5.)
+// -inf logits sent every chunk the second way: 144 against 94 us at 4096 x 65536
+// bf16 with a hundredth of them masked, 89 against 92 without masks.)
 // 4096 x 131072 bf16: 174 us, 6.2 TB/s, 87% of the 7.13 TB/s plain read; loads
-// that do not go past the caches gave 80 instead of 70 us at 3072 x 65536.
+// that do not go past the caches gave 103 instead of 92 us at 4096 x 65536.
 
 #include "sf_device.h"
 #include "sf_host.h"
@@ -55,8 +55,8 @@ __device__ __forceinline__ void row_rebase(RowState& a, float b, float R, float 
 }
 
 
-// Vectors of a chunk per lane (2 or 8: within 2% at 3072 x 65536; 2 is slower by
-// a third at 2048 x 32000, 8 spills with 1024 threads).
+// Vectors of a chunk per lane (2, 4, 8: 98, 92, 95 us at 4096 x 65536, 34, 28, 27
+// at 2048 x 32000; 8 spills with 1024 threads).
 constexpr int kRowU = 4;
 
 // Adds `live` vectors a lane and an edge logit (-inf: none) after taking their
@@ -456,7 +456,8 @@ struct RowShape {
 
 // Measured (bf16, us, a wave / 256 / 1024 threads a row / 256 threads in parts):
 //   300 x 1000: 3.4 / 4.0 / 6.4;  4096 x 16000: 27 / 30 / 64;  2048 x 32000:
-//   26.5 / 28.3 / 46;  8192 x 8000: 27.5 / 28.5;  8192 x 32003: 96 / 89;  3072 x 65536: 78 / 70 / 103;  1024 x 16000: 13.0 / 11.7 / 18;
+//   26.5 / 28.3 / 46;  8192 x 8000: 27.5 / 28.5;  8192 x 32003: 96 / 89;
+//   4096 x 65536: 100 / 94 / 137;  1024 x 16000: 13.0 / 11.7 / 18;
 //   512 x 16000: 11.5 / 7.8 / 9.5;  256 x 32000: 17.8 / 8.7 / 7.5;  128 x 65536:
 //   32 / 11.8 / 9.1 / 9.9;  64 x 131072: 59 / 19 / 12.5 / 9.9;  1 x 65536: 25 / 10 /
 //   7.8 / 5.2;  1 x 262144: 105 / 31 / 18 / 6.3.
