@@ -4,7 +4,8 @@ The library is a C ABI (``include/stagefrontier.h``) over hand-written HIP
 kernels; ``paper_2606_06751_amd.stagefrontier`` is its Python binding, and
 ``paper_2606_06751_amd.train`` that of the second header
 (``include/stagefrontier_train.h``: the numbers that a training step itself
-yields).  The bindings are imported on first attribute access so that ``import
+yields), ``paper_2606_06751_amd.draw`` of the third
+(``include/stagefrontier_draw.h``: what a policy step draws at random).  The bindings are imported on first attribute access so that ``import
 paper_2606_06751_amd`` alone loads nothing.
 """
 __version__ = "0.1.0"
@@ -19,6 +20,9 @@ _TRAIN_NAMES = ("sf_token_logp", "sf_token_logp_grad", "sf_token_logp_workspace"
                 "sf_policy_loss_workspace", "sf_grad_norm", "sf_grad_norm_workspace", "sf_grad_clip", "GradSet",
                 "SF_F32", "SF_BF16", "SF_F16", "SF_MEAN_TOKENS", "SF_MEAN_SEQUENCES", "SF_SUM_TOKENS")
 
+_DRAW_NAMES = ("sf_uniform", "sf_dropout", "sf_token_sample", "sf_token_sample_workspace", "sf_draft_verify",
+               "sf_draft_verify_workspace")
+
 
 def __getattr__(name):
     if name in _BINDING_NAMES:
@@ -27,4 +31,7 @@ def __getattr__(name):
     if name in _TRAIN_NAMES:
         from . import train
         return getattr(train, name)
+    if name in _DRAW_NAMES:
+        from . import draw
+        return getattr(draw, name)
     raise AttributeError(name)

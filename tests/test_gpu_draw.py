@@ -1,0 +1,644 @@
+"""The draws of stagefrontier_draw.h against their definitions (draw_ref.py), at
+the sizes, masks and layouts where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+import draw_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+KINDS = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+INF, NAN = math.inf, math.nan
+
+
+@pytest.fixture(scope="module")
+def dr():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_06751_amd import draw
+    return draw
+
+
+def key_of(seed, step):
+    return torch.tensor([seed, step], dtype=torch.int64, device=DEV)
+
+
+# -- uniform numbers -------------------------------------------------------
+
+@pytest.mark.parametrize("first,n", [(0, 1), (0, 4), (1, 1), (3, 2), (5, 1023), (2, 4096), (7, 0), ((1 << 34) - 3, 9),
+                                     ((1 << 60) - 5, 5), (123456789012, 2050)])
+def test_uniform(dr, first, n):
+    seed, step, site = -987654321012345678, (1 << 33) + 5, 4000000000
+    got = dr.sf_uniform(n, key_of(seed, step), site=site, first=first).cpu().numpy()
+    np.testing.assert_array_equal(got, ref.uniform(seed, step, site, first, n).astype(np.float32))
+
+
+def test_uniform_many(dr):
+    """More numbers than a launch has lanes; parts are the whole's."""
+    k, n = key_of(5, 1), 5000011
+    a = dr.sf_uniform(n, k)
+    assert a.min() >= 0 and a.max() < 1 and abs(a.double().mean().item() - 0.5) < 5 / math.sqrt(12 * n)
+    assert torch.equal(dr.sf_uniform(1001, k, first=n - 1001), a[-1001:])
+    np.testing.assert_array_equal(a[-9:].cpu().numpy(), ref.uniform(5, 1, 0, n - 9, 9).astype(np.float32))
+    for other in (dr.sf_uniform(n, key_of(6, 1)), dr.sf_uniform(n, key_of(5, 2)), dr.sf_uniform(n, k, site=1)):
+        # equal at chance's rate, n 2^-24 = 0.3
+        assert (a == other).sum() < 8 and abs(((a - 0.5) * (other - 0.5)).double().mean().item()) < 5 / (12 * math.sqrt(n))
+
+
+# -- dropout -----------------------------------------------------------------
+
+def rows(N, C, kind, seed, pad=0, shift=0):
+    """Entries as rows of a larger buffer that starts ``shift`` entries in."""
+    g = torch.Generator().manual_seed(seed)
+    buf = (torch.randn(N * (C + pad) + shift, generator=g) * 3.0).to(KINDS[kind])
+    return buf.to(DEV)[shift:].view(N, C + pad)[:, :C]
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def check_dropout(x, out, keep, p, residual, kind):
+    want, bound = ref.dropout(f64(x), keep, p, None if residual is None else f64(residual), kind)
+    off = np.abs(f64(out) - want)
+    assert (off <= bound).all(), "%d of %d off, worst %g" % ((off > bound).sum(), off.size, off.max())
+
+
+@pytest.mark.parametrize("kind,out_kind", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"),
+                                           ("f16", "f32"), ("f32", "f16"), ("f16", "bf16"), ("bf16", "f16")])
+@pytest.mark.parametrize("N,C,pad,shift,first,more,with_residual", [
+    (1, 1, 0, 0, 0, 0, True), (1, 7, 0, 1, 3, 0, False), (3, 5, 2, 3, 1, 4, True), (4, 8, 0, 0, 0, 0, False),
+    (5, 16, 0, 0, 8, 16, True), (2, 63, 1, 1, 0, 1, True), (7, 257, 0, 0, 0, 0, True), (33, 100, 3, 5, 77, 203, False),
+    (2, 2049, 0, 1, (1 << 35) + 1, 0, True), (300, 3, 0, 0, 0, 0, True), (1, 5000, 0, 3, (1 << 60) - 5000, 0, True)])
+def test_dropout(dr, kind, out_kind, N, C, pad, shift, first, more, with_residual):
+    seed, step, site, p = 1234567890123456789, 3, 11, 0.3
+    x = rows(N, C, kind, N + C, pad, shift)
+    r = rows(N, C, out_kind, N + C + 1, pad, 0) if with_residual else None
+    index = first + np.arange(N)[:, None] * (C + more) + np.arange(C)
+    keep = ref.kept(seed, step, site, p, index)
+    out = dr.sf_dropout(x, p, key_of(seed, step), site=site, first=first, index_stride=C + more, residual=r,
+                        out_dtype=KINDS[out_kind])
+    assert out.dtype is KINDS[out_kind]
+    check_dropout(x, out, keep, p, r, out_kind)
+
+
+@pytest.mark.parametrize("p", [0.0, 1e-6, 2.0 ** -16, 0.1, 0.5, 0.999, 1 - 2.0 ** -17, 1.0])
+def test_dropout_probabilities(dr, p):
+    """From nothing dropped to everything, the scale with the probability taken."""
+    x = rows(3, 1001, "f32", 4)
+    keep = ref.kept(8, 0, 0, p, np.arange(3003).reshape(3, 1001))
+    out = dr.sf_dropout(x, p, key_of(8, 0))
+    check_dropout(x, out, keep, p, None, "f32")
+    assert p not in (0.0, 1e-6) or torch.equal(out, x)
+    assert p < 1 - 2.0 ** -17 or not out.any()
+
+
+def test_dropout_values_that_are_not_finite(dr):
+    """A dropped entry counts as 0 whatever it holds; a kept one passes."""
+    x = torch.full((4, 999), NAN, device=DEV)
+    x[1], x[2] = INF, -INF
+    r = torch.ones(4, 999, device=DEV)
+    keep = torch.tensor(ref.kept(2, 2, 2, 0.5, np.arange(3996).reshape(4, 999)), device=DEV)
+    out = dr.sf_dropout(x, 0.5, key_of(2, 2), site=2, residual=r)
+    assert (out[~keep] == 1).all() and torch.isnan(out[0][keep[0]]).all()
+    assert (out[1][keep[1]] == INF).all() and (out[2][keep[2]] == -INF).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_dropout_in_place_and_around(dr, kind):
+    """Onto x, onto the residual; what lies between and around rows stays."""
+    k = key_of(3, 4)
+    buf, rbuf = rows(6, 120, kind, 1), rows(6, 120, kind, 2)
+    x, r = buf[1:5, 8:108], rbuf[1:5, 8:108]
+    want = dr.sf_dropout(x, 0.2, k, residual=r)
+    a, b = buf.clone(), rbuf.clone()
+    assert dr.sf_dropout(a[1:5, 8:108], 0.2, k, residual=r, out=a[1:5, 8:108]).data_ptr() == a[1:5, 8:108].data_ptr()
+    dr.sf_dropout(x, 0.2, k, residual=b[1:5, 8:108], out=b[1:5, 8:108])
+    for got, was in ((a, buf), (b, rbuf)):
+        assert torch.equal(got[1:5, 8:108], want)
+        got[1:5, 8:108] = was[1:5, 8:108]
+        assert torch.equal(got, was)
+    # the very same tensor as both
+    both = dr.sf_dropout(x, 0.2, k, residual=x)
+    check_dropout(x, both, ref.kept(3, 4, 0, 0.2, np.arange(400).reshape(4, 100)), 0.2, x, kind)
+
+
+def test_dropout_parts_are_the_whole(dr):
+    """Rows and columns that ranks hold draw their part of one mask."""
+    k, x = key_of(77, 5), rows(50, 300, "bf16", 9)
+    whole = dr.sf_dropout(x, 0.4, k, site=6)
+    for c0, c1 in ((0, 100), (100, 207), (207, 300)):
+        for r0, r1 in ((0, 13), (13, 50)):
+            part = dr.sf_dropout(x[r0:r1, c0:c1], 0.4, k, site=6, first=r0 * 300 + c0, index_stride=300)
+            assert torch.equal(part, whole[r0:r1, c0:c1])
+
+
+def test_dropout_gradient(dr):
+    """The same call on the output's gradient is the derivative: against
+    differences of a loss in 64 bits, and added to another gradient."""
+    k, p = key_of(21, 0), 0.25
+    x, r = rows(5, 77, "f32", 3), rows(5, 77, "f32", 4)
+    g = rows(5, 77, "f32", 5)
+    gx = dr.sf_dropout(g, p, k, site=1)
+    keep = ref.kept(21, 0, 1, p, np.arange(385).reshape(5, 77))
+    # the loss is linear: its difference quotient over a step of 1 is exact but for the outputs' roundings
+    base = f64(dr.sf_dropout(x, p, k, site=1, residual=r))
+    for i, j in ((0, 0), (1, 8), (2, 76), (4, 33), (3, 5)):
+        moved = x.clone()
+        moved[i, j] += 1.0
+        step = f64(moved)[i, j] - f64(x)[i, j]
+        diff = (f64(dr.sf_dropout(moved, p, k, site=1, residual=r)) - base) * f64(g)
+        # two outputs within 2 u of their size (below 40) each
+        assert abs(diff.sum() / step - f64(gx)[i, j]) <= 8 * ref.U * 40 * abs(f64(g)[i, j])
+    check_dropout(g, gx, keep, p, None, "f32")
+    check_dropout(g, dr.sf_dropout(g, p, k, site=1, residual=r), keep, p, r, "f32")
+    # a bfloat16 gradient of a float32 residual
+    check_dropout(g, dr.sf_dropout(g, p, k, site=1, out_dtype=torch.bfloat16), keep, p, None, "bf16")
+
+
+@pytest.mark.parametrize("N,C", [(70000, 3), (3, 3000001), (131073, 9)])
+def test_dropout_more_than_a_launch(dr, N, C):
+    """More rows than a grid holds, rows of many turns: the mask's share, ends of
+    rows and equal parts."""
+    x = torch.ones(N, C + 1, device=DEV)[:, :C]
+    out = dr.sf_dropout(x, 0.125, key_of(1, 1), residual=None)
+    share = (out == 0).double().mean().item()
+    assert abs(share - 0.125) < 5 * math.sqrt(0.11 / (N * C)) and ((out == 0) | (out == 8 / 7)).all()
+    lo = max(0, N - 4)
+    keep = ref.kept(1, 1, 0, 0.125, (np.arange(lo, N)[:, None] * C + np.arange(max(0, C - 40), C)))
+    np.testing.assert_array_equal((out[lo:, max(0, C - 40):] != 0).cpu().numpy(), keep)
+    assert torch.equal(dr.sf_dropout(x.contiguous(), 0.125, key_of(1, 1)), out)
+
+
+# -- sampling ----------------------------------------------------------------
+
+def check_sample(dr, logits, u, inv_t, **kw):
+    token, logp = dr.sf_token_sample(logits, u, inv_temperature=inv_t, **kw)
+    x, us, t, lp = f64(logits), u.cpu().numpy(), token.cpu().numpy(), logp.cpu().numpy()
+    for i in range(len(us)):
+        want, near, value = ref.sample(x[i], float(us[i]), inv_t)
+        assert t[i] in near, "row %d: token %d for %d" % (i, t[i], want)
+        v = value(t[i])
+        if math.isfinite(v):
+            assert abs(lp[i] - v) <= ref.logp_bound(v), "row %d: %r for %r" % (i, lp[i], v)
+        else:
+            np.testing.assert_equal(float(lp[i]), v)
+    return token, logp
+
+
+def uniforms(N, seed):
+    return torch.rand(N, generator=torch.Generator().manual_seed(seed)).to(DEV)
+
+
+SHAPES = [(1, 1, 0, 0), (1, 2, 0, 1), (3, 5, 0, 3), (2, 8, 0, 0), (5, 9, 2, 7), (7, 63, 0, 1), (4, 64, 3, 0), (9, 257, 0, 5),
+          (3, 1023, 1, 0), (4, 1024, 0, 0), (4, 1025, 0, 1), (6, 2048, 0, 0), (6, 2049, 0, 3), (2, 4096, 0, 0), (5, 8191, 0, 1),
+          (1, 16385, 0, 3), (3, 40001, 0, 1), (1, 131072, 0, 0), (2, 200003, 5, 1), (1100, 515, 0, 1), (600, 4100, 6, 2),
+          (520, 9001, 0, 1), (4100, 2305, 0, 1)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,V,pad,shift", SHAPES)
+def test_sample(dr, kind, N, V, pad, shift):
+    check_sample(dr, rows(N, V, kind, 7 * N + V, pad, shift), uniforms(N, V), 1.0 / 0.7)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("copies", [1, 60, 400])
+def test_sample_masked_and_extreme_logits(dr, kind, copies):
+    low = torch.finfo(KINDS[kind]).min
+    V = 9000
+    x = torch.randn(13, V, generator=torch.Generator().manual_seed(1)).to(KINDS[kind])
+    x[1] = -INF                        # nothing left
+    x[2] = -INF
+    x[2, 4321] = 2.0                   # one left
+    x[3, ::2] = -INF
+    x[4] = low                         # all at the type's lowest value: uniform
+    x[5, 1:] = low
+    x[6, 100] = INF
+    x[7, 8999] = NAN
+    x[8] = -60000.0                    # masked by a large number throughout
+    x[9] = 0.0
+    x[9, 7] = 1000.0                   # one certain
+    x[10] = -INF
+    x[10, 8000:] = 1.0                 # whole parts of the row masked
+    x[11] = -INF
+    x[11, 5] = NAN                     # nothing else left
+    x[12] = -INF
+    x[12, 8999] = low
+    u = torch.tensor([0.3, 0.5, 0.999, 0.0, 0.7, 0.99, 0.5, 0.5, 0.25, 0.9, 0.0, 0.5, 0.999]).repeat(copies)
+    u[0] = 1.0 - 2.0 ** -24
+    logits = x.repeat(copies, 1).to(DEV)
+    if copies == 1:
+        token, logp = check_sample(dr, logits, u.to(DEV), 1.0)
+        assert token[[1, 6, 7, 11]].tolist() == [-1] * 4 and token[[2, 5, 9, 10, 12]].tolist() == [4321, 0, 7, 8000, 8999]
+        assert logp[1] == -INF and torch.isnan(logp[[6, 7, 11]]).all()
+    else:
+        # whole rows, parts of rows: the same tokens in every copy
+        u[0] = 0.3
+        token, logp = dr.sf_token_sample(logits, u.to(DEV))
+        check_sample(dr, logits[-13:].contiguous(), u[-13:].to(DEV), 1.0)
+        one = dr.sf_token_sample(logits[:13], u[:13].to(DEV))
+        assert torch.equal(token.view(copies, 13), one[0].expand(copies, 13))
+        assert torch.equal(logp.view(copies, 13).nan_to_num(7.0), one[1].nan_to_num(7.0).expand(copies, 13))
+
+
+@pytest.mark.parametrize("inv_t", [2.0 ** -149, 1e-20, 1e-3, 37.0, 1e4, 1e6, 1e12, 2.0 ** 100])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 1e30])
+def test_sample_far_temperatures(dr, kind, inv_t, scale):
+    """From a flat to a certain distribution, masked entries among them."""
+    x = rows(6, 3001, kind, 21, 1, 1) * scale
+    x[:, ::3] = -INF
+    check_sample(dr, x, torch.tensor([0.0, 0.1, 0.5, 0.9, 1 - 2.0 ** -24, 0.3], device=DEV), inv_t)
+
+
+def test_sample_greedy(dr):
+    """The first of the largest logits at a temperature near 0 and u = 0."""
+    x = rows(40, 5003, "bf16", 5)
+    token, logp = dr.sf_token_sample(x, torch.zeros(40, device=DEV), inv_temperature=2.0 ** 100)
+    top = x.float().max(1, keepdim=True).values
+    assert torch.equal(token, (x.float() == top).int().argmax(1))
+    want = -torch.log((x.float() == top).sum(1).double())
+    assert (logp.double() - want).abs().max() <= 2 * ref.U * 8
+
+
+@pytest.mark.parametrize("N,V", [(50, 700), (50, 20000), (700, 20000), (5000, 700)])
+def test_sample_rows_that_take_no_part(dr, N, V):
+    """They are not read: they hold NaN here; the others are unmoved."""
+    x, u = rows(N, V, "bf16", 3), uniforms(N, 4)
+    want = dr.sf_token_sample(x, u)
+    off = torch.rand(N, generator=torch.Generator().manual_seed(5)) < 0.4
+    bad = torch.tensor([-1.0, 1.0, NAN, INF, -INF, 2.0, -1e-30])
+    x, u = x.clone(), u.clone()
+    x[off] = NAN
+    u[off] = bad[torch.arange(int(off.sum())) % len(bad)].to(DEV)
+    token, logp = dr.sf_token_sample(x, u)
+    off = off.to(DEV)
+    assert (token[off] == -1).all() and (logp[off] == 0).all()
+    assert torch.equal(token[~off], want[0][~off]) and torch.equal(logp[~off], want[1][~off])
+
+
+def test_sample_does_not_depend_on_split_or_address(dr):
+    """The same row, alone and among many, at any alignment: the same bits."""
+    V = 30011
+    one = rows(1, V, "bf16", 6)
+    u = torch.rand(200, generator=torch.Generator().manual_seed(8)).to(DEV)
+    many = dr.sf_token_sample(one.expand(200, V).contiguous(), u)
+    for N in (1, 3, 40):
+        got = dr.sf_token_sample(one.expand(N, V).contiguous(), u[:N].contiguous())
+        assert torch.equal(got[0], many[0][:N]) and torch.equal(got[1], many[1][:N])
+    lots = dr.sf_token_sample(one.expand(5000, V).contiguous(), u.repeat(25))
+    assert torch.equal(lots[0].view(25, 200), many[0].expand(25, 200))
+    assert torch.equal(lots[1].view(25, 200), many[1].expand(25, 200))
+    buf = torch.zeros(V + 64, dtype=torch.bfloat16, device=DEV)
+    for shift in (1, 3, 8, 33):
+        buf[shift:shift + V] = one[0]
+        got = dr.sf_token_sample(buf[shift:shift + V].view(1, V), u[7:8].contiguous())
+        assert got[0] == many[0][7] and got[1] == many[1][7]
+
+
+def test_sample_frequencies(dr):
+    """Tokens come with their probabilities (5 standard deviations of each)."""
+    N, p = 400000, torch.tensor([0.5, 0.25, 0.0, 0.125, 0.1, 0.02, 0.005])
+    x = p.log().to(DEV).expand(N, 7).contiguous()
+    token, _ = dr.sf_token_sample(x, dr.sf_uniform(N, key_of(99, 1)))
+    got = torch.bincount(token, minlength=7).double().cpu() / N
+    assert ((got - p.double()).abs() <= 5 * (p * (1 - p) / N).sqrt() + 1e-9).all()
+
+
+# -- verification --------------------------------------------------------------
+
+def batch(counts, V, kind, seed, noise=0.7, pad=0, shift=0, lookup=False, masked=0.0):
+    """Target rows, drafts' rows and drafts drawn from them on the CPU."""
+    g = torch.Generator().manual_seed(seed)
+    D, B = int(sum(counts)), len(counts)
+    start = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int64)
+    target = rows(D + B, V, kind, seed + 1, pad, shift)
+    if masked:
+        target[(torch.rand(D + B, V, generator=g) < masked).to(DEV)] = -INF
+    at = torch.arange(D) + torch.repeat_interleave(torch.arange(B), torch.tensor(list(counts), dtype=torch.int64))
+    q = rows(max(D, 1), V, kind, seed + 2, pad, shift)[:D]
+    q.copy_(target[at.to(DEV)].float() + noise * q.float() / 3.0)
+    e = -torch.log(torch.rand(D, V, generator=g).clamp(min=1e-30))
+    draft = (q.float().cpu() - e.log()).argmax(1) if D else torch.zeros(0, dtype=torch.int64)
+    u = torch.rand(D + B, generator=g)
+    return target, None if lookup else q, draft.to(DEV), start.to(DEV), u.to(DEV)
+
+
+def check_verify(dr, target, q, draft, start, u, inv_t=1.0, iq=1.0, **kw):
+    accepted, token, logp = dr.sf_draft_verify(target, q, draft, start, u, inv_temperature=inv_t, draft_inv_temperature=iq, **kw)
+    x, xq = f64(target), None if q is None else f64(q)
+    s, d, us = start.tolist(), draft.tolist(), [float(v) for v in u.cpu().numpy()]
+    acc, tok, lp = accepted.tolist(), token.tolist(), [float(v) for v in logp.cpu().numpy()]
+    close = 0
+    for b in range(len(s) - 1):
+        i, n = s[b] + b, s[b + 1] - s[b]
+        want = ref.verify(x[i:i + n + 1], None if xq is None else xq[s[b]:s[b + 1]], d[s[b]:s[b + 1]], us[i:i + n + 1], inv_t, iq)
+        if want is None:
+            close += 1
+            continue
+        k, near, value, logps = want
+        assert acc[b] == k, "sequence %d: %d accepted for %d" % (b, acc[b], k)
+        assert tok[i:i + k] == d[s[b]:s[b] + k] and tok[i + k] in near, "sequence %d" % b
+        assert tok[i + k + 1:i + n + 1] == [-1] * (n - k) and lp[i + k + 1:i + n + 1] == [0.0] * (n - k)
+        for got, v in zip(lp[i:i + k + 1], logps + [value(tok[i + k])]):
+            if math.isfinite(v):
+                assert abs(got - v) <= ref.logp_bound(v)
+            else:
+                np.testing.assert_equal(got, v)
+    assert close <= 1 + len(acc) // 10
+    return accepted, token, logp
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lookup", [False, True])
+@pytest.mark.parametrize("counts,V,pad,shift", [
+    ([1], 1, 0, 0), ([0], 5, 0, 0), ([3], 2, 0, 1), ([2, 0, 4], 9, 1, 3), ([5], 300, 0, 0), ([0, 9, 1, 3, 4], 1025, 0, 1),
+    ([4] * 9, 2048, 0, 0), ([7, 0, 3], 4099, 2, 5), ([5], 40001, 0, 1), ([1, 2], 131072, 0, 0), ([3] * 40 + [0] * 20, 515, 3, 0),
+    ([2, 3, 1] * 200, 130, 0, 1), ([17, 33, 0, 5], 600, 0, 0)])
+def test_verify(dr, kind, lookup, counts, V, pad, shift):
+    target, q, draft, start, u = batch(counts, V, kind, 11 * len(counts) + V, pad=pad, shift=shift, lookup=lookup)
+    check_verify(dr, target, q, draft, start, u, float(np.float32(1 / 0.8)), float(np.float32(1 / 1.1)))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_verify_all_of_one_kind(dr, kind):
+    """Drafts from the target itself are all accepted; ones that the target
+    forbids none; all but the last entry of the target's mass taken."""
+    counts, V = [3, 0, 5, 1], 2500
+    target, q, draft, start, u = batch(counts, V, kind, 3, noise=0.0)
+    accepted, _, _ = check_verify(dr, target, q, draft, start, u)
+    assert accepted.tolist() == counts
+    rowsof = (torch.arange(9) + torch.tensor([0, 0, 0, 2, 2, 2, 2, 2, 3])).to(DEV)
+    target[rowsof, draft] = -INF
+    accepted, token, _ = check_verify(dr, target, q, draft, start, u)
+    assert accepted.tolist() == [0, 0, 0, 0] and (token[[0, 4, 5, 11]] >= 0).all()
+    # drafts of probability 0 in their own distribution
+    target, q, draft, start, u = batch(counts, V, kind, 4)
+    q[torch.arange(9, device=DEV), draft] = -INF
+    assert check_verify(dr, target, q, draft, start, u)[0].tolist() == counts
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B", [14, 1400])
+def test_verify_rows_without_an_answer(dr, kind, B):
+    """Masked, infinite and undefined logits, uniform numbers outside, drafts
+    that are none: at the first row, at a later one, at the last."""
+    counts, V = [3] * 14, 3001
+    target, q, draft, start, u = batch(counts, V, kind, 8, noise=0.0)
+    t = lambda b, k: 4 * b + k  # noqa: E731
+    for b, (what, k) in enumerate([(w, k) for w in ("empty", "nan", "inf", "out") for k in (0, 1, 3)]):
+        i = t(b, k)
+        if what == "empty":
+            target[i] = -INF
+        elif what == "nan":
+            target[i, 3000] = NAN
+        elif what == "inf":
+            target[i, 17] = INF
+        else:
+            u[i] = [-1.0, 1.0, NAN][k % 3]
+    draft[3 * 12 + 1] = -1
+    draft[3 * 13] = V
+    q[3 * 13 + 1] = NAN                # behind where the sequence ends: not looked at
+    u[t(13, 2)] = 5.0
+    if B > 14:
+        n = B // 14
+        many = (target.repeat(n, 1), q.repeat(n, 1), draft.repeat(n), torch.arange(B + 1, device=DEV) * 3, u.repeat(n))
+        one = dr.sf_draft_verify(target, q, draft, start, u)
+        for a, b in zip(one, dr.sf_draft_verify(*many)):
+            assert torch.equal(b.nan_to_num(5.0).view(n, -1), a.nan_to_num(5.0).expand(n, -1))
+        return
+    accepted, token, logp = check_verify(dr, target, q, draft, start, u)
+    assert accepted.tolist() == [0, 1, 3] * 4 + [1, 0]
+    check_verify(dr, target, None, draft, start, u)
+    # the draft's own rows: nothing left counts as 0, NaN and infinity end a sequence
+    q[0], q[3, 5], q[6, 7], q[9] = -INF, NAN, INF, -INF
+    target[:16] = rows(16, V, kind, 1)
+    u[:16] = 0.5
+    draft[9] = 5
+    target[t(3, 0), 5] = -INF
+    accepted, token, logp = check_verify(dr, target, q, draft, start, u)
+    assert accepted[0] >= 1 and accepted[1:4].tolist() == [0, 0, 0]
+    assert token[[4, 8]].tolist() == [-1, -1] and torch.isnan(logp[[4, 8]]).all() and token[12] >= 0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("inv_t,iq", [(1e-20, 1.0), (1.0, 1e-20), (1e3, 1e3), (2.0 ** 100, 1.0), (2.0 ** 100, 2.0 ** 100)])
+def test_verify_far_temperatures(dr, kind, inv_t, iq):
+    target, q, draft, start, u = batch([2, 4, 0, 1, 3, 3], 1501, kind, 5, masked=0.3)
+    check_verify(dr, target, q, draft, start, u, inv_t, iq)
+
+
+def test_verify_leaves_rows_of_no_sequence(dr):
+    """Rows before the first and behind the last sequence are neither judged nor
+    written."""
+    target, q, draft, _, u = batch([8, 0, 0], 700, "bf16", 2)
+    start = torch.tensor([2, 4, 4, 6], device=DEV)
+    acc, tok, lp = torch.full((3,), 77, device=DEV), torch.full((11,), 77, device=DEV), torch.full((11,), 77.0, device=DEV)
+    dr.sf_draft_verify(target, q, draft, start, u, out_accepted=acc, out_token=tok, out_logp=lp)
+    # their rows of the target are 2..4, 5 and 6..8
+    assert (tok[[0, 1, 9, 10]] == 77).all() and (lp[[0, 1, 9, 10]] == 77).all() and (tok[2:9] != 77).all()
+    got = dr.sf_draft_verify(target[2:9], q[2:6], draft[2:6].contiguous(), start - 2, u[2:9].contiguous())
+    assert torch.equal(got[0], acc) and torch.equal(got[1], tok[2:9]) and torch.equal(got[2], lp[2:9])
+
+
+def test_verify_starts_outside_stay_inside(dr):
+    """Starts that the contract rules out: results are unspecified, but nothing
+    outside the arrays is touched."""
+    target, q, draft, _, u = batch([6, 0], 300, "f32", 2)
+    guard = torch.full((64,), 7, dtype=torch.int64, device=DEV)
+    for bad in ([-5, 3, 6], [0, 900, 6], [0, 1 << 62, -(1 << 62)], [6, 0, 6], [3, 3, 3]):
+        tok = guard.clone()
+        dr.sf_draft_verify(target, q, draft, torch.tensor(bad, device=DEV), u, out_token=tok[16:24])
+        assert (tok[:16] == 7).all() and (tok[24:] == 7).all()
+
+
+@pytest.mark.parametrize("lookup", [False, True])
+def test_verified_frequencies(dr, lookup):
+    """Two tokens verified are distributed as the target's (5 standard
+    deviations of each pair)."""
+    B, V = 200000, 5
+    p = torch.tensor([[0.4, 0.3, 0.2, 0.1, 0.0], [0.05, 0.05, 0.2, 0.3, 0.4]])
+    q = torch.tensor([0.1, 0.5, 0.1, 0.2, 0.1])
+    key = key_of(4, 2)
+    x = torch.stack([p[0], p[1]]).log().to(DEV).repeat(B, 1)
+    xq = q.log().to(DEV).expand(B, V).contiguous()
+    if lookup:
+        draft = torch.full((B,), 1, device=DEV)
+    else:
+        draft, _ = dr.sf_token_sample(xq, dr.sf_uniform(B, key, site=1))
+    start = torch.arange(B + 1, device=DEV)
+    acc, token, _ = dr.sf_draft_verify(x, None if lookup else xq, draft, start, dr.sf_uniform(2 * B, key, site=2))
+    first, second = token[0::2], token[1::2]
+    got = torch.bincount(first, minlength=V).double().cpu() / B
+    assert ((got - p[0].double()).abs() <= 5 * (p[0] * (1 - p[0]) / B).sqrt() + 1e-9).all()
+    went = acc == 1
+    share = 0.3 if lookup else torch.minimum(p[0], q).sum().item()
+    assert abs(went.double().mean().item() - share) < 5 * math.sqrt(share * (1 - share) / B)
+    got = torch.bincount(second[went], minlength=V).double().cpu() / int(went.sum())
+    assert ((got - p[1].double()).abs() <= 5 * (p[1] * (1 - p[1]) / int(went.sum())).sqrt() + 1e-9).all()
+    assert (second[~went] == -1).all()
+
+
+def test_verify_without_drafts_is_sampling(dr):
+    x, u = rows(30, 9001, "bf16", 4), uniforms(30, 5)
+    none = torch.zeros(0, dtype=torch.int64, device=DEV)
+    for q in (None, x[:0]):
+        acc, token, logp = dr.sf_draft_verify(x, q, none, torch.zeros(31, dtype=torch.int64, device=DEV), u, inv_temperature=0.7)
+        want = dr.sf_token_sample(x, u, inv_temperature=0.7)
+        assert not acc.any() and torch.equal(token, want[0]) and torch.equal(logp, want[1])
+
+
+def test_large_offsets(dr):
+    """Rows that begin beyond 2^31 entries of their buffer."""
+    V, N, stride = 1031, 5, 600000000
+    buf = torch.empty(stride * (N - 1) + V, dtype=torch.bfloat16, device=DEV)
+    x = buf.as_strided((N, V), (stride, 1))
+    x.copy_(rows(N, V, "bf16", 3))
+    check_sample(dr, x, uniforms(N, 1), 1.0)
+    start = torch.tensor([0, 2, 3], device=DEV)
+    q = rows(3, V, "bf16", 5)
+    check_verify(dr, x, q, q.float().argmax(1), start, uniforms(N, 2))
+    keep = ref.kept(1, 1, 0, 0.5, np.arange(N * V).reshape(N, V))
+    y = buf.as_strided((N, V), (stride, 1), 0)
+    want = dr.sf_dropout(x.contiguous(), 0.5, key_of(1, 1))
+    assert torch.equal(dr.sf_dropout(x, 0.5, key_of(1, 1), out=y), want)
+    assert torch.equal(want != 0, torch.tensor(keep, device=DEV) & (want != 0))
+
+
+# -- as they are used -----------------------------------------------------------
+
+def rollout(dr, tr, hidden, weight, small, key, state):
+    """One verification of a policy's drafts from its dropped-out features, and
+    the loss's numbers of what came of it."""
+    B, K = state["B"], state["K"]
+    h = dr.sf_dropout(hidden, 0.1, key, site=1)
+    target = h @ weight
+    q = (h @ small).view(B, K + 1, -1)[:, :K].reshape(B * K, -1)
+    draft, _ = dr.sf_token_sample(q, dr.sf_uniform(B * K, key, site=2))
+    acc, token, logp = dr.sf_draft_verify(target, q, draft, state["start"], dr.sf_uniform(B * (K + 1), key, site=3))
+    again, _, _ = tr.sf_token_logp(target, token, entropy=False)
+    return h, acc, token, logp, again
+
+
+def setup_rollout():
+    B, K, W, V = 6, 3, 40, 1201
+    hidden, weight = rows(B * (K + 1), W, "f32", 1), rows(W, V, "f32", 2) * 0.1
+    small = weight + rows(W, V, "f32", 3) * 0.03
+    return hidden, weight, small, dict(B=B, K=K, start=torch.arange(B + 1, device=DEV) * K)
+
+
+def test_together(dr):
+    from paper_2606_06751_amd import train as tr
+    hidden, weight, small, state = setup_rollout()
+    h, acc, token, logp, again = rollout(dr, tr, hidden, weight, small, key_of(1, 0), state)
+    target = h @ weight
+    on = token >= 0
+    assert torch.equal(on.view(6, 4).sum(1) - 1, acc)
+    # the log-probabilities that the draws had are those of the token operator, whose sums are in 32 bits
+    assert (logp - again).abs().max() <= 1e-5 and not logp[~on].any() and not again[~on].any()
+    q = (h @ small).view(6, 4, -1)[:, :3].reshape(18, -1)
+    draft, _ = dr.sf_token_sample(q, dr.sf_uniform(18, key_of(1, 0), site=2))
+    check_verify(dr, target, q, draft, state["start"], dr.sf_uniform(24, key_of(1, 0), site=3))
+
+
+def test_together_in_a_graph(dr):
+    """Captured once, replayed with another step each time, with eager work of
+    the program's between: every replay gives what the eager calls give."""
+    from paper_2606_06751_amd import train as tr
+    hidden, weight, small, state = setup_rollout()
+    key = key_of(31, 0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        rollout(dr, tr, hidden, weight, small, key, state)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        key[1] += 1
+        got = rollout(dr, tr, hidden, weight, small, key, state)
+    seen = []
+    for step in range(1, 6):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert key.tolist() == [31, step]
+        want = rollout(dr, tr, hidden, weight, small, key_of(31, step), state)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        seen.append(got[0].clone())
+        torch.rand(1000, device=DEV).sum().item()
+    assert not torch.equal(seen[0], seen[1])
+
+
+def test_other_streams(dr):
+    """Calls on a stream that is not the current one, two at once with a
+    workspace each."""
+    x, u = rows(3, 200003, "bf16", 1), uniforms(3, 2)
+    target, q, draft, start, uv = batch([4, 2], 30011, "bf16", 7)
+    want, wantv = dr.sf_token_sample(x, u), dr.sf_draft_verify(target, q, draft, start, uv)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = dr.sf_token_sample(x, u, stream=a)
+        gotv = dr.sf_draft_verify(target, q, draft, start, uv, stream=b.cuda_stream)
+        got2 = dr.sf_token_sample(x, u, stream=b)
+        torch.cuda.synchronize()
+        for g, w in list(zip(got, want)) + list(zip(gotv, wantv)) + list(zip(got2, want)):
+            assert torch.equal(g, w)
+
+
+def test_writes_count_as_writes(dr):
+    """What a call writes into a caller's tensor, autograd knows of."""
+    key = key_of(1, 1)
+    x, u = rows(4, 301, "f32", 1), torch.zeros(4, device=DEV)
+    outs = [torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(4, device=DEV), torch.zeros(4, 301, device=DEV),
+            torch.zeros(2, dtype=torch.int64, device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(4, device=DEV)]
+    dr.sf_uniform(4, key, out=u)
+    dr.sf_token_sample(x, u, out_token=outs[0], out_logp=outs[1])
+    dr.sf_dropout(x, 0.1, key, out=outs[2])
+    dr.sf_draft_verify(x, x[:2], outs[0][:2], torch.tensor([0, 1, 2], device=DEV), u, out_accepted=outs[3], out_token=outs[4],
+                       out_logp=outs[5])
+    for v in [u] + outs:
+        assert v._version == 1
+    assert x._version == key._version == 0
+    w = torch.ones(4, 301, device=DEV, requires_grad=True)
+    y = (x * w).relu()  # saves its result
+    dr.sf_dropout(y.detach(), 0.5, key, out=y.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    assert not dr.sf_dropout(w, 0.5, key).requires_grad
+
+
+def test_binding_refusals(dr):
+    from paper_2606_06751_amd import StageFrontierError
+    key, x, u = key_of(1, 1), rows(4, 300, "f32", 1), torch.zeros(4, device=DEV)
+    d, s = torch.zeros(2, dtype=torch.int64, device=DEV), torch.tensor([0, 1, 2], device=DEV)
+    for bad, error in (
+            (lambda: dr.sf_uniform(-1, key), Exception), (lambda: dr.sf_uniform(4, key[:1]), ValueError),
+            (lambda: dr.sf_uniform(4, key.cpu()), ValueError), (lambda: dr.sf_uniform(4, key.int()), TypeError),
+            (lambda: dr.sf_uniform(4, key, site=-1), ValueError), (lambda: dr.sf_uniform(4, key, first=-1), StageFrontierError),
+            (lambda: dr.sf_uniform(4, key, out=u[:3]), ValueError),
+            (lambda: dr.sf_dropout(x, 1.5, key), StageFrontierError), (lambda: dr.sf_dropout(x[0], 0.1, key), ValueError),
+            (lambda: dr.sf_dropout(x.t(), 0.1, key), ValueError), (lambda: dr.sf_dropout(x.double(), 0.1, key), TypeError),
+            (lambda: dr.sf_dropout(x, 0.1, key, index_stride=299), StageFrontierError),
+            (lambda: dr.sf_dropout(x, 0.1, key, residual=x.bfloat16(), out=x.clone()), TypeError),
+            (lambda: dr.sf_dropout(x, 0.1, key, residual=x[:3]), ValueError),
+            (lambda: dr.sf_dropout(x[:, 1:], 0.1, key, out=x[:, :-1]), StageFrontierError),
+            (lambda: dr.sf_dropout(x, 0.1, key, site=1 << 32), ValueError),
+            (lambda: dr.sf_token_sample(x, u[:3]), ValueError), (lambda: dr.sf_token_sample(x, u.double()), TypeError),
+            (lambda: dr.sf_token_sample(x.t(), u), ValueError), (lambda: dr.sf_token_sample(x, u, inv_temperature=0.0), StageFrontierError),
+            (lambda: dr.sf_token_sample(x, u, out_token=torch.zeros(4, device=DEV)), TypeError),
+            (lambda: dr.sf_token_sample(x, u, out_logp=u), StageFrontierError),
+            (lambda: dr.sf_draft_verify(x, x[:2], d, s[:2], u), ValueError), (lambda: dr.sf_draft_verify(x[:3], x[:2], d, s, u), ValueError),
+            (lambda: dr.sf_draft_verify(x, x[:1], d, s, u), ValueError), (lambda: dr.sf_draft_verify(x, x[:2].half(), d, s, u), ValueError),
+            (lambda: dr.sf_draft_verify(x, x[:2], d.int(), s, u), TypeError), (lambda: dr.sf_draft_verify(x, x[:2], d, s, u[:3]), ValueError),
+            (lambda: dr.sf_draft_verify(x, x[:2], d, s, u, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV)), ValueError),
+            (lambda: dr.sf_draft_verify(x, x[:2], d, s, u, draft_inv_temperature=-1.0), StageFrontierError)):
+        with pytest.raises(error):
+            bad()
+    torch.cuda.synchronize()
