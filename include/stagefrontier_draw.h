@@ -15,8 +15,8 @@
  * replayed graph draws anew when the step in device memory has been raised.
  * Tokens are decided in 64-bit arithmetic: they are those of the definition,
  * whatever the sizes, the strides and the split of the work, but where a uniform
- * number lies within about 2^-44 of a border between two.  Probabilities below
- * 2^-1000 of a row's largest count as 0.
+ * number lies within about 2^-38 of a border between two.  Probabilities below
+ * 2^-700 of a row's largest may count as 0.
  *
  * Conventions are those of stagefrontier.h: device pointers, asynchronous on
  * the caller's stream, buffers and workspaces allocated by the caller, no

@@ -14,44 +14,127 @@ namespace sfk {
 
 constexpr int kRowsWG = 256;
 constexpr int kRowsWaves = kRowsWG / 64;
+static_assert(kRowsWaves == kSegU, "a wave for each vector of a segment");
+constexpr int64_t kFewSegments = 1024;
 constexpr int kLdsSegs = 1024;  // of a row that one workgroup takes
-
-struct RowArg {
-    int64_t stride;
-    int V, nseg;
-    double c;
-    float inv_t;
-};
 
 __device__ __forceinline__ bool in_unit(float u) { return u >= 0.0f && u < 1.0f; }
 
-// Draws a row's token by one wave from its segments' sums.
-template <int DT>
+// What is written of a row without a token: there is nothing to draw from, or it
+// is not a number.
+__device__ __forceinline__ float no_token(const RowSum& r) { return r.s == 0.0 ? -INFINITY : NAN; }
+
+// Draws a row's token from its segments' sums: by one wave, or by every wave of a
+// workgroup.
+template <int DT, bool GROUP>
 __device__ __forceinline__ void draw_token(const typename Elem<DT>::T* row, const RowSum* seg, const RowSum& r, double u,
-                                           RowArg z, int lane, int64_t* token, float* logp)
+                                           const RowArg& z, PickShared* shared, int64_t* token, float* logp)
 {
+    const int lane = threadIdx.x & 63;
     int t = -1;
     if (r.s > 0.0) {
         const double target = u * r.s;
         const Place at = pick_weight([&](int i) { return seg_weight(seg[i], r.m, z.c); }, z.nseg, target, lane);
-        const double m = r.m;
-        t = pick_entry<DT>([&](int j) { return pow2_any((double)(float)row[j] - m, z.c); }, at.i, z.V, at.base, target, lane);
+        auto value = [&](float x, int) { return pow2_any((double)x - (double)r.m, z.c); };
+        t = GROUP ? pick_entry_group<DT>(row, value, at, z.V, target, *shared) : pick_entry<DT>(row, value, at, z.V, target, lane);
     }
-    if (lane == 0) {
+    if (GROUP ? threadIdx.x == 0 : lane == 0) {
         *token = t;
-        *logp = t >= 0 ? row_logp((float)row[t], r, z.inv_t) : r.s == 0.0 ? -INFINITY : NAN;
+        *logp = t >= 0 ? row_logp((float)row[t], r, z.inv_t) : no_token(r);
     }
 }
 
-// Rows of a wave each (WAVES = 1) or a workgroup each.
-template <int DT, int WAVES>
-__global__ __launch_bounds__(kRowsWG) void k_token_sample(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
+// Rows of one segment, LIVE vectors a lane: a wave each, which keeps the powers
+// from the sum to the choice, with the next row on its way.
+template <int DT, int LIVE>
+__global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
+                                                         const float* __restrict__ uniform, RowArg z,
+                                                         int64_t* __restrict__ token, float* __restrict__ logp)
+{
+    constexpr int E = kVec<DT>;
+    const int lane = threadIdx.x & 63;
+    const int64_t step = (int64_t)gridDim.x * kRowsWaves;
+    int64_t i = (int64_t)blockIdx.x * kRowsWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (i >= N) return;
+    float u = uniform[i];
+    SegData<DT> a;
+    if (in_unit(u)) a = seg_load<DT, LIVE>(logits + i * z.stride, 0, z.V, lane);
+    for (;;) {
+        const int64_t next = i + step;
+        const float u_next = next < N ? uniform[next] : -1.0f;
+        SegData<DT> b;
+        if (in_unit(u_next)) b = seg_load<DT, LIVE>(logits + next * z.stride, 0, z.V, lane);
+        int t = -1;
+        float lp = 0.0f;
+        if (in_unit(u)) {
+            const bool above = __any(seg_above<DT>(a, z.top)), edge = __any(a.edge != -INFINITY);
+            double v[LIVE][E], ve[1] = {0.0}, own[LIVE], sum[LIVE], s = 0.0, edges = 0.0;
+#pragma unroll
+            for (int k = 0; k < LIVE; ++k) {
+                own[k] = 0.0;
+#pragma unroll
+                for (int j = 0; j < E; ++j) own[k] += v[k][j] = pow2_held((float)a.y[k][j], z);
+                sum[k] = wave_scan_f64(own[k]);
+                s += lane_f64(sum[k], 63);
+            }
+            if (edge) {
+                ve[0] = pow2_held(a.edge, z);
+                edges = wave_scan_f64(ve[0]);
+                s += lane_f64(edges, 63);
+            }
+            const typename Elem<DT>::T* row = logits + i * z.stride;
+            if (!above && sum_is_ordinary(s)) {
+                const double target = (double)u * s, none = 0x1p-999;
+                double run = 0.0;
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < LIVE; ++k) {
+                    const double behind = run + lane_f64(sum[k], 63);
+                    if (!found && (behind > target || k == LIVE - 1)) {
+                        int last = -1;
+                        const int hit = pick_scanned<E>(v[k], own[k], sum[k], run, target, lane, last, none);
+                        t = hit >= 0 ? hit + k * 64 * E : last >= 0 ? last + k * 64 * E : t;
+                        found = hit >= 0;
+                    }
+                    run = behind;
+                }
+                if (!found && edge) {
+                    int last = -1;
+                    const int hit = pick_scanned<1>(ve, ve[0], edges, run, target, lane, last, none);
+                    t = hit >= 0 ? hit + z.V - z.V % E : last >= 0 ? last + z.V - z.V % E : t;
+                }
+                lp = t >= 0 ? row_logp((float)row[t], {s, 0.0f, 0.0f}, z.inv_t) : 0.0f;
+            } else {
+                const RowSum r = seg_sum_any<DT>(a, z.c);
+                if (r.s > 0.0) {
+                    const double target = (double)u * r.s;
+                    t = pick_entry<DT>(row, [&](float x, int) { return pow2_any((double)x - (double)r.m, z.c); }, {0, 0.0}, z.V,
+                                       target, lane);
+                }
+                lp = t >= 0 ? row_logp((float)row[t], r, z.inv_t) : no_token(r);
+            }
+        }
+        if (lane == 0) {
+            token[i] = t;
+            logp[i] = lp;
+        }
+        if (next >= N) break;
+        i = next;
+        u = u_next;
+        a = b;
+    }
+}
+
+// Rows of a wave each (WAVES = 1) or a workgroup of WG threads each.
+template <int DT, int WG, int WAVES>
+__global__ __launch_bounds__(WG) void k_token_sample(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
                                                           const float* __restrict__ uniform, RowArg z,
                                                           int64_t* __restrict__ token, float* __restrict__ logp)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int ROWS = kRowsWaves / WAVES;
+    constexpr int ROWS = WG / 64 / WAVES;
     __shared__ RowSum seg[ROWS][kLdsSegs / ROWS];
+    __shared__ PickShared shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sub = WAVES == 1 ? wave : 0, w0 = WAVES == 1 ? 0 : wave;
     for (int64_t i = (int64_t)blockIdx.x * ROWS + sub; i < N; i += (int64_t)gridDim.x * ROWS) {
@@ -65,15 +148,14 @@ __global__ __launch_bounds__(kRowsWG) void k_token_sample(const typename Elem<DT
         }
         const T* row = logits + i * z.stride;
         for (int s = w0; s < z.nseg; s += WAVES) {
-            const RowSum a = seg_sum<DT>(seg_load<DT>(row, s, z.V, lane), z.c);
+            const RowSum a = seg_sum<DT>(seg_load<DT>(row, s, z.V, lane), seg_live<DT>(s, z.V), z);
             if (lane == 0) seg[sub][s] = a;
         }
         if (WAVES > 1)
             __syncthreads();
         else
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (w0 == 0)
-            draw_token<DT>(row, seg[sub], row_sum(seg[sub], z.nseg, z.c, lane), u, z, lane, token + i, logp + i);
+        draw_token<DT, (WAVES > 1)>(row, seg[sub], row_sum(seg[sub], z.nseg, z.c, lane), u, z, &shared, token + i, logp + i);
         if (WAVES > 1) __syncthreads();
     }
 }
@@ -94,33 +176,67 @@ __global__ __launch_bounds__(kRowsWG) void k_row_segments(const typename Elem<DT
         const bool first = i < rows_a;
         if (first && uniform && !in_unit(uniform[i])) continue;
         const T* row = first ? a + i * za.stride : b + (i - rows_a) * zb.stride;
-        const double c = first ? za.c : zb.c;
+        const RowArg& z = first ? za : zb;
         for (int s = s0; s < s1; ++s) {
-            const RowSum r = seg_sum<DT>(seg_load<DT>(row, s, za.V, lane), c);
+            const RowSum r = seg_sum<DT>(seg_load<DT>(row, s, za.V, lane), seg_live<DT>(s, za.V), z);
             if (lane == 0) out[i * za.nseg + s] = r;
         }
     }
 }
 
-// Draws from rows whose segments are summed: a wave each.
+// The same with a workgroup a segment: where there are few, a segment by one wave is
+// a good part of the call's time.
+template <int DT>
+__global__ __launch_bounds__(kRowsWG) void k_row_segment(const typename Elem<DT>::T* __restrict__ a, int64_t rows_a, RowArg za,
+                                                         const typename Elem<DT>::T* __restrict__ b, int64_t rows_b, RowArg zb,
+                                                         const float* __restrict__ uniform, int per, RowSum* __restrict__ out)
+{
+    __shared__ double part[kSegU][64];
+    __shared__ int above[kSegU];
+    for (int64_t i = blockIdx.y; i < rows_a + rows_b; i += gridDim.y) {
+        const bool first = i < rows_a;
+        if (first && uniform && !in_unit(uniform[i])) continue;
+        const typename Elem<DT>::T* row = first ? a + i * za.stride : b + (i - rows_a) * zb.stride;
+        const RowSum r = seg_sum_group<DT>(row, blockIdx.x, first ? za : zb, part, above);
+        if (threadIdx.x == 0) out[i * za.nseg + blockIdx.x] = r;
+    }
+}
+
+template <int DT>
+static int sum_segments(const void* a, int64_t rows_a, RowArg za, const void* b, int64_t rows_b, RowArg zb,
+                        const float* uniform, RowSum* out, sf_stream_t stream)
+{
+    const int64_t rows = rows_a + rows_b, all = rows * za.nseg;
+    int per = (int)(all < 16384 ? 1 : all > 16 * 16384 ? 16 : all / 16384);
+    void* args[] = {(void*)&a,  (void*)&rows_a,  (void*)&za,  (void*)&b,  (void*)&rows_b,
+                    (void*)&zb, (void*)&uniform, (void*)&per, (void*)&out};
+    const bool few = all <= kFewSegments;
+    const int64_t each = few ? 1 : (int64_t)kRowsWaves * per;
+    return launch(few ? (const void*)&k_row_segment<DT> : (const void*)&k_row_segments<DT>,
+                  dim3((unsigned)((za.nseg + each - 1) / each), (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
+                  stream);
+}
+
+// Draws from rows whose segments are summed: a workgroup each.
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_token_draw(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
                                                         const float* __restrict__ uniform, RowArg z,
                                                         const RowSum* __restrict__ sums, int64_t* __restrict__ token,
                                                         float* __restrict__ logp)
 {
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = (int64_t)blockIdx.x * kRowsWaves + (threadIdx.x >> 6); i < N; i += (int64_t)gridDim.x * kRowsWaves) {
+    __shared__ PickShared shared;
+    for (int64_t i = blockIdx.x; i < N; i += gridDim.x) {
         const float u = uniform[i];
         if (!in_unit(u)) {
-            if (lane == 0) {
+            if (threadIdx.x == 0) {
                 token[i] = -1;
                 logp[i] = 0.0f;
             }
             continue;
         }
         const RowSum* seg = sums + i * z.nseg;
-        draw_token<DT>(logits + i * z.stride, seg, row_sum(seg, z.nseg, z.c, lane), u, z, lane, token + i, logp + i);
+        draw_token<DT, true>(logits + i * z.stride, seg, row_sum(seg, z.nseg, z.c, threadIdx.x & 63), u, z, &shared, token + i,
+                             logp + i);
     }
 }
 
@@ -163,43 +279,43 @@ struct VerifyArg {
 // A sequence's first draft and its number of drafts, held within the arrays.
 __device__ __forceinline__ int64_t held(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-// What becomes of row k of a sequence with n drafts, by one wave.
+// What becomes of row k of a sequence with n drafts, by one wave.  What it reads
+// is asked for before it is known to be needed: a wave waits for two answers of
+// memory, not five.
 template <int DT>
 __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b, int64_t s, int64_t n, int64_t k, int lane)
 {
     const int64_t i = s + b + k;
+    const int64_t d = k < n ? a.draft[s + k] : -1;
     const float u = a.uniform[i];
+    const bool some = d >= 0 && d < a.z.V, judged = some && a.drafts;
+    const float x = some ? (float)a.target[i * a.z.stride + d] : 0.0f;
+    const float y = judged ? (float)a.drafts[(s + k) * a.zq.stride + d] : 0.0f;
     Verdict v = {};
+    v.p = row_sum(a.sums + i * a.z.nseg, a.z.nseg, a.z.c, lane);
+    if (judged) v.q = row_sum(a.sums + (a.D + a.B + s + k) * a.z.nseg, a.z.nseg, a.zq.c, lane);
     v.what = ROW_END;
     if (!in_unit(u)) return v;
-    v.p = row_sum(a.sums + i * a.z.nseg, a.z.nseg, a.z.c, lane);
     if (!(v.p.s > 0.0)) {
-        v.logp = v.p.s == 0.0 ? -INFINITY : NAN;
+        v.logp = no_token(v.p);
         return v;
     }
     v.what = ROW_PLAIN;
-    if (k == n) return v;
-    const int64_t d = a.draft[s + k];
-    if (d < 0 || d >= a.z.V) return v;
-    const float x = (float)a.target[i * a.z.stride + d];
+    if (!some) return v;
     const double pd = pow2_any((double)x - (double)v.p.m, a.z.c) / v.p.s;
     double qd = 1.0;
-    if (a.drafts) {
-        v.q = row_sum(a.sums + (a.D + a.B + s + k) * a.z.nseg, a.z.nseg, a.zq.c, lane);
+    if (judged) {
         if (v.q.s != v.q.s) {
             v.what = ROW_END;
             v.logp = NAN;
             return v;
         }
-        if (v.q.s == 0.0)
-            qd = 0.0;
-        else
-            qd = pow2_any((double)(float)a.drafts[(s + k) * a.zq.stride + d] - (double)v.q.m, a.zq.c) / v.q.s;
+        qd = v.q.s > 0.0 ? pow2_any((double)y - (double)v.q.m, a.zq.c) / v.q.s : 0.0;
     }
     if ((double)u * qd < pd) {
         v.what = ROW_ACCEPT;
         v.logp = row_logp(x, v.p, a.z.inv_t);
-    } else if (!a.drafts) {
+    } else if (!judged) {
         v.what = ROW_OTHER;
     } else if (v.q.s > 0.0) {
         v.what = ROW_RESIDUAL;
@@ -207,15 +323,21 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     return v;
 }
 
-template <int DT>
-__device__ __forceinline__ double entry_residual(float xp, float xq, const Verdict& v, double p_of, double q_of, RowArg z,
-                                                 RowArg zq)
-{
+// max(p - q, 0) of an entry.
+struct Residual {
+    double mp, mq, cp, cq, p_of, q_of;
+    __device__ Residual(const Verdict& v, const RowArg& z, const RowArg& zq)
+        : mp(v.p.m), mq(v.q.m), cp(z.c), cq(zq.c), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s)
+    {
+    }
+    __device__ __forceinline__ double operator()(float xp, float xq) const
+    {
 #pragma clang fp contract(off)  // equal rows leave nothing
-    const double p = pow2_any((double)xp - (double)v.p.m, z.c) * p_of;
-    const double q = pow2_any((double)xq - (double)v.q.m, zq.c) * q_of;
-    return p > q ? p - q : 0.0;
-}
+        const double p = pow2_any((double)xp - mp, cp) * p_of;
+        const double q = pow2_any((double)xq - mq, cq) * q_of;
+        return p > q ? p - q : 0.0;
+    }
+};
 
 // Where a sequence ends, for the launch that draws its token.
 struct Outcome {
@@ -224,16 +346,16 @@ struct Outcome {
     int64_t draft;     // the draft refused
 };
 
-// Draws a sequence's last token by one wave.
+// Draws a sequence's last token by every wave of a workgroup.
 template <int DT>
-__device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, const Outcome& o, int lane)
+__device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, const Outcome& o, PickShared& shared)
 {
     typedef typename Elem<DT>::T T;
+    const int lane = threadIdx.x & 63;
     const Verdict& v = o.v;
-    const double u = a.uniform[o.last];
-    const bool drawn = v.what != ROW_END && in_unit((float)u);
-    if (!drawn) {
-        if (lane == 0) {
+    const float u = a.uniform[o.last];
+    if (v.what == ROW_END || !in_unit(u)) {
+        if (threadIdx.x == 0) {
             a.token[o.at] = -1;
             a.logp[o.at] = v.what == ROW_END ? v.logp : 0.0f;
         }
@@ -249,50 +371,52 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
         total = wave_sum_f64(total);
         if (total >= kLeastResidual) {
             const T* xq = a.drafts + (o.at - b) * a.zq.stride;
-            const double p_of = 1.0 / v.p.s, q_of = 1.0 / v.q.s, target = u * total;
+            const Residual residual(v, a.z, a.zq);
+            const double target = (double)u * total;
             const Place at = pick_weight([&](int g) { return part[g]; }, a.z.nseg, target, lane);
-            t = pick_entry<DT>(
-                [&](int j) { return entry_residual<DT>((float)xp[j], (float)xq[j], v, p_of, q_of, a.z, a.zq); }, at.i,
-                a.z.V, at.base, target, lane);
+            t = pick_entry_group<DT>(xp, [&](float x, int j) { return residual(x, (float)xq[j]); }, at, a.z.V, target, shared);
         }
     } else if (v.what == ROW_OTHER) {
         const int d = (int)o.draft, gd = d / kSeg<DT>;
-        const double m = v.p.m;
-        auto value = [&](int j) { return j == d ? 0.0 : pow2_any((double)(float)xp[j] - m, a.z.c); };
+        auto value = [&](float x, int j) { return j == d ? 0.0 : pow2_any((double)x - (double)v.p.m, a.z.c); };
         double own = 0.0;
-        for (int j = gd * kSeg<DT> + lane; j < a.z.V && j < (gd + 1) * kSeg<DT>; j += 64) own += value(j);
+        for (int j = gd * kSeg<DT> + lane; j < a.z.V && j < (gd + 1) * kSeg<DT>; j += 64) own += value((float)xp[j], j);
         own = wave_sum_f64(own);
         auto weight = [&](int g) { return g == gd ? own : seg_weight(seg[g], v.p.m, a.z.c); };
         double total = 0.0;
         for (int g = lane; g < a.z.nseg; g += 64) total += weight(g);
         total = wave_sum_f64(total);
         if (total >= kLeastResidual * v.p.s) {
-            const double target = u * total;
-            const Place at = pick_weight(weight, a.z.nseg, target, lane);
-            t = pick_entry<DT>(value, at.i, a.z.V, at.base, target, lane);
+            const double target = (double)u * total;
+            t = pick_entry_group<DT>(xp, value, pick_weight(weight, a.z.nseg, target, lane), a.z.V, target, shared);
         }
     }
     if (t < 0) {  // from p, also where rounding leaves nothing else
-        draw_token<DT>(xp, seg, v.p, u, a.z, lane, a.token + o.at, a.logp + o.at);
-    } else if (lane == 0) {
+        draw_token<DT, true>(xp, seg, v.p, u, a.z, &shared, a.token + o.at, a.logp + o.at);
+    } else if (threadIdx.x == 0) {
         a.token[o.at] = t;
         a.logp[o.at] = row_logp((float)xp[t], v.p, a.z.inv_t);
     }
 }
 
+constexpr int kVerifyWG = 512;
+constexpr int kVerifyWaves = kVerifyWG / 64;
+
 // A workgroup takes a sequence, or part blockIdx.x of its residual's sums: the
-// drafts four at a time (every part the same), then segments of the residual.
+// drafts eight at a time (every part the same), then segments of the residual.
 // With one part it draws the token, too.
-template <int DT>
-__global__ __launch_bounds__(kRowsWG) void k_draft_verify(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
+template <int DT, bool FEW>
+__global__ __launch_bounds__(kVerifyWG) void k_draft_verify(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
     typedef typename Elem<DT>::T T;
-    __shared__ Verdict row[kRowsWaves];
+    __shared__ Verdict row[kVerifyWaves];
+    __shared__ PickShared shared;
+    __shared__ double part[FEW ? kVerifyWaves : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
         const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
         int64_t end;
-        for (int64_t k0 = 0;; k0 += kRowsWaves) {
+        for (int64_t k0 = 0;; k0 += kVerifyWaves) {
             const int64_t k = k0 + wave;
             Verdict v = {};
             v.what = ROW_PLAIN;
@@ -300,23 +424,23 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_verify(VerifyArg<DT> a, Outco
             if (lane == 0) row[wave] = v;
             __syncthreads();
             int w = 0;
-            while (w < kRowsWaves && row[w].what == ROW_ACCEPT) ++w;
+            while (w < kVerifyWaves && row[w].what == ROW_ACCEPT) ++w;
             if (blockIdx.x == 0 && wave < w && lane == 0) {
                 a.token[s + b + k] = a.draft[s + k];
                 a.logp[s + b + k] = v.logp;
             }
             end = k0 + w;
-            if (w < kRowsWaves) break;  // row n at the latest
+            if (w < kVerifyWaves) break;  // row n at the latest
             __syncthreads();
         }
         Outcome o;
-        o.v = row[end % kRowsWaves];
+        o.v = row[end % kVerifyWaves];
         o.at = s + b + end;
         o.last = s + b + n;
         o.draft = end < n ? a.draft[s + end] : -1;
         if (blockIdx.x == 0) {
             if (threadIdx.x == 0) a.accepted[b] = end;
-            for (int64_t k = end + 1 + threadIdx.x; k <= n; k += kRowsWG) {
+            for (int64_t k = end + 1 + threadIdx.x; k <= n; k += kVerifyWG) {
                 a.token[s + b + k] = -1;
                 a.logp[s + b + k] = 0.0f;
             }
@@ -325,32 +449,53 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_verify(VerifyArg<DT> a, Outco
         if (o.v.what == ROW_RESIDUAL) {
             const T* xp = a.target + o.at * a.z.stride;
             const T* xq = a.drafts + (s + end) * a.zq.stride;
-            const double p_of = 1.0 / o.v.p.s, q_of = 1.0 / o.v.q.s;
-            for (int g = (int)blockIdx.x * kRowsWaves + wave; g < a.z.nseg; g += (int)gridDim.x * kRowsWaves) {
+            const Residual residual(o.v, a.z, a.zq);
+            // a segment by four waves, added in the order of one wave's
+            if (FEW) {
+                const int g = (int)blockIdx.x * 2 + wave / kSegU, k = wave % kSegU;
+                const int at = g * kSeg<DT> + (k * 64 + lane) * kVec<DT>, tail = a.z.V - a.z.V % kVec<DT> + lane;
+                double sum = 0.0;
+                if (at + kVec<DT> <= a.z.V) {
+                    const VecU<DT> x = *(const VecU<DT>*)(xp + at), y = *(const VecU<DT>*)(xq + at);
+#pragma unroll
+                    for (int j = 0; j < kVec<DT>; ++j) sum += residual((float)x[j], (float)y[j]);
+                }
+                part[wave][lane] = sum;
+                __syncthreads();
+                if (k == 0 && g < a.z.nseg) {
+                    sum = g == a.z.nseg - 1 && tail < a.z.V ? residual((float)xp[tail], (float)xq[tail]) : 0.0;
+                    for (int i = 0; i < kSegU; ++i) sum += part[wave + i][lane];
+                    sum = wave_sum_f64(sum);
+                    if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
+                }
+            }
+            for (int g = FEW ? a.z.nseg : (int)blockIdx.x * kVerifyWaves + wave; g < a.z.nseg; g += (int)gridDim.x * kVerifyWaves) {
                 const SegData<DT> x = seg_load<DT>(xp, g, a.z.V, lane), y = seg_load<DT>(xq, g, a.z.V, lane);
-                double sum = entry_residual<DT>(x.edge, y.edge, o.v, p_of, q_of, a.z, a.zq);
+                double sum = residual(x.edge, y.edge);
 #pragma unroll
-                for (int k = 0; k < kSegU; ++k)
+                for (int k = 0; k < kSegU; ++k) {
+                    double own = 0.0;
 #pragma unroll
-                    for (int j = 0; j < kVec<DT>; ++j)
-                        sum += entry_residual<DT>((float)x.y[k][j], (float)y.y[k][j], o.v, p_of, q_of, a.z, a.zq);
+                    for (int j = 0; j < kVec<DT>; ++j) own += residual((float)x.y[k][j], (float)y.y[k][j]);
+                    sum += own;
+                }
                 sum = wave_sum_f64(sum);
                 if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
             }
         }
         __syncthreads();
-        if (gridDim.x == 1 && wave == 0) draw_last<DT>(a, b, o, lane);
+        if (gridDim.x == 1) draw_last<DT>(a, b, o, shared);
         __syncthreads();
     }
 }
 
-// Draws the last tokens of sequences whose residuals were summed by parts.
+// Draws the last tokens of sequences whose residuals were summed by parts: a
+// workgroup each.
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_draft_draw(VerifyArg<DT> a, const Outcome* __restrict__ outcomes)
 {
-    const int lane = threadIdx.x & 63;
-    for (int64_t b = (int64_t)blockIdx.x * kRowsWaves + (threadIdx.x >> 6); b < a.B; b += (int64_t)gridDim.x * kRowsWaves)
-        draw_last<DT>(a, b, outcomes[b], lane);
+    __shared__ PickShared shared;
+    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) draw_last<DT>(a, b, outcomes[b], shared);
 }
 
 static inline bool rows_ok(int32_t dtype, int64_t N, int64_t V, int64_t stride, float inv_t)
@@ -362,23 +507,27 @@ static inline bool rows_ok(int32_t dtype, int64_t N, int64_t V, int64_t stride, 
 
 static inline RowArg row_arg(int32_t dtype, int64_t V, int64_t stride, float inv_t)
 {
-    return {stride, (int)V, (int)seg_count(dtype, V), (double)inv_t * kLog2eD, inv_t};
+    const double c = (double)inv_t * kLog2eD, far = 1000.0 / c;
+    const float limit = far < 3.4e38 ? (float)far : INFINITY;
+    return {stride, (int)V, (int)seg_count(dtype, V), c, inv_t, -limit, limit};
 }
 
-// Segments a wave takes where rows are split over workgroups.
-static inline int segs_per_wave(int64_t rows, int64_t nseg)
+// Vectors a lane of a row of one segment.
+static inline int seg_live(int dtype, int64_t V)
 {
-    const int64_t per = rows * nseg / 16384;
-    return (int)(per < 1 ? 1 : per > 16 ? 16 : per);
+    const int step = dtype == SF_F32 ? 64 * kVec<SF_F32> : 64 * kVec<SF_BF16>;
+    return (int)((V - V % (step / 64) + step - 1) / step);
 }
 
 static inline unsigned up_to(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
 
-// Waves of a row: 1, kRowsWaves, or 0 where rows are split over workgroups.
-static inline int sample_waves(int64_t N, int64_t nseg)
+// Threads that a row has to itself: 64, kRowsWG or 1024, or 0 where rows are split
+// over workgroups.
+static inline int sample_threads(int64_t N, int64_t nseg)
 {
-    if (nseg <= 2 || (N >= 4096 && nseg <= kLdsSegs / kRowsWaves)) return 1;
-    return N >= 512 && nseg <= kLdsSegs ? kRowsWaves : 0;
+    if (nseg == 1 || (N >= 4096 && nseg <= kLdsSegs / kRowsWaves)) return 64;
+    if (N >= 512) return nseg <= kLdsSegs ? kRowsWG : 0;
+    return nseg <= 32 ? 1024 : 0;
 }
 
 }  // namespace sfk
@@ -389,7 +538,7 @@ SF_API int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V)
 {
     if (!rows_ok(dtype, N, V, V, 1.0f)) return -1;
     const int64_t nseg = seg_count(dtype, V);
-    return N == 0 || sample_waves(N, nseg) ? 0 : N * nseg * (int64_t)sizeof(RowSum);
+    return N == 0 || sample_threads(N, nseg) ? 0 : N * nseg * (int64_t)sizeof(RowSum);
 }
 
 SF_API int sf_token_sample(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t row_stride,
@@ -414,32 +563,36 @@ SF_API int sf_token_sample(const void* logits, int32_t dtype, int64_t N, int64_t
             if (sizes[j] > 0 && !disjoint(outs[i], sizes[i], outs[j], sizes[j])) return SF_EINVAL;
     }
     RowArg z = row_arg(dtype, V, row_stride, inv_temperature);
-    const int waves = sample_waves(N, z.nseg);
+    const int threads = sample_threads(N, z.nseg);
     void* args[] = {(void*)&logits, (void*)&N, (void*)&uniform, (void*)&z, (void*)&out_token, (void*)&out_logp};
-    if (waves) {
-        const void* fn[2][3] = {{(const void*)&k_token_sample<SF_F32, 1>, (const void*)&k_token_sample<SF_BF16, 1>,
-                                 (const void*)&k_token_sample<SF_F16, 1>},
-                                {(const void*)&k_token_sample<SF_F32, kRowsWaves>, (const void*)&k_token_sample<SF_BF16, kRowsWaves>,
-                                 (const void*)&k_token_sample<SF_F16, kRowsWaves>}};
-        const int rows = kRowsWaves / waves;
-        return launch(fn[waves > 1][dtype], dim3(up_to((N + rows - 1) / rows, 1 << 21)), dim3(kRowsWG), args, 0, stream);
+    if (z.nseg == 1) {
+        const int live = seg_live(dtype, V);
+        const void* fn[3][3] = {
+            {(const void*)&k_token_short<SF_F32, 1>, (const void*)&k_token_short<SF_BF16, 1>, (const void*)&k_token_short<SF_F16, 1>},
+            {(const void*)&k_token_short<SF_F32, 2>, (const void*)&k_token_short<SF_BF16, 2>, (const void*)&k_token_short<SF_F16, 2>},
+            {(const void*)&k_token_short<SF_F32, 4>, (const void*)&k_token_short<SF_BF16, 4>, (const void*)&k_token_short<SF_F16, 4>}};
+        return launch(fn[live <= 1 ? 0 : live == 2 ? 1 : 2][dtype], dim3(up_to((N + kRowsWaves - 1) / kRowsWaves, 2048)),
+                      dim3(kRowsWG), args, 0, stream);
     }
-    const void* none = nullptr;
-    int64_t zero = 0;
-    int per = segs_per_wave(N, z.nseg);
-    const int64_t each = (int64_t)kRowsWaves * per;
-    void* sum_args[] = {(void*)&logits, (void*)&N, (void*)&z, (void*)&none, (void*)&zero, (void*)&z, (void*)&uniform,
-                        (void*)&per, (void*)&workspace};
-    const void* sums[3] = {(const void*)&k_row_segments<SF_F32>, (const void*)&k_row_segments<SF_BF16>,
-                           (const void*)&k_row_segments<SF_F16>};
-    const int rc = launch(sums[dtype], dim3((unsigned)((z.nseg + each - 1) / each), up_to(N, 65535)), dim3(kRowsWG), sum_args,
-                          0, stream);
+    if (threads) {
+        const void* fn[3][3] = {{(const void*)&k_token_sample<SF_F32, kRowsWG, 1>, (const void*)&k_token_sample<SF_BF16, kRowsWG, 1>,
+                                 (const void*)&k_token_sample<SF_F16, kRowsWG, 1>},
+                                {(const void*)&k_token_sample<SF_F32, kRowsWG, 4>, (const void*)&k_token_sample<SF_BF16, kRowsWG, 4>,
+                                 (const void*)&k_token_sample<SF_F16, kRowsWG, 4>},
+                                {(const void*)&k_token_sample<SF_F32, 1024, 16>, (const void*)&k_token_sample<SF_BF16, 1024, 16>,
+                                 (const void*)&k_token_sample<SF_F16, 1024, 16>}};
+        const int wg = threads == 64 ? kRowsWG : threads, rows = wg / threads;
+        return launch(fn[threads == 64 ? 0 : threads == kRowsWG ? 1 : 2][dtype], dim3(up_to((N + rows - 1) / rows, 1 << 21)),
+                      dim3(wg), args, 0, stream);
+    }
+    auto sums = dtype == SF_F32 ? sum_segments<SF_F32> : dtype == SF_BF16 ? sum_segments<SF_BF16> : sum_segments<SF_F16>;
+    const int rc = sums(logits, N, z, nullptr, 0, z, uniform, (RowSum*)workspace, stream);
     if (rc != SF_OK) return rc;
     void* draw_args[] = {(void*)&logits, (void*)&N, (void*)&uniform, (void*)&z, (void*)&workspace, (void*)&out_token,
                          (void*)&out_logp};
     const void* draw[3] = {(const void*)&k_token_draw<SF_F32>, (const void*)&k_token_draw<SF_BF16>,
                            (const void*)&k_token_draw<SF_F16>};
-    return launch(draw[dtype], dim3(up_to((N + kRowsWaves - 1) / kRowsWaves, 1 << 21)), dim3(kRowsWG), draw_args, 0, stream);
+    return launch(draw[dtype], dim3(up_to(N, 1 << 21)), dim3(kRowsWG), draw_args, 0, stream);
 }
 
 // The workspace: the segments' sums of the target's rows and of the drafts', the
@@ -469,22 +622,19 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     double* residual = (double*)(ws + verify_sums(D, B, z.nseg));
     Outcome* outcomes = (Outcome*)(ws + verify_sums(D, B, z.nseg) + verify_residuals(B, z.nseg));
     int64_t rows = D + B, more = drafts ? D : 0;
-    const void* none = nullptr;
-    int per = segs_per_wave(rows + more, z.nseg);
-    const int64_t each = (int64_t)kRowsWaves * per;
-    void* sum_args[] = {(void*)&target, (void*)&rows, (void*)&z,    (void*)&drafts, (void*)&more,
-                        (void*)&zq,     (void*)&none, (void*)&per, (void*)&sums};
-    int rc = launch((const void*)&k_row_segments<DT>, dim3((unsigned)((z.nseg + each - 1) / each), up_to(rows + more, 65535)),
-                    dim3(kRowsWG), sum_args, 0, stream);
+    int rc = sum_segments<DT>(target, rows, z, drafts, more, zq, nullptr, sums, stream);
     if (rc != SF_OK) return rc;
     VerifyArg<DT> a = {(const T*)target, (const T*)drafts, draft, start, uniform, D, B, z, zq, sums, residual, accepted, token, logp};
-    // parts of a residual: about 1024 workgroups in all
-    const int64_t most = (z.nseg + kRowsWaves - 1) / kRowsWaves, want = 1024 / B;
-    const int64_t parts = !drafts || want < 2 ? 1 : most < want ? most : want;
+    // Parts of a residual: two segments each where there are few, else about 1024
+    // workgroups in all.
+    const bool few = drafts && B * z.nseg <= kFewSegments;
+    const int64_t most = (z.nseg + kVerifyWaves - 1) / kVerifyWaves, want = 1024 / B;
+    const int64_t parts = few ? (z.nseg + 1) / 2 : !drafts || want < 2 ? 1 : most < want ? most : want;
     void* args[] = {(void*)&a, (void*)&outcomes};
-    rc = launch((const void*)&k_draft_verify<DT>, dim3((unsigned)parts, up_to(B, 65535)), dim3(kRowsWG), args, 0, stream);
+    rc = launch(few ? (const void*)&k_draft_verify<DT, true> : (const void*)&k_draft_verify<DT, false>,
+                dim3((unsigned)parts, up_to(B, 65535)), dim3(kVerifyWG), args, 0, stream);
     if (rc != SF_OK || parts == 1) return rc;
-    return launch((const void*)&k_draft_draw<DT>, dim3(up_to((B + kRowsWaves - 1) / kRowsWaves, 1 << 21)), dim3(kRowsWG), args,
+    return launch((const void*)&k_draft_draw<DT>, dim3(up_to(B, 1 << 21)), dim3(kRowsWG), args,
                   0, stream);
 }
 

@@ -3,6 +3,8 @@
 // of an entry by its place in the cumulative sums.
 #pragma once
 
+#include <type_traits>
+
 #include "sf_train.h"
 
 namespace sfk {
@@ -40,31 +42,42 @@ __device__ __forceinline__ Words draw_words(const int64_t* key, int64_t block, u
 
 // -- powers of two in 64 bits ------------------------------------------------
 
-// 2^(d c) for |d c| < 2^31, within 2^-45: the whole part by the addition of
-// 1.5 * 2^52, whose sum holds it in its low word, the rest f in [-1/2, 1/2] by the
-// interpolation of 2^f of degree 9 at Chebyshev's points (error 1.9e-14; degree
-// 8 gives 1.1e-12, one multiply-add less of 18).  A product that rounds once, in
-// either multiply-add, so d need not be rounded to a whole number of anything.
-__device__ __forceinline__ double pow2(double d, double c)
+// 2^f for f in [-1/2, 1/2] within 2^-39.7: the interpolation of degree 8 at
+// Chebyshev's points.  (Each degree is one of 16 instructions an entry, and a
+// factor of 58 in the error.)
+__device__ __forceinline__ double pow2_rest(double f)
 {
-    const double big = 6755399441055744.0;
-    const double whole = fma(d, c, big);
-    const double f = fma(d, c, big - whole);
-    double p = 1.0205905413765595e-07;
-    p = fma(p, f, 1.325964524488711e-06);
-    p = fma(p, f, 1.5252672924850737e-05);
-    p = fma(p, f, 0.0001540343375125101);
-    p = fma(p, f, 0.0013333558200794592);
-    p = fma(p, f, 0.009618129193934313);
-    p = fma(p, f, 0.05550410866465167);
-    p = fma(p, f, 0.2402265069564034);
-    p = fma(p, f, 0.6931471805599462);
-    p = fma(p, f, 1.0000000000000135);
+    double p = 1.3255224878668817e-06;
+    p = fma(p, f, 1.5310079402249296e-05);
+    p = fma(p, f, 0.00015403455852453838);
+    p = fma(p, f, 0.0013333450568000645);
+    p = fma(p, f, 0.009618129159402558);
+    p = fma(p, f, 0.05550410941205933);
+    p = fma(p, f, 0.2402265069581299);
+    p = fma(p, f, 0.6931471805459335);
+    return fma(p, f, 1.0);
+}
+
+// The sum of kWhole and a number below 2^31 is a whole number plus kWhole, and holds
+// it in its low word.
+constexpr double kWhole = 6755399441055744.0;  // 1.5 * 2^52
+
+// 2^(x c) for |x c| < 2^31: x c = whole + f by two multiply-adds, each rounded once.
+__device__ __forceinline__ double pow2(double x, double c)
+{
+    const double whole = fma(x, c, kWhole);
+    const double p = pow2_rest(fma(x, c, kWhole - whole));
     return ldexp(p, (int)(uint32_t)(uint64_t)__double_as_longlong(whole));
 }
 
-// The same for any d c up to 0 and any c > 0: nothing is left below 2^-1000.
-__device__ __forceinline__ double pow2_any(double d, double c) { return d * c < -1000.0 ? 0.0 : pow2(d, c); }
+// 2^(d c) for any d c up to 0 (or somewhat above): 0 below 2^-1000, NaN for NaN.
+// (Chosen, not branched for: the power of 0 in its place.)
+__device__ __forceinline__ double pow2_any(double d, double c)
+{
+    const bool far = d * c < -1000.0;
+    const double p = pow2(far ? 0.0 : d, c);
+    return far ? 0.0 : p;
+}
 
 // -- rows of logits by segments ----------------------------------------------
 
@@ -81,20 +94,40 @@ static inline int64_t seg_count(int dtype, int64_t V)
     return (V + seg - 1) / seg;
 }
 
-// s = sum 2^((x - m) c) over a segment or row, m its largest x.  m = -inf: nothing
-// but -inf, s = 0.  s is NaN where there is +inf or NaN.
+// What a call knows of its rows.
+struct RowArg {
+    int64_t stride;
+    int V, nseg;
+    double c;  // log2(e) / T
+    float inv_t;
+    float floor, top;  // x c = -1000 and 1000
+};
+
+// s = sum 2^((x - m) c) over a segment or row.  m is 0 for a segment of ordinary
+// logits, else its largest x; a row's is the largest of its segments'.  m = -inf:
+// nothing but -inf, s = 0.  s is NaN where there is +inf or NaN.
 struct RowSum {
     double s;
     float m, pad;
 };
 
+// What a lane holds of a segment: its vectors, and one of the entries behind the
+// row's last whole vector; -inf where there is none.
 template <int DT>
 struct SegData {
     VecU<DT> y[kSegU];
-    float edge;  // an entry behind the last whole vector, -inf: none
+    float edge;
 };
 
+// How many of a segment's vectors have entries.
 template <int DT>
+__device__ __forceinline__ int seg_live(int seg, int V)
+{
+    const int n = V - seg * kSeg<DT>, step = 64 * kVec<DT>;
+    return n >= kSeg<DT> ? kSegU : (n - n % kVec<DT> + step - 1) / step;
+}
+
+template <int DT, int LIVE = kSegU>
 __device__ __forceinline__ SegData<DT> seg_load(const typename Elem<DT>::T* row, int seg, int V, int lane)
 {
     typedef typename Elem<DT>::T T;
@@ -102,14 +135,14 @@ __device__ __forceinline__ SegData<DT> seg_load(const typename Elem<DT>::T* row,
     const int at = seg * kSeg<DT> + lane * E;
     SegData<DT> a;
     a.edge = -INFINITY;
-    if (seg * kSeg<DT> + kSeg<DT> <= V) {
+    if (LIVE == kSegU && seg * kSeg<DT> + kSeg<DT> <= V) {
 #pragma unroll
         for (int k = 0; k < kSegU; ++k) a.y[k] = __builtin_nontemporal_load((const VecU<DT>*)(row + at + k * 64 * E));
     } else {
 #pragma unroll
         for (int k = 0; k < kSegU; ++k) {
             a.y[k] = (VecU<DT>)(T)-INFINITY;
-            if (at + k * 64 * E + E <= V) a.y[k] = __builtin_nontemporal_load((const VecU<DT>*)(row + at + k * 64 * E));
+            if (k < LIVE && at + k * 64 * E + E <= V) a.y[k] = __builtin_nontemporal_load((const VecU<DT>*)(row + at + k * 64 * E));
         }
         const int tail = V - V % E + lane;
         if (tail < V) a.edge = (float)row[tail];
@@ -117,51 +150,133 @@ __device__ __forceinline__ SegData<DT> seg_load(const typename Elem<DT>::T* row,
     return a;
 }
 
-// The segment's sum, in every lane.  Where no entry lies so far below the
-// largest that its power leaves 64 bits' range, none is asked about.
+// The larger, NaN where one of them is, unlike fmaxf.
+__device__ __forceinline__ float max_or_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// The segment's sum, in every lane, for any logits: relative to the largest, each
+// entry asked about.
 template <int DT>
-__device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, double c)
+__device__ __forceinline__ RowSum seg_sum_any(const SegData<DT>& a, double c)
 {
     constexpr int E = kVec<DT>;
-    float top = a.edge, low = INFINITY;
+    float top = a.edge;
 #pragma unroll
     for (int k = 0; k < kSegU; ++k)
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            top = fmaxf(top, (float)a.y[k][j]);
-            low = fminf(low, (float)a.y[k][j]);
-        }
+        for (int j = 0; j < E; ++j) top = max_or_nan(top, (float)a.y[k][j]);
     const float m = wave_max_f32(top);
-    double s = 0.0;
-    if (m == -INFINITY || m == INFINITY) {
-        bool nan = m == INFINITY || a.edge != a.edge;
+    if (__any(!(top < INFINITY))) return {(double)NAN, m, 0.0f};
+    if (m == -INFINITY) return {0.0, m, 0.0f};
+    double s = pow2_any((double)a.edge - (double)m, c);
 #pragma unroll
-        for (int k = 0; k < kSegU; ++k)
+    for (int k = 0; k < kSegU; ++k)
 #pragma unroll
-            for (int j = 0; j < E; ++j) nan |= (float)a.y[k][j] != (float)a.y[k][j];
-        return {__any(nan) ? (double)NAN : 0.0, m, 0.0f};
-    }
-    const double md = m;
-    if (__any(!(((double)low - md) * c >= -1000.0))) {
-        s = pow2_any((double)a.edge - md, c);
-#pragma unroll
-        for (int k = 0; k < kSegU; ++k)
-#pragma unroll
-            for (int j = 0; j < E; ++j) s += pow2_any((double)(float)a.y[k][j] - md, c);
-    } else {
-        // (a segment with an edge lacks a vector, so it holds -inf and is not summed here)
-#pragma unroll
-        for (int k = 0; k < kSegU; ++k)
-#pragma unroll
-            for (int j = 0; j < E; ++j) s += pow2((double)(float)a.y[k][j] - md, c);
-    }
+        for (int j = 0; j < E; ++j) s += pow2_any((double)(float)a.y[k][j] - (double)m, c);
     return {wave_sum_f64(s), m, 0.0f};
 }
 
-// A segment's weight relative to the row's largest entry.
+// A power as a segment of ordinary logits takes it: held at 2^-1000 below, NaN for NaN.
+__device__ __forceinline__ double pow2_held(float x, const RowArg& z) { return pow2((double)max_or_nan(x, z.floor), z.c); }
+
+template <int DT>
+__device__ __forceinline__ double vector_sum(const VecU<DT>& y, const RowArg& z)
+{
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < kVec<DT>; ++j) s += pow2_held((float)y[j], z);
+    return s;
+}
+
+// A vector's bits as whole numbers, whose order is that of positive entries, NaN
+// above all: packed comparisons take half an instruction an entry.
+template <int DT>
+using VecBits = typename std::conditional<DT == SF_F32, int32_t, int16_t>::type __attribute__((ext_vector_type(kVec<DT>)));
+template <int DT>
+__device__ __forceinline__ bool bits_above(const VecBits<DT>& top, float limit)
+{
+    const auto bits = __builtin_bit_cast(typename std::conditional<DT == SF_F32, int32_t, int16_t>::type,
+                                         (typename Elem<DT>::T)limit);
+    bool above = false;
+#pragma unroll
+    for (int j = 0; j < kVec<DT>; ++j) above |= top[j] >= bits;
+    return above;
+}
+template <int DT>
+__device__ __forceinline__ bool vector_above(const VecU<DT>& y, float limit)
+{
+    return bits_above<DT>(__builtin_bit_cast(VecBits<DT>, y), limit);
+}
+// Whether an entry of the lane lies at or above a positive limit.
+template <int DT>
+__device__ __forceinline__ bool seg_above(const SegData<DT>& a, float limit)
+{
+    VecBits<DT> top = __builtin_bit_cast(VecBits<DT>, (VecU<DT>)a.y[0]);
+#pragma unroll
+    for (int k = 1; k < kSegU; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(VecBits<DT>, (VecU<DT>)a.y[k]));
+    return bits_above<DT>(top, limit) || !(a.edge < limit);
+}
+
+// Whether sums of powers taken as they are keep what counts: at least 2^800 over
+// what is held, and far from the largest number.
+__device__ __forceinline__ bool sum_is_ordinary(double s) { return s > 0x1p-200 && s < 0x1p900; }
+
+// The segment's sum, in every lane.  64 bits have room for powers of ordinary
+// logits as they are, so no maximum is looked for: only whether one lies above
+// that room.  Where the sum shows that the segment is another, it is done again.
+template <int DT>
+__device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, int live, const RowArg& z)
+{
+    constexpr int E = kVec<DT>;
+    const bool above = __any(seg_above<DT>(a, z.top));
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kSegU; ++k)
+        if (k < live) s += vector_sum<DT>(a.y[k], z);
+    if (__any(a.edge != -INFINITY)) s += pow2_held(a.edge, z);
+    s = wave_sum_f64(s);
+    if (!above && sum_is_ordinary(s)) return {s, 0.0f, 0.0f};
+    return seg_sum_any<DT>(a, z.c);
+}
+
+// The same by four waves of a workgroup, a vector each, whose sums meet in `part`
+// lane by lane: the same additions in the same order.  Wave-uniform in the first
+// wave only; every wave of the workgroup takes part.
+template <int DT>
+__device__ __forceinline__ RowSum seg_sum_group(const typename Elem<DT>::T* row, int seg, const RowArg& z, double (&part)[kSegU][64],
+                                                int (&above)[kSegU])
+{
+    typedef typename Elem<DT>::T T;
+    constexpr int E = kVec<DT>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at = seg * kSeg<DT> + (wave * 64 + lane) * E;
+    VecU<DT> y = (VecU<DT>)(T)-INFINITY;
+    if (at + E <= z.V) y = *(const VecU<DT>*)(row + at);
+    const int tail = z.V - z.V % E + lane;
+    float edge = -INFINITY;
+    if (wave == 0 && tail < z.V && tail < (seg + 1) * kSeg<DT>) edge = (float)row[tail];
+    const bool high = __any(vector_above<DT>(y, z.top) || !(edge < z.top));
+    __syncthreads();  // a former segment's are read
+    part[wave][lane] = vector_sum<DT>(y, z);
+    if (lane == 0) above[wave] = high;
+    __syncthreads();
+    if (wave != 0) return {};
+    const int live = seg_live<DT>(seg, z.V);
+    double s = 0.0;
+    bool any = false;
+    for (int k = 0; k < kSegU; ++k) {
+        any |= above[k] != 0;
+        if (k < live) s += part[k][lane];
+    }
+    if (__any(edge != -INFINITY)) s += pow2_held(edge, z);
+    s = wave_sum_f64(s);
+    if (!any && sum_is_ordinary(s)) return {s, 0.0f, 0.0f};
+    return seg_sum_any<DT>(seg_load<DT>(row, seg, z.V, lane), z.c);
+}
+
+// A segment's weight relative to the row's reference.
 __device__ __forceinline__ double seg_weight(const RowSum& a, float top, double c)
 {
-    return a.m == -INFINITY ? a.s : a.s * pow2_any((double)a.m - (double)top, c);
+    return a.m == top ? a.s : a.m == -INFINITY ? a.s : a.s * pow2_any((double)a.m - (double)top, c);
 }
 
 // Joins a row's segments by one wave, in every lane.
@@ -175,10 +290,23 @@ __device__ __forceinline__ RowSum row_sum(const RowSum* seg, int n, double c, in
     return {wave_sum_f64(s), top, 0.0f};
 }
 
+// log2 s for s > 0, within 2^-39: that of the fraction in 32 bits, and the logarithm
+// of the little by which its power misses the fraction.  (A fourth of the
+// instructions of log().)
+__device__ __forceinline__ double log2_of(double s)
+{
+    int whole;
+    const double x = frexp(s, &whole);  // in [1/2, 1)
+    const double l = (double)__builtin_amdgcn_logf((float)x);
+    const double d = fma(x, pow2(-l, 1.0), -1.0);  // below 2^-20
+    return (double)whole + fma(fma(d, -0.5, 1.0) * d, kLog2eD, l);
+}
+
 // log p of an entry, rounded once.
 __device__ __forceinline__ float row_logp(float x, const RowSum& r, float inv_t)
 {
-    return (float)(((double)x - (double)r.m) * (double)inv_t - log(r.s));
+    constexpr double ln2 = 0.69314718055994530942;
+    return (float)fma(-ln2, log2_of(r.s), ((double)x - (double)r.m) * (double)inv_t);
 }
 
 // -- the choice of an entry --------------------------------------------------
@@ -233,42 +361,109 @@ __device__ __forceinline__ Place pick_weight(F weight, int n, double target, int
     return last;
 }
 
-// The same over the entries of a segment: value(j) of entry j, asked for below V
-// only.  Entries are taken vector by vector, so that their order is the row's.
-// -1 where none has weight, or there is no segment.
+// Of E neighbouring entries a lane, whose sums are `own` and whose inclusive sums
+// over the lanes are `sum`: the number of the first whose inclusive sum from `run`
+// on passes `target`, wave-uniform, -1: none.  `last` becomes the number of the last
+// that has weight, if there is one.  Weights up to `none` count as 0.
+template <int E>
+__device__ __forceinline__ int pick_scanned(const double (&v)[E], double own, double sum, double run, double target, int lane,
+                                            int& last, double none = 0.0)
+{
+    double r = run + (sum - own);
+    int first = -1, mine = -1;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        r += v[j];
+        if (v[j] > none) {
+            mine = lane * E + j;
+            if (first < 0 && r > target) first = mine;
+        }
+    }
+    if (first < 0 && run + sum > target) first = mine;  // (between the two orders of summation)
+    const uint64_t past = __ballot(first >= 0), some = __ballot(mine >= 0);
+    if (some) last = __builtin_amdgcn_readlane(mine, 63 - __builtin_clzll(some));
+    return past ? __builtin_amdgcn_readlane(first, __builtin_ctzll(past)) : -1;
+}
+
+// A lane's entries of vector k of a segment as `value(x, at)` weighs them, 0 behind the row.
 template <int DT, class F>
-__device__ __forceinline__ int pick_entry(F value, int seg, int V, double base, double target, int lane)
+__device__ __forceinline__ void entry_values(const typename Elem<DT>::T* row, int at, int V, F value, double (&v)[kVec<DT>])
 {
     constexpr int E = kVec<DT>;
-    double run = base;
+    if (at + E <= V) {
+        const VecU<DT> x = *(const VecU<DT>*)(row + at);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = value((float)x[j], at + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = at + j < V ? value((float)row[at + j], at + j) : 0.0;
+    }
+}
+
+// The entry of a segment whose inclusive sum, from `base` on, passes `target`, or
+// the last with weight where rounding leaves none; -1 where none has weight, or
+// there is no segment.  By one wave, vector by vector, in the row's order.
+template <int DT, class F>
+__device__ __forceinline__ int pick_entry(const typename Elem<DT>::T* row, F value, Place p, int V, double target, int lane)
+{
+    constexpr int E = kVec<DT>;
     int last = -1;
 #pragma unroll 1
-    for (int k = seg < 0 ? kSegU : 0; k < kSegU; ++k) {
-        const int at = seg * kSeg<DT> + (k * 64 + lane) * E;
-        double v[E], own = 0.0;
+    for (int k = p.i < 0 ? kSegU : 0; k < kSegU; ++k) {
+        const int first = p.i * kSeg<DT> + k * 64 * E;
+        double v[E];
+        entry_values<DT>(row, first + lane * E, V, value, v);
+        double own = 0.0;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            v[j] = at + j < V ? value(at + j) : 0.0;
-            own += v[j];
-        }
+        for (int j = 0; j < E; ++j) own += v[j];
         const double sum = wave_scan_f64(own);
-        double r = run + (sum - own);
-        int first = -1;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            r += v[j];
-            if (v[j] > 0.0) {
-                last = at + j;
-                if (first < 0 && r > target) first = at + j;
-            }
-        }
-        if (own > 0.0 && first < 0 && run + sum > target) first = last;
-        const uint64_t past = __ballot(first >= 0);
-        if (past) return __builtin_amdgcn_readlane(first, __builtin_ctzll(past));
-        run += lane_f64(sum, 63);
+        int some = -1;
+        const int hit = pick_scanned<E>(v, own, sum, p.base, target, lane, some);
+        p.base += lane_f64(sum, 63);
+        if (hit >= 0) return first + hit;
+        if (some >= 0) last = first + some;
     }
-    for (int off = 32; off > 0; off >>= 1) last = max(last, __shfl_xor(last, off, 64));
     return last;
+}
+
+// The same by the first kSegU waves of a workgroup, a vector each, in every lane;
+// every wave of it takes part.
+struct PickShared {
+    double sum[kSegU];
+    int hit[kSegU], last[kSegU];
+};
+template <int DT, class F>
+__device__ __forceinline__ int pick_entry_group(const typename Elem<DT>::T* row, F value, Place p, int V, double target,
+                                                PickShared& shared)
+{
+    constexpr int E = kVec<DT>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool works = wave < kSegU && p.i >= 0;
+    const int first = p.i * kSeg<DT> + wave * 64 * E;
+    double v[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = 0.0;
+    if (works) entry_values<DT>(row, first + lane * E, V, value, v);
+    double own = 0.0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) own += v[j];
+    const double sum = wave_scan_f64(own);
+    __syncthreads();  // a former choice is read
+    if (lane == 63 && wave < kSegU) shared.sum[wave] = sum;
+    __syncthreads();
+    double run = p.base;
+    for (int w = 0; w < wave && w < kSegU; ++w) run += shared.sum[w];
+    int last = -1;
+    const int hit = pick_scanned<E>(v, own, sum, run, target, lane, last);
+    if (lane == 0 && wave < kSegU) {
+        shared.hit[wave] = hit < 0 ? -1 : first + hit;
+        shared.last[wave] = last < 0 ? -1 : first + last;
+    }
+    __syncthreads();
+    int t = -1;
+    for (int w = 0; w < kSegU; ++w) t = shared.last[w] >= 0 ? shared.last[w] : t;
+    for (int w = kSegU - 1; w >= 0; --w) t = shared.hit[w] >= 0 ? shared.hit[w] : t;
+    return t;
 }
 
 }  // namespace sfk

@@ -3,8 +3,9 @@ and Python's whole numbers, with the error that each operator's last steps may
 leave.  They share no code with the kernels or the binding.
 
 Tokens are held to the definition's, but where the uniform number lies within
-MARGIN of a border between two: the kernels' powers of two are within 2^-45, sums
-of them within 2^-45 of the sum plus 2^-53 for each addition on the longest path.
+MARGIN of a border between two: the kernels' powers of two are within 2^-39.7,
+sums of them as near, plus 2^-53 for each addition on the longest path, and a
+place in the cumulative sums is a quotient of two of them: 2^-38.7 in all.
 """
 import math
 
@@ -13,8 +14,10 @@ import numpy as np
 U = 2.0 ** -24
 HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
 TINY = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133, "f16": 2.0 ** -25}
-MARGIN = 2.0 ** -42
+MARGIN = 2.0 ** -38
 LEAST = 2.0 ** -30
+TINIEST = np.longdouble(2.0) ** -700
+LOST = "p and q of a draft are both too small to tell"
 WORD = (1 << 32) - 1
 
 
@@ -61,8 +64,7 @@ def dropout(x, keep, p, residual, kind):
 
 
 def softmax(x, inv_t):
-    """p in extended precision, 0 below 2^-1000 of the largest; None for nothing
-    but -inf, NaN where +inf or NaN is."""
+    """p in extended precision; None for nothing but -inf, NaN where +inf or NaN is."""
     x = np.asarray(x, np.float64)
     if not (x < np.inf).all():
         return np.nan
@@ -71,7 +73,6 @@ def softmax(x, inv_t):
     # products of a float and a float are exact in 64 bits
     z = (x * float(np.float32(inv_t))).astype(np.longdouble)
     e = np.exp(z - z.max())
-    e[e < np.longdouble(2.0) ** -1000] = 0
     return e / e.sum()
 
 
@@ -103,7 +104,7 @@ def sample(x, u, inv_t):
 
 def logp_bound(want):
     """One rounding, and the 64-bit steps before it."""
-    return U * abs(want) + 2.0 ** -40 * (1 + abs(want)) if math.isfinite(want) else 0.0
+    return U * abs(want) + 2.0 ** -38 * (1 + abs(want)) if math.isfinite(want) else 0.0
 
 
 def verify(target, drafts, draft, u, inv_t, draft_inv_t):
@@ -133,6 +134,9 @@ def verify(target, drafts, draft, u, inv_t, draft_inv_t):
                     return k, {-1}, lambda t: math.nan, logps
                 if q is None:
                     q = np.zeros(V, np.longdouble)
+            # (what lies below 2^-700 of a row's largest may count as 0)
+            if p[d] < TINIEST * p.max() and (u[k] == 0.0 or q[d] < TINIEST * max(q.max(), p.max())):
+                return LOST
             if p[d] > 0 and abs(u[k] * q[d] - p[d]) < MARGIN * p[d]:
                 return None
             if u[k] * q[d] < p[d]:
@@ -141,10 +145,10 @@ def verify(target, drafts, draft, u, inv_t, draft_inv_t):
             weights = np.maximum(p - q, 0)
         if not 0.0 <= u[n] < 1.0:
             return k, {-1}, lambda t: 0.0, logps
-        # what p and q leave of each other is only as good as they are: p and q are within 2^-44 of their
-        # size, so cumulative sums of the differences within 2^-43 in all, relative to the share that is left
+        # what p and q leave of each other is only as good as they are: each is within 2^-38.7 of its size,
+        # so cumulative sums of the differences within 2^-37.7, relative to the share that is left
         share = float(weights.sum())
         if share < LEAST:
             weights, share = p, 1.0
-        t, near = pick(weights, u[n], MARGIN / share)
+        t, near = pick(weights, u[n], 2 * MARGIN / share)
         return k, near, lambda t: log_p(p[t]), logps
