@@ -7,6 +7,7 @@
 namespace sfk {
 
 constexpr int kDrawWG = 256;
+constexpr int64_t kLastCache = 256 << 20;  // bytes that the chip's last cache holds
 
 // One block of four numbers a lane and turn.
 __global__ __launch_bounds__(kDrawWG) void k_uniform(const int64_t* __restrict__ key, uint32_t site, int64_t first,
@@ -40,9 +41,16 @@ struct DropShape {
 template <int DT>
 using Eight = typename Elem<DT>::T __attribute__((ext_vector_type(8), aligned(sizeof(typename Elem<DT>::T))));
 
+template <bool FAR, class V>
+__device__ __forceinline__ V load_eight(const V* p)
+{
+    if (FAR) return __builtin_nontemporal_load(p);
+    return *p;
+}
+
 // A lane takes the eight entries of one block of the generator, whose place in
 // the row depends on the row's first index.
-template <int XT, int OT>
+template <int XT, int OT, bool FAR>
 __global__ __launch_bounds__(kDrawWG) void k_dropout(const typename Elem<XT>::T* x, const int64_t* __restrict__ key,
                                                      const typename Elem<OT>::T* residual, typename Elem<OT>::T* out,
                                                      DropShape p)
@@ -61,8 +69,8 @@ __global__ __launch_bounds__(kDrawWG) void k_dropout(const typename Elem<XT>::T*
             Eight<XT> v;
             Eight<OT> w;
             if (whole) {
-                v = *(const Eight<XT>*)(xr + at);
-                if (residual) w = *(const Eight<OT>*)(rr + at);
+                v = load_eight<FAR>((const Eight<XT>*)(xr + at));
+                if (residual) w = load_eight<FAR>((const Eight<OT>*)(rr + at));
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -80,7 +88,10 @@ __global__ __launch_bounds__(kDrawWG) void k_dropout(const typename Elem<XT>::T*
                 w[j] = (O)(residual ? fmaf(xv, s, (float)w[j]) : xv * s);
             }
             if (whole) {
-                *(Eight<OT>*)(o + at) = w;
+                if (FAR)
+                    __builtin_nontemporal_store(w, (Eight<OT>*)(o + at));
+                else
+                    *(Eight<OT>*)(o + at) = w;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -149,15 +160,17 @@ SF_API int sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t C, int64_
     }
     a.threshold = (uint32_t)(p * 65536.0 + 0.5);
     a.scale = a.threshold < 65536 ? (float)(65536.0 / (65536 - (int)a.threshold)) : 0.0f;
+    const bool far = a.N * a.C * (xb + (residual ? 2 : 1) * ob) > kLastCache;
     const int64_t blocks = a.C / 8 + 2;  // a row's, at most
     if (a.N > 1)
         while (a.lanes > 1 && a.lanes / 2 >= blocks) a.lanes /= 2;
     const int64_t across = (blocks + a.lanes - 1) / a.lanes, down = (a.N * a.lanes + kDrawWG - 1) / kDrawWG;
     void* args[] = {(void*)&x, (void*)&key, (void*)&residual, (void*)&out, (void*)&a};
-    const void* fn[3][3] = {
-        {(const void*)&k_dropout<SF_F32, SF_F32>, (const void*)&k_dropout<SF_F32, SF_BF16>, (const void*)&k_dropout<SF_F32, SF_F16>},
-        {(const void*)&k_dropout<SF_BF16, SF_F32>, (const void*)&k_dropout<SF_BF16, SF_BF16>, (const void*)&k_dropout<SF_BF16, SF_F16>},
-        {(const void*)&k_dropout<SF_F16, SF_F32>, (const void*)&k_dropout<SF_F16, SF_BF16>, (const void*)&k_dropout<SF_F16, SF_F16>}};
-    return launch(fn[dtype][out_dtype], dim3((unsigned)(across < (1 << 20) ? across : 1 << 20), (unsigned)(down < 65535 ? down : 65535)),
+#define SF_DROPOUT(X, O) {(const void*)&k_dropout<X, O, false>, (const void*)&k_dropout<X, O, true>}
+    const void* fn[3][3][2] = {{SF_DROPOUT(SF_F32, SF_F32), SF_DROPOUT(SF_F32, SF_BF16), SF_DROPOUT(SF_F32, SF_F16)},
+                               {SF_DROPOUT(SF_BF16, SF_F32), SF_DROPOUT(SF_BF16, SF_BF16), SF_DROPOUT(SF_BF16, SF_F16)},
+                               {SF_DROPOUT(SF_F16, SF_F32), SF_DROPOUT(SF_F16, SF_BF16), SF_DROPOUT(SF_F16, SF_F16)}};
+#undef SF_DROPOUT
+    return launch(fn[dtype][out_dtype][far], dim3((unsigned)(across < (1 << 20) ? across : 1 << 20), (unsigned)(down < 65535 ? down : 65535)),
                   dim3(kDrawWG), args, 0, stream);
 }

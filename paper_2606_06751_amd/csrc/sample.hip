@@ -16,6 +16,7 @@ constexpr int kRowsWG = 256;
 constexpr int kRowsWaves = kRowsWG / 64;
 static_assert(kRowsWaves == kSegU, "a wave for each vector of a segment");
 constexpr int64_t kFewSegments = 1024;
+constexpr int64_t kManySegments = 65536;
 constexpr int kLdsSegs = 1024;  // of a row that one workgroup takes
 
 __device__ __forceinline__ bool in_unit(float u) { return u >= 0.0f && u < 1.0f; }
@@ -160,45 +161,22 @@ __global__ __launch_bounds__(WG) void k_token_sample(const typename Elem<DT>::T*
     }
 }
 
-// Sums of the segments of two groups of rows (those of b behind those of a), each
-// wave `per` neighbouring segments; rows of a whose uniform number says that they
-// take no part are left out.
+// Sums of the segments of two groups of rows (those of b behind those of a), a wave
+// each; rows of a whose uniform number says that they take no part are left out.
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_row_segments(const typename Elem<DT>::T* __restrict__ a, int64_t rows_a, RowArg za,
                                                           const typename Elem<DT>::T* __restrict__ b, int64_t rows_b, RowArg zb,
-                                                          const float* __restrict__ uniform, int per, RowSum* __restrict__ out)
+                                                          const float* __restrict__ uniform, RowSum* __restrict__ out)
 {
-    typedef typename Elem<DT>::T T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int s0 = ((int)blockIdx.x * kRowsWaves + wave) * per;
-    const int s1 = min(s0 + per, za.nseg);
-    for (int64_t i = blockIdx.y; i < rows_a + rows_b; i += gridDim.y) {
-        const bool first = i < rows_a;
-        if (first && uniform && !in_unit(uniform[i])) continue;
-        const T* row = first ? a + i * za.stride : b + (i - rows_a) * zb.stride;
-        const RowArg& z = first ? za : zb;
-        for (int s = s0; s < s1; ++s) {
-            const RowSum r = seg_sum<DT>(seg_load<DT>(row, s, za.V, lane), seg_live<DT>(s, za.V), z);
-            if (lane == 0) out[i * za.nseg + s] = r;
-        }
-    }
-}
-
-// The same with a workgroup a segment: where there are few, a segment by one wave is
-// a good part of the call's time.
-template <int DT>
-__global__ __launch_bounds__(kRowsWG) void k_row_segment(const typename Elem<DT>::T* __restrict__ a, int64_t rows_a, RowArg za,
-                                                         const typename Elem<DT>::T* __restrict__ b, int64_t rows_b, RowArg zb,
-                                                         const float* __restrict__ uniform, int per, RowSum* __restrict__ out)
-{
-    __shared__ double part[kSegU][64];
-    __shared__ int above[kSegU];
+    const int g = (int)blockIdx.x * kRowsWaves + wave;
+    if (g >= za.nseg) return;
     for (int64_t i = blockIdx.y; i < rows_a + rows_b; i += gridDim.y) {
         const bool first = i < rows_a;
         if (first && uniform && !in_unit(uniform[i])) continue;
         const typename Elem<DT>::T* row = first ? a + i * za.stride : b + (i - rows_a) * zb.stride;
-        const RowSum r = seg_sum_group<DT>(row, blockIdx.x, first ? za : zb, part, above);
-        if (threadIdx.x == 0) out[i * za.nseg + blockIdx.x] = r;
+        const RowSum r = seg_sum<DT>(seg_load<DT>(row, g, za.V, lane), seg_live<DT>(g, za.V), first ? za : zb);
+        if (lane == 0) out[i * za.nseg + g] = r;
     }
 }
 
@@ -206,14 +184,10 @@ template <int DT>
 static int sum_segments(const void* a, int64_t rows_a, RowArg za, const void* b, int64_t rows_b, RowArg zb,
                         const float* uniform, RowSum* out, sf_stream_t stream)
 {
-    const int64_t rows = rows_a + rows_b, all = rows * za.nseg;
-    int per = (int)(all < 16384 ? 1 : all > 16 * 16384 ? 16 : all / 16384);
-    void* args[] = {(void*)&a,  (void*)&rows_a,  (void*)&za,  (void*)&b,  (void*)&rows_b,
-                    (void*)&zb, (void*)&uniform, (void*)&per, (void*)&out};
-    const bool few = all <= kFewSegments;
-    const int64_t each = few ? 1 : (int64_t)kRowsWaves * per;
-    return launch(few ? (const void*)&k_row_segment<DT> : (const void*)&k_row_segments<DT>,
-                  dim3((unsigned)((za.nseg + each - 1) / each), (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
+    const int64_t rows = rows_a + rows_b;
+    void* args[] = {(void*)&a, (void*)&rows_a, (void*)&za, (void*)&b, (void*)&rows_b, (void*)&zb, (void*)&uniform, (void*)&out};
+    return launch((const void*)&k_row_segments<DT>,
+                  dim3((za.nseg + kRowsWaves - 1) / kRowsWaves, (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
                   stream);
 }
 
@@ -323,19 +297,39 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     return v;
 }
 
-// max(p - q, 0) of an entry.
+// max(p - q, 0) of entries.  Of two rows of ordinary logits powers are taken as they
+// are; what is held at 2^-1000 counts in no sum.
 struct Residual {
-    double mp, mq, cp, cq, p_of, q_of;
+    RowArg z, zq;
+    double mp, mq, p_of, q_of;
+    bool plain;
     __device__ Residual(const Verdict& v, const RowArg& z, const RowArg& zq)
-        : mp(v.p.m), mq(v.q.m), cp(z.c), cq(zq.c), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s)
+        : z(z), zq(zq), mp(v.p.m), mq(v.q.m), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s), plain(v.p.m == 0.0f && v.q.m == 0.0f)
     {
     }
+    __device__ __forceinline__ double left(double p, double q) const { return fmax(fma(p, p_of, -(q * q_of)), 0.0); }
     __device__ __forceinline__ double operator()(float xp, float xq) const
     {
-#pragma clang fp contract(off)  // equal rows leave nothing
-        const double p = pow2_any((double)xp - mp, cp) * p_of;
-        const double q = pow2_any((double)xq - mq, cq) * q_of;
-        return p > q ? p - q : 0.0;
+        return left(pow2_any((double)xp - mp, z.c), pow2_any((double)xq - mq, zq.c));
+    }
+    template <int DT>
+    __device__ __forceinline__ double sum(const VecU<DT>& x, const VecU<DT>& y) const
+    {
+        double s = 0.0;
+        if (plain) {
+#pragma unroll
+            for (int j = 0; j < kVec<DT>; ++j) s += left(pow2_held((float)x[j], z), pow2_held((float)y[j], zq));
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < kVec<DT>; ++j) s += (*this)((float)x[j], (float)y[j]);
+        }
+        return s;
+    }
+    // of a segment, from its lanes' sums
+    __device__ __forceinline__ double segment(double s) const
+    {
+        s = wave_sum_f64(s);
+        return s > 0x1p-900 ? s : 0.0;
     }
 };
 
@@ -379,9 +373,7 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
     } else if (v.what == ROW_OTHER) {
         const int d = (int)o.draft, gd = d / kSeg<DT>;
         auto value = [&](float x, int j) { return j == d ? 0.0 : pow2_any((double)x - (double)v.p.m, a.z.c); };
-        double own = 0.0;
-        for (int j = gd * kSeg<DT> + lane; j < a.z.V && j < (gd + 1) * kSeg<DT>; j += 64) own += value((float)xp[j], j);
-        own = wave_sum_f64(own);
+        const double own = entry_sum_group<DT>(xp, value, gd, a.z.V, shared);
         auto weight = [&](int g) { return g == gd ? own : seg_weight(seg[g], v.p.m, a.z.c); };
         double total = 0.0;
         for (int g = lane; g < a.z.nseg; g += 64) total += weight(g);
@@ -402,90 +394,163 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
 constexpr int kVerifyWG = 512;
 constexpr int kVerifyWaves = kVerifyWG / 64;
 
-// A workgroup takes a sequence, or part blockIdx.x of its residual's sums: the
-// drafts eight at a time (every part the same), then segments of the residual.
-// With one part it draws the token, too.
-template <int DT, bool FEW>
-__global__ __launch_bounds__(kVerifyWG) void k_draft_verify(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
+// Where sequence b ends, found by a workgroup: its rows eight at a time.  One of the
+// workgroups that do the same (`writes`) writes what is accepted.
+template <int DT>
+__device__ __forceinline__ Outcome judge(const VerifyArg<DT>& a, int64_t b, Verdict (&row)[kVerifyWaves], bool writes)
 {
-    typedef typename Elem<DT>::T T;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
+    int64_t end;
+    for (int64_t k0 = 0;; k0 += kVerifyWaves) {
+        const int64_t k = k0 + wave;
+        Verdict v = {};
+        v.what = ROW_PLAIN;
+        if (k <= n) v = row_verdict<DT>(a, b, s, n, k, lane);
+        __syncthreads();  // former ones are read
+        if (lane == 0) row[wave] = v;
+        __syncthreads();
+        int w = 0;
+        while (w < kVerifyWaves && row[w].what == ROW_ACCEPT) ++w;
+        if (writes && wave < w && lane == 0) {
+            a.token[s + b + k] = a.draft[s + k];
+            a.logp[s + b + k] = v.logp;
+        }
+        end = k0 + w;
+        if (w < kVerifyWaves) break;  // row n at the latest
+    }
+    Outcome o;
+    o.v = row[end % kVerifyWaves];
+    o.at = s + b + end;
+    o.last = s + b + n;
+    o.draft = end < n ? a.draft[s + end] : -1;
+    if (writes) {
+        if (threadIdx.x == 0) a.accepted[b] = end;
+        for (int64_t k = end + 1 + threadIdx.x; k <= n; k += kVerifyWG) {
+            a.token[s + b + k] = -1;
+            a.logp[s + b + k] = 0.0f;
+        }
+    }
+    return o;
+}
+
+// Whether the first k1 drafts of sequences are accepted, a workgroup each.
+template <int DT>
+__global__ __launch_bounds__(kRowsWG) void k_draft_alive(VerifyArg<DT> a, int64_t k1, Outcome* __restrict__ outcomes)
+{
+    __shared__ int what[kRowsWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
+        bool alive = n >= k1;
+        for (int64_t k = wave; alive && k - wave < k1; k += kRowsWaves) {
+            const int is = k < k1 ? row_verdict<DT>(a, b, s, n, k, lane).what : ROW_ACCEPT;
+            __syncthreads();  // former ones are read
+            if (lane == 0) what[wave] = is;
+            __syncthreads();
+            for (int w = 0; w < kRowsWaves; ++w) alive &= what[w] == ROW_ACCEPT;
+        }
+        if (threadIdx.x == 0) outcomes[b].v.what = alive ? ROW_ACCEPT : ROW_END;
+        __syncthreads();
+    }
+}
+
+// Sums of segments of the rows k0 .. k1 - 1 of every sequence, a wave a segment of
+// every gridDim.z-th of them.  With k0 > 0 only of sequences that are alive: rows
+// behind a refused draft are not read.
+template <int DT>
+__global__ __launch_bounds__(kRowsWG) void k_draft_segments(VerifyArg<DT> a, int64_t k0, int64_t k1,
+                                                            const Outcome* __restrict__ outcomes, RowSum* __restrict__ sums)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = (int)blockIdx.x * kRowsWaves + wave;
+    if (g >= a.z.nseg) return;
+    const int live = seg_live<DT>(g, a.z.V);
+    for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
+        if (k0 > 0 && outcomes[b].v.what != ROW_ACCEPT) continue;
+        const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
+        const int64_t end = n + 1 < k1 ? n + 1 : k1;
+        // rows of the target and the drafts in turn, by one piece of code
+        const int kinds = a.drafts ? 2 : 1;
+        for (int64_t j = kinds * k0 + blockIdx.z; j < kinds * end; j += gridDim.z) {
+            const int64_t k = kinds == 2 ? j / 2 : j;
+            const bool drafts = kinds == 2 && (j & 1);
+            if (drafts && k == n) continue;
+            const int64_t i = drafts ? s + k : s + b + k;
+            const RowArg& z = drafts ? a.zq : a.z;
+            const RowSum r = seg_sum<DT>(seg_load<DT>((drafts ? a.drafts : a.target) + i * z.stride, g, z.V, lane), live, z);
+            if (lane == 0) sums[(i + (drafts ? a.D + a.B : 0)) * z.nseg + g] = r;
+        }
+    }
+}
+
+// Judges sequences, and (DRAW) draws their last tokens where no residual's sums
+// are needed for it.
+template <int DT, bool DRAW>
+__global__ __launch_bounds__(kVerifyWG) void k_draft_judge(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
+{
     __shared__ Verdict row[kVerifyWaves];
     __shared__ PickShared shared;
-    __shared__ double part[FEW ? kVerifyWaves : 1][64];
+    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const Outcome o = judge<DT>(a, b, row, true);
+        if (DRAW)
+            draw_last<DT>(a, b, o, shared);
+        else if (threadIdx.x == 0)
+            outcomes[b] = o;
+    }
+}
+
+// Where there are few segments: judges a sequence in every workgroup of it, which
+// then takes two segments of its residual, four waves each.
+template <int DT>
+__global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
+{
+    constexpr int E = kVec<DT>;
+    __shared__ Verdict row[kVerifyWaves];
+    __shared__ double part[kVerifyWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = (int)blockIdx.x * (kVerifyWaves / kSegU) + wave / kSegU, k = wave % kSegU;
+    const int at = g * kSeg<DT> + (k * 64 + lane) * E, tail = a.z.V - a.z.V % E + lane;
     for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
-        const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
-        int64_t end;
-        for (int64_t k0 = 0;; k0 += kVerifyWaves) {
-            const int64_t k = k0 + wave;
-            Verdict v = {};
-            v.what = ROW_PLAIN;
-            if (k <= n) v = row_verdict<DT>(a, b, s, n, k, lane);
-            if (lane == 0) row[wave] = v;
-            __syncthreads();
-            int w = 0;
-            while (w < kVerifyWaves && row[w].what == ROW_ACCEPT) ++w;
-            if (blockIdx.x == 0 && wave < w && lane == 0) {
-                a.token[s + b + k] = a.draft[s + k];
-                a.logp[s + b + k] = v.logp;
-            }
-            end = k0 + w;
-            if (w < kVerifyWaves) break;  // row n at the latest
-            __syncthreads();
-        }
-        Outcome o;
-        o.v = row[end % kVerifyWaves];
-        o.at = s + b + end;
-        o.last = s + b + n;
-        o.draft = end < n ? a.draft[s + end] : -1;
-        if (blockIdx.x == 0) {
-            if (threadIdx.x == 0) a.accepted[b] = end;
-            for (int64_t k = end + 1 + threadIdx.x; k <= n; k += kVerifyWG) {
-                a.token[s + b + k] = -1;
-                a.logp[s + b + k] = 0.0f;
-            }
-            if (gridDim.x > 1 && threadIdx.x == 0) outcomes[b] = o;
-        }
-        if (o.v.what == ROW_RESIDUAL) {
-            const T* xp = a.target + o.at * a.z.stride;
-            const T* xq = a.drafts + (s + end) * a.zq.stride;
-            const Residual residual(o.v, a.z, a.zq);
-            // a segment by four waves, added in the order of one wave's
-            if (FEW) {
-                const int g = (int)blockIdx.x * 2 + wave / kSegU, k = wave % kSegU;
-                const int at = g * kSeg<DT> + (k * 64 + lane) * kVec<DT>, tail = a.z.V - a.z.V % kVec<DT> + lane;
-                double sum = 0.0;
-                if (at + kVec<DT> <= a.z.V) {
-                    const VecU<DT> x = *(const VecU<DT>*)(xp + at), y = *(const VecU<DT>*)(xq + at);
-#pragma unroll
-                    for (int j = 0; j < kVec<DT>; ++j) sum += residual((float)x[j], (float)y[j]);
-                }
-                part[wave][lane] = sum;
-                __syncthreads();
-                if (k == 0 && g < a.z.nseg) {
-                    sum = g == a.z.nseg - 1 && tail < a.z.V ? residual((float)xp[tail], (float)xq[tail]) : 0.0;
-                    for (int i = 0; i < kSegU; ++i) sum += part[wave + i][lane];
-                    sum = wave_sum_f64(sum);
-                    if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
-                }
-            }
-            for (int g = FEW ? a.z.nseg : (int)blockIdx.x * kVerifyWaves + wave; g < a.z.nseg; g += (int)gridDim.x * kVerifyWaves) {
-                const SegData<DT> x = seg_load<DT>(xp, g, a.z.V, lane), y = seg_load<DT>(xq, g, a.z.V, lane);
-                double sum = residual(x.edge, y.edge);
-#pragma unroll
-                for (int k = 0; k < kSegU; ++k) {
-                    double own = 0.0;
-#pragma unroll
-                    for (int j = 0; j < kVec<DT>; ++j) own += residual((float)x.y[k][j], (float)y.y[k][j]);
-                    sum += own;
-                }
-                sum = wave_sum_f64(sum);
-                if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
-            }
-        }
+        const Outcome o = judge<DT>(a, b, row, blockIdx.x == 0);
+        if (blockIdx.x == 0 && threadIdx.x == 0) outcomes[b] = o;
+        if (o.v.what != ROW_RESIDUAL) continue;
+        const typename Elem<DT>::T* xp = a.target + o.at * a.z.stride;
+        const typename Elem<DT>::T* xq = a.drafts + (o.at - b) * a.zq.stride;
+        const Residual residual(o.v, a.z, a.zq);
+        double sum = 0.0;
+        if (at + E <= a.z.V) sum = residual.template sum<DT>(*(const VecU<DT>*)(xp + at), *(const VecU<DT>*)(xq + at));
+        part[wave][lane] = sum;  // (a former sequence's are read: judge waits)
         __syncthreads();
-        if (gridDim.x == 1) draw_last<DT>(a, b, o, shared);
-        __syncthreads();
+        if (k == 0 && g < a.z.nseg) {
+            sum = g == a.z.nseg - 1 && tail < a.z.V ? residual((float)xp[tail], (float)xq[tail]) : 0.0;
+            for (int i = 0; i < kSegU; ++i) sum += part[wave + i][lane];
+            sum = residual.segment(sum);
+            if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
+        }
+    }
+}
+
+// The sums of the residuals' segments of sequences that are judged, a wave each.
+template <int DT>
+__global__ __launch_bounds__(kRowsWG) void k_draft_residual(VerifyArg<DT> a, const Outcome* __restrict__ outcomes)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = (int)blockIdx.x * kRowsWaves + wave;
+    if (g >= a.z.nseg) return;
+    for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
+        const Outcome& o = outcomes[b];
+        if (o.v.what != ROW_RESIDUAL) continue;
+        const SegData<DT> x = seg_load<DT>(a.target + o.at * a.z.stride, g, a.z.V, lane);
+        const SegData<DT> y = seg_load<DT>(a.drafts + (o.at - b) * a.zq.stride, g, a.z.V, lane);
+        const Residual residual(o.v, a.z, a.zq);
+        double sum = __any(x.edge != -INFINITY) ? residual(x.edge, y.edge) : 0.0;
+        const int live = seg_live<DT>(g, a.z.V);
+#pragma unroll
+        for (int k = 0; k < kSegU; ++k)
+            if (k < live) sum += residual.template sum<DT>(x.y[k], y.y[k]);
+        sum = residual.segment(sum);
+        if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
     }
 }
 
@@ -621,21 +686,42 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     RowSum* sums = (RowSum*)ws;
     double* residual = (double*)(ws + verify_sums(D, B, z.nseg));
     Outcome* outcomes = (Outcome*)(ws + verify_sums(D, B, z.nseg) + verify_residuals(B, z.nseg));
-    int64_t rows = D + B, more = drafts ? D : 0;
-    int rc = sum_segments<DT>(target, rows, z, drafts, more, zq, nullptr, sums, stream);
-    if (rc != SF_OK) return rc;
+    const int64_t rows = D + B, more = drafts ? D : 0;
     VerifyArg<DT> a = {(const T*)target, (const T*)drafts, draft, start, uniform, D, B, z, zq, sums, residual, accepted, token, logp};
-    // Parts of a residual: two segments each where there are few, else about 1024
-    // workgroups in all.
-    const bool few = drafts && B * z.nseg <= kFewSegments;
-    const int64_t most = (z.nseg + kVerifyWaves - 1) / kVerifyWaves, want = 1024 / B;
-    const int64_t parts = few ? (z.nseg + 1) / 2 : !drafts || want < 2 ? 1 : most < want ? most : want;
+    int rc;
+    if (D >= 2 * B && (rows + more) * z.nseg > (drafts ? kManySegments : kManySegments / 4)) {
+        // the first rows, then those behind accepted drafts
+        int64_t k0 = 0, k1 = drafts ? 1 + D / B / 3 : 1, all = (int64_t)1 << 31;
+        const int64_t kinds = drafts ? 2 : 1, rest = kinds * (D / B - k1 + 1);
+        void* first[] = {(void*)&a, (void*)&k0, (void*)&k1, (void*)&outcomes, (void*)&sums};
+        void* alive[] = {(void*)&a, (void*)&k1, (void*)&outcomes};
+        void* others[] = {(void*)&a, (void*)&k1, (void*)&all, (void*)&outcomes, (void*)&sums};
+        const unsigned gx = (z.nseg + kRowsWaves - 1) / kRowsWaves, gy = up_to(B, 65535);
+        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, (unsigned)(kinds * k1 < 64 ? kinds * k1 : 64)), dim3(kRowsWG), first, 0, stream);
+        if (rc != SF_OK) return rc;
+        rc = launch((const void*)&k_draft_alive<DT>, dim3(up_to(B, 1 << 21)), dim3(kRowsWG), alive, 0, stream);
+        if (rc != SF_OK) return rc;
+        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, (unsigned)(rest < 6 ? rest : 6)), dim3(kRowsWG), others, 0, stream);
+    } else {
+        rc = sum_segments<DT>(target, rows, z, drafts, more, zq, nullptr, sums, stream);
+    }
+    if (rc != SF_OK) return rc;
     void* args[] = {(void*)&a, (void*)&outcomes};
-    rc = launch(few ? (const void*)&k_draft_verify<DT, true> : (const void*)&k_draft_verify<DT, false>,
-                dim3((unsigned)parts, up_to(B, 65535)), dim3(kVerifyWG), args, 0, stream);
-    if (rc != SF_OK || parts == 1) return rc;
-    return launch((const void*)&k_draft_draw<DT>, dim3(up_to(B, 1 << 21)), dim3(kRowsWG), args,
-                  0, stream);
+    const dim3 draws(up_to(B, 1 << 21));
+    if (!drafts)
+        return launch((const void*)&k_draft_judge<DT, true>, draws, dim3(kVerifyWG), args, 0, stream);
+    if (B * z.nseg <= kFewSegments) {
+        constexpr int each = kVerifyWaves / kSegU;
+        rc = launch((const void*)&k_draft_few<DT>, dim3((z.nseg + each - 1) / each, up_to(B, 65535)), dim3(kVerifyWG), args, 0,
+                    stream);
+    } else {
+        rc = launch((const void*)&k_draft_judge<DT, false>, draws, dim3(kVerifyWG), args, 0, stream);
+        if (rc != SF_OK) return rc;
+        rc = launch((const void*)&k_draft_residual<DT>, dim3((z.nseg + kRowsWaves - 1) / kRowsWaves, up_to(B, 65535)),
+                    dim3(kRowsWG), args, 0, stream);
+    }
+    if (rc != SF_OK) return rc;
+    return launch((const void*)&k_draft_draw<DT>, draws, dim3(kRowsWG), args, 0, stream);
 }
 
 }  // namespace sfk

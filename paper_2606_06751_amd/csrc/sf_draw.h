@@ -201,11 +201,6 @@ __device__ __forceinline__ bool bits_above(const VecBits<DT>& top, float limit)
     for (int j = 0; j < kVec<DT>; ++j) above |= top[j] >= bits;
     return above;
 }
-template <int DT>
-__device__ __forceinline__ bool vector_above(const VecU<DT>& y, float limit)
-{
-    return bits_above<DT>(__builtin_bit_cast(VecBits<DT>, y), limit);
-}
 // Whether an entry of the lane lies at or above a positive limit.
 template <int DT>
 __device__ __forceinline__ bool seg_above(const SegData<DT>& a, float limit)
@@ -236,41 +231,6 @@ __device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, int live, const 
     s = wave_sum_f64(s);
     if (!above && sum_is_ordinary(s)) return {s, 0.0f, 0.0f};
     return seg_sum_any<DT>(a, z.c);
-}
-
-// The same by four waves of a workgroup, a vector each, whose sums meet in `part`
-// lane by lane: the same additions in the same order.  Wave-uniform in the first
-// wave only; every wave of the workgroup takes part.
-template <int DT>
-__device__ __forceinline__ RowSum seg_sum_group(const typename Elem<DT>::T* row, int seg, const RowArg& z, double (&part)[kSegU][64],
-                                                int (&above)[kSegU])
-{
-    typedef typename Elem<DT>::T T;
-    constexpr int E = kVec<DT>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int at = seg * kSeg<DT> + (wave * 64 + lane) * E;
-    VecU<DT> y = (VecU<DT>)(T)-INFINITY;
-    if (at + E <= z.V) y = *(const VecU<DT>*)(row + at);
-    const int tail = z.V - z.V % E + lane;
-    float edge = -INFINITY;
-    if (wave == 0 && tail < z.V && tail < (seg + 1) * kSeg<DT>) edge = (float)row[tail];
-    const bool high = __any(vector_above<DT>(y, z.top) || !(edge < z.top));
-    __syncthreads();  // a former segment's are read
-    part[wave][lane] = vector_sum<DT>(y, z);
-    if (lane == 0) above[wave] = high;
-    __syncthreads();
-    if (wave != 0) return {};
-    const int live = seg_live<DT>(seg, z.V);
-    double s = 0.0;
-    bool any = false;
-    for (int k = 0; k < kSegU; ++k) {
-        any |= above[k] != 0;
-        if (k < live) s += part[k][lane];
-    }
-    if (__any(edge != -INFINITY)) s += pow2_held(edge, z);
-    s = wave_sum_f64(s);
-    if (!any && sum_is_ordinary(s)) return {s, 0.0f, 0.0f};
-    return seg_sum_any<DT>(seg_load<DT>(row, seg, z.V, lane), z.c);
 }
 
 // A segment's weight relative to the row's reference.
@@ -432,6 +392,27 @@ struct PickShared {
     double sum[kSegU];
     int hit[kSegU], last[kSegU];
 };
+// The sum of a segment's values by the first kSegU waves, in every lane.
+template <int DT, class F>
+__device__ __forceinline__ double entry_sum_group(const typename Elem<DT>::T* row, F value, int seg, int V, PickShared& shared)
+{
+    constexpr int E = kVec<DT>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    double v[E], own = 0.0;
+    if (wave < kSegU) {
+        entry_values<DT>(row, seg * kSeg<DT> + (wave * 64 + lane) * E, V, value, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) own += v[j];
+    }
+    own = wave_sum_f64(own);
+    __syncthreads();  // former sums are read
+    if (lane == 0 && wave < kSegU) shared.sum[wave] = own;
+    __syncthreads();
+    own = 0.0;
+    for (int w = 0; w < kSegU; ++w) own += shared.sum[w];
+    return own;
+}
+
 template <int DT, class F>
 __device__ __forceinline__ int pick_entry_group(const typename Elem<DT>::T* row, F value, Place p, int V, double target,
                                                 PickShared& shared)

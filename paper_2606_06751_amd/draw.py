@@ -23,7 +23,7 @@ import ctypes
 import torch
 
 from .stagefrontier import SF_OK, StageFrontierError, _check, _lib, _new, _stream_handle
-from .train import _DTYPES, _out, _rows, _space, _wrote
+from .train import _DTYPES, _out, _space, _wrote
 
 
 def _declare(lib):
@@ -71,8 +71,16 @@ def sf_uniform(n: int, key: torch.Tensor, site: int = 0, first: int = 0, out: to
 
 
 def _matrix(t: torch.Tensor, name: str, shape=None, like: torch.Tensor | None = None) -> int:
-    """Checks rows of entries (a matrix, or a vector as one row) and returns
-    their stride."""
+    """Checks rows of entries and returns their stride.  (As in ``_check``, the
+    good path is one chained test.)"""
+    try:
+        if (t.dtype in _DTYPES and t.is_cuda and t.dim() == 2 and (shape is None or t.shape == shape)
+                and (like is None or t.get_device() == like.get_device())):
+            (N, C), (down, across) = t.shape, t.stride()
+            if (across == 1 or C <= 1) and (down >= C or N <= 1):
+                return down if N > 1 else C
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
         raise TypeError("%s must be a float32, bfloat16 or float16 torch.Tensor" % name)
     if not t.is_cuda:
@@ -83,12 +91,9 @@ def _matrix(t: torch.Tensor, name: str, shape=None, like: torch.Tensor | None = 
         raise ValueError("%s is on %s, the call's other arrays on %s" % (name, t.device, like.device))
     if t.dim() != 2:
         raise ValueError("%s must be [N, C]" % name)
-    N, C = t.shape
-    if C > 1 and t.stride(1) != 1:
+    if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError("%s must have its rows' entries next to each other" % name)
-    if N > 1 and t.stride(0) < C:
-        raise ValueError("%s must have rows that do not overlap" % name)
-    return t.stride(0) if N > 1 else C
+    raise ValueError("%s must have rows that do not overlap" % name)
 
 
 def sf_dropout(x: torch.Tensor, p: float, key: torch.Tensor, site: int = 0, first: int = 0,
@@ -111,12 +116,12 @@ def sf_dropout(x: torch.Tensor, p: float, key: torch.Tensor, site: int = 0, firs
         kind = out.dtype
         if out_dtype is not None and kind is not out_dtype:
             raise TypeError("out must be a %s torch.Tensor" % out_dtype)
+        out_stride = _matrix(out, "out", x.shape, x)
     else:
         kind = out_dtype or (x.dtype if residual is None else residual.dtype)
         if kind not in _DTYPES:
             raise TypeError("out_dtype must be float32, bfloat16 or float16")
-        out = _new((N, C), kind, dev, stream)
-    out_stride = _matrix(out, "out", x.shape, x)
+        out, out_stride = _new((N, C), kind, dev, stream), C
     residual_stride = C
     if residual is not None:
         residual_stride = _matrix(residual, "residual", x.shape, x)
@@ -141,11 +146,11 @@ def sf_token_sample(logits: torch.Tensor, uniform: torch.Tensor, inv_temperature
     ``uniform`` [N] float32, a row whose number lies outside [0, 1) takes no
     part.  Returns ``(out_token [N] int64, out_logp [N] float32)``.
     """
-    stride = _rows(logits, "logits")
+    stride = _matrix(logits, "logits")
     N, V = logits.shape
     dev = logits.device
     _check(uniform, "uniform", torch.float32, (N,), logits)
-    given = (out_token, out_logp)
+    given = out_token is not None or out_logp is not None
     out_token = _out(out_token, "out_token", torch.int64, (N,), logits, stream)
     out_logp = _out(out_logp, "out_logp", torch.float32, (N,), logits, stream)
     dtype = _DTYPES[logits.dtype]
@@ -157,7 +162,8 @@ def sf_token_sample(logits: torch.Tensor, uniform: torch.Tensor, inv_temperature
                               _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_token_sample")
-    _wrote(*given)
+    if given:
+        _wrote(out_token, out_logp)
     return out_token, out_logp
 
 
@@ -175,27 +181,30 @@ def sf_draft_verify(target_logits: torch.Tensor, draft_logits: torch.Tensor | No
     drafts are certain; ``uniform`` [D + B] float32.  Returns ``(out_accepted
     [B] int64, out_token [D + B] int64, out_logp [D + B] float32)``.
     """
-    stride = _rows(target_logits, "target_logits")
-    if not isinstance(draft, torch.Tensor) or not isinstance(seq_start, torch.Tensor):
-        raise TypeError("draft and seq_start must be torch.Tensors")
-    if draft.dim() != 1 or seq_start.dim() != 1 or seq_start.shape[0] < 1:
-        raise ValueError("draft must be [D] and seq_start [B + 1]")
-    D, B, V = draft.shape[0], seq_start.shape[0] - 1, target_logits.shape[1]
-    dev = target_logits.device
-    if target_logits.shape[0] != D + B:
-        raise ValueError("target_logits must have D + B = %d rows, got %d" % (D + B, target_logits.shape[0]))
+    stride = _matrix(target_logits, "target_logits")
+    try:
+        (D,), (ends,) = draft.shape, seq_start.shape
+    except AttributeError:
+        raise TypeError("draft and seq_start must be torch.Tensors") from None
+    except ValueError:
+        raise ValueError("draft must be [D] and seq_start [B + 1]") from None
+    B, (rows, V), dev = ends - 1, target_logits.shape, target_logits.device
+    if B < 0:
+        raise ValueError("seq_start must be [B + 1]")
+    if rows != D + B:
+        raise ValueError("target_logits must have D + B = %d rows, got %d" % (D + B, rows))
     draft_stride = V
     if draft_logits is not None:
-        draft_stride = _rows(draft_logits, "draft_logits")
-        if draft_logits.dtype is not target_logits.dtype or draft_logits.shape != (D, V) or draft_logits.device != dev:
-            raise ValueError("draft_logits must have the target's type and device, and [D, V] entries")
+        draft_stride = _matrix(draft_logits, "draft_logits", (D, V), target_logits)
+        if draft_logits.dtype is not target_logits.dtype:
+            raise TypeError("draft_logits must have the target's type")
     _check(draft, "draft", torch.int64, (D,), target_logits)
-    _check(seq_start, "seq_start", torch.int64, (B + 1,), target_logits)
-    _check(uniform, "uniform", torch.float32, (D + B,), target_logits)
-    given = (out_accepted, out_token, out_logp)
+    _check(seq_start, "seq_start", torch.int64, (ends,), target_logits)
+    _check(uniform, "uniform", torch.float32, (rows,), target_logits)
+    given = out_accepted is not None or out_token is not None or out_logp is not None
     out_accepted = _out(out_accepted, "out_accepted", torch.int64, (B,), target_logits, stream)
-    out_token = _out(out_token, "out_token", torch.int64, (D + B,), target_logits, stream)
-    out_logp = _out(out_logp, "out_logp", torch.float32, (D + B,), target_logits, stream)
+    out_token = _out(out_token, "out_token", torch.int64, (rows,), target_logits, stream)
+    out_logp = _out(out_logp, "out_logp", torch.float32, (rows,), target_logits, stream)
     dtype = _DTYPES[target_logits.dtype]
     need = _lib.sf_draft_verify_workspace(dtype, D, B, V)
     if need != 0:
@@ -208,5 +217,6 @@ def sf_draft_verify(target_logits: torch.Tensor, draft_logits: torch.Tensor | No
                               need, _stream_handle(stream, dev))
     if rc != SF_OK:
         raise StageFrontierError(rc, "sf_draft_verify")
-    _wrote(*given)
+    if given:
+        _wrote(out_accepted, out_token, out_logp)
     return out_accepted, out_token, out_logp

@@ -635,7 +635,7 @@ def test_binding_refusals(dr):
             (lambda: dr.sf_token_sample(x, u, out_token=torch.zeros(4, device=DEV)), TypeError),
             (lambda: dr.sf_token_sample(x, u, out_logp=u), StageFrontierError),
             (lambda: dr.sf_draft_verify(x, x[:2], d, s[:2], u), ValueError), (lambda: dr.sf_draft_verify(x[:3], x[:2], d, s, u), ValueError),
-            (lambda: dr.sf_draft_verify(x, x[:1], d, s, u), ValueError), (lambda: dr.sf_draft_verify(x, x[:2].half(), d, s, u), ValueError),
+            (lambda: dr.sf_draft_verify(x, x[:1], d, s, u), ValueError), (lambda: dr.sf_draft_verify(x, x[:2].half(), d, s, u), TypeError),
             (lambda: dr.sf_draft_verify(x, x[:2], d.int(), s, u), TypeError), (lambda: dr.sf_draft_verify(x, x[:2], d, s, u[:3]), ValueError),
             (lambda: dr.sf_draft_verify(x, x[:2], d, s, u, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV)), ValueError),
             (lambda: dr.sf_draft_verify(x, x[:2], d, s, u, draft_inv_temperature=-1.0), StageFrontierError)):
