@@ -51,6 +51,21 @@ def sf_draft_verify_workspace(dtype: torch.dtype, D: int, B: int, V: int) -> int
     return int(_lib.sf_draft_verify_workspace(_DTYPES.get(dtype, -1), D, B, V))
 
 
+_current_device = torch._C._cuda_getDevice
+
+
+def _call(fn, device, *args):
+    """The library's call, with the tensors' device as the current one: the
+    handle of a device's default stream does not name the device."""
+    if _current_device() == device.index:
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args)
+    if rc != SF_OK:
+        raise StageFrontierError(rc, fn.__name__)
+
+
 def _site(site) -> int:
     if not 0 <= site < 1 << 32:
         raise ValueError("site must lie in [0, 2^32)")
@@ -63,9 +78,8 @@ def sf_uniform(n: int, key: torch.Tensor, site: int = 0, first: int = 0, out: to
     _check(key, "key", torch.int64, (2,))
     given = out
     out = _out(out, "out", torch.float32, (n,), key, stream)
-    rc = _lib.sf_uniform(key.data_ptr(), _site(site), first, n, out.data_ptr(), _stream_handle(stream, key.device))
-    if rc != SF_OK:
-        raise StageFrontierError(rc, "sf_uniform")
+    _call(_lib.sf_uniform, key.device, key.data_ptr(), _site(site), first, n, out.data_ptr(),
+          _stream_handle(stream, key.device))
     _wrote(given)
     return out
 
@@ -127,11 +141,9 @@ def sf_dropout(x: torch.Tensor, p: float, key: torch.Tensor, site: int = 0, firs
         residual_stride = _matrix(residual, "residual", x.shape, x)
         if residual.dtype is not kind:
             raise TypeError("residual must have the output's type")
-    rc = _lib.sf_dropout(x.data_ptr(), _DTYPES[x.dtype], N, C, x_stride, p, key.data_ptr(), _site(site), first,
-                         C if index_stride is None else index_stride, None if residual is None else residual.data_ptr(),
-                         residual_stride, out.data_ptr(), _DTYPES[kind], out_stride, _stream_handle(stream, dev))
-    if rc != SF_OK:
-        raise StageFrontierError(rc, "sf_dropout")
+    _call(_lib.sf_dropout, dev, x.data_ptr(), _DTYPES[x.dtype], N, C, x_stride, p, key.data_ptr(), _site(site), first,
+          C if index_stride is None else index_stride, None if residual is None else residual.data_ptr(),
+          residual_stride, out.data_ptr(), _DTYPES[kind], out_stride, _stream_handle(stream, dev))
     _wrote(given)
     return out
 
@@ -157,11 +169,9 @@ def sf_token_sample(logits: torch.Tensor, uniform: torch.Tensor, inv_temperature
     need = _lib.sf_token_sample_workspace(dtype, N, V)
     if need != 0:
         workspace = _space(workspace, need, "sf_token_sample", logits, stream)
-    rc = _lib.sf_token_sample(logits.data_ptr(), dtype, N, V, stride, uniform.data_ptr(), inv_temperature,
-                              out_token.data_ptr(), out_logp.data_ptr(), None if need == 0 else workspace.data_ptr(), need,
-                              _stream_handle(stream, dev))
-    if rc != SF_OK:
-        raise StageFrontierError(rc, "sf_token_sample")
+    _call(_lib.sf_token_sample, dev, logits.data_ptr(), dtype, N, V, stride, uniform.data_ptr(), inv_temperature,
+          out_token.data_ptr(), out_logp.data_ptr(), None if need == 0 else workspace.data_ptr(), need,
+          _stream_handle(stream, dev))
     if given:
         _wrote(out_token, out_logp)
     return out_token, out_logp
@@ -210,13 +220,11 @@ def sf_draft_verify(target_logits: torch.Tensor, draft_logits: torch.Tensor | No
     if need != 0:
         workspace = _space(workspace, need, "sf_draft_verify", target_logits, stream)
     # without drafts there are no rows of theirs, which is not the same as certain ones, but none is looked at
-    rc = _lib.sf_draft_verify(target_logits.data_ptr(), None if draft_logits is None or D == 0 else draft_logits.data_ptr(),
-                              dtype, D, B, V, stride, draft_stride, draft.data_ptr(), seq_start.data_ptr(),
-                              uniform.data_ptr(), inv_temperature, draft_inv_temperature, out_accepted.data_ptr(),
-                              out_token.data_ptr(), out_logp.data_ptr(), None if need == 0 else workspace.data_ptr(),
-                              need, _stream_handle(stream, dev))
-    if rc != SF_OK:
-        raise StageFrontierError(rc, "sf_draft_verify")
+    _call(_lib.sf_draft_verify, dev, target_logits.data_ptr(),
+          None if draft_logits is None or D == 0 else draft_logits.data_ptr(), dtype, D, B, V, stride, draft_stride,
+          draft.data_ptr(), seq_start.data_ptr(), uniform.data_ptr(), inv_temperature, draft_inv_temperature,
+          out_accepted.data_ptr(), out_token.data_ptr(), out_logp.data_ptr(), None if need == 0 else workspace.data_ptr(),
+          need, _stream_handle(stream, dev))
     if given:
         _wrote(out_accepted, out_token, out_logp)
     return out_accepted, out_token, out_logp

@@ -256,6 +256,35 @@ def test_sample_far_temperatures(dr, kind, inv_t, scale):
     check_sample(dr, x, torch.tensor([0.0, 0.1, 0.5, 0.9, 1 - 2.0 ** -24, 0.3], device=DEV), inv_t)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [900, 9000, 70001])
+def test_sample_rows_far_from_zero(dr, kind, V):
+    """Powers beyond what a segment takes as they are, in whole rows and in parts of
+    them, on both sides of each limit."""
+    x = rows(12, V, kind, 31).float()
+    x[0] += 2000.0
+    x[1] -= 2000.0
+    x[2, : V // 2] -= 5000.0
+    x[3, V // 3] = 3000.0
+    x[4] = 650.0            # 2^938 each
+    x[5] = 620.0            # 2^894 each
+    x[6] = -130.0           # 2^-188 each
+    x[7] = -140.0           # 2^-202 each
+    x[8, V // 2:] = -INF
+    x[8, : V // 2] -= 690.0
+    x[9, 0] = 690.0         # one entry takes all
+    x[10, -1] = -700.0
+    x[11] = -693.5          # at the floor
+    x[11, V // 5] = 10.0
+    x = x.to(KINDS[kind])
+    u = torch.tensor([0.3, 0.6, 0.2, 0.9, 0.1, 0.7, 0.4, 0.8, 0.999, 0.5, 1 - 2.0 ** -24, 0.9999], device=DEV)
+    check_sample(dr, x, u, 1.0)
+    check_sample(dr, x, u, 0.25)
+    many = dr.sf_token_sample(x.repeat(50, 1), u.repeat(50))
+    one = dr.sf_token_sample(x, u)
+    assert torch.equal(many[0].view(50, 12), one[0].expand(50, 12)) and torch.equal(many[1].view(50, 12), one[1].expand(50, 12))
+
+
 def test_sample_greedy(dr):
     """The first of the largest logits at a temperature near 0 and u = 0."""
     x = rows(40, 5003, "bf16", 5)
@@ -363,6 +392,25 @@ def check_verify(dr, target, q, draft, start, u, inv_t=1.0, iq=1.0, **kw):
 def test_verify(dr, kind, lookup, counts, V, pad, shift):
     target, q, draft, start, u = batch(counts, V, kind, 11 * len(counts) + V, pad=pad, shift=shift, lookup=lookup)
     check_verify(dr, target, q, draft, start, u, float(np.float32(1 / 0.8)), float(np.float32(1 / 1.1)))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lookup", [False, True])
+@pytest.mark.parametrize("counts,V,times", [
+    ([3, 2, 4, 0, 1, 9, 5], 130, 200), ([3, 2, 4, 0, 1, 9, 5], 130, 2500), ([8, 3, 5], 2500, 150), ([8, 3, 5], 2500, 1000),
+    ([4, 4], 70003, 6), ([4, 4], 70003, 130), ([3, 1, 2], 20000, 40), ([2, 2, 2], 300, 7000)])
+def test_verify_in_large_batches(dr, kind, lookup, counts, V, times):
+    """The same sequences, few and many: sums all at once, rounds of them that leave
+    rows out, residuals by part and by segment."""
+    target, q, draft, start, u = batch(counts, V, kind, 17 * V + times, lookup=lookup, shift=1)
+    one = check_verify(dr, target, q, draft, start, u) if V < 10000 else dr.sf_draft_verify(target, q, draft, start, u)
+    n, B = int(start[-1]), len(counts)
+    starts = (start[:-1][None, :] + torch.arange(times, device=DEV)[:, None] * n).reshape(-1)
+    starts = torch.cat([starts, torch.tensor([n * times], device=DEV)])
+    many = dr.sf_draft_verify(target.repeat(times, 1), None if q is None else q.repeat(times, 1), draft.repeat(times), starts,
+                              u.repeat(times))
+    for a, b in zip(one, many):
+        assert torch.equal(b.view(times, -1), a.expand(times, -1))
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
@@ -590,6 +638,54 @@ def test_other_streams(dr):
         torch.cuda.synchronize()
         for g, w in list(zip(got, want)) + list(zip(gotv, wantv)) + list(zip(got2, want)):
             assert torch.equal(g, w)
+
+
+def test_two_graphs(dr):
+    """Two captured calls, each with the workspace of its capture, replayed in turn
+    and at once on two streams."""
+    target, q, draft, start, u = batch([4, 2, 3], 30011, "bf16", 7)
+    x, ux = rows(3, 200003, "bf16", 1), uniforms(3, 2)
+    want = list(dr.sf_draft_verify(target, q, draft, start, u)) + list(dr.sf_token_sample(x, ux))
+    torch.cuda.synchronize()
+    graphs, got = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    with torch.cuda.graph(graphs[0]):
+        got += dr.sf_draft_verify(target, q, draft, start, u)
+    with torch.cuda.graph(graphs[1]):
+        got += dr.sf_token_sample(x, ux)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(4):
+        for t in got:
+            t.fill_(-5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(a):
+            graphs[0].replay()
+        with torch.cuda.stream(b):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g, w)
+        torch.rand(1000, device=DEV).sum().item()
+
+
+def test_device_that_is_not_the_current_one(dr, monkeypatch):
+    """The tensors' device is made the current one for the call."""
+    entered = []
+
+    class Guard:
+        def __init__(self, device):
+            entered.append(device)
+
+        def __enter__(self):
+            pass
+
+        def __exit__(self, *a):
+            return False
+
+    key, x = key_of(1, 1), rows(3, 70, "f32", 1)
+    want = dr.sf_dropout(x, 0.5, key)
+    monkeypatch.setattr(dr, "_current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    assert torch.equal(dr.sf_dropout(x, 0.5, key), want) and entered == [x.device]
 
 
 def test_writes_count_as_writes(dr):
