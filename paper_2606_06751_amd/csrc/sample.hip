@@ -17,6 +17,7 @@ constexpr int kRowsWaves = kRowsWG / 64;
 static_assert(kRowsWaves == kSegU, "a wave for each vector of a segment");
 constexpr int64_t kFewSegments = 1024;
 constexpr int64_t kManySegments = 65536;
+constexpr int64_t kTableSegments = 8192;
 constexpr int kLdsSegs = 1024;  // of a row that one workgroup takes
 
 __device__ __forceinline__ bool in_unit(float u) { return u >= 0.0f && u < 1.0f; }
@@ -200,6 +201,50 @@ __global__ __launch_bounds__(kRowsWG) void k_row_segments(const typename Elem<DT
     }
 }
 
+// The sums of the segments of many bfloat16 rows, by powers from a table that each of
+// the workgroups, one a compute unit, makes once; rows as for k_row_segments, of one
+// temperature.
+__global__ __launch_bounds__(kTableWG) void k_row_table(const __bf16* __restrict__ a, uint32_t rows_a, RowArg za,
+                                                        const __bf16* __restrict__ b, uint32_t rows_b, RowArg zb, uint32_t begin,
+                                                        const float* __restrict__ uniform, RowSum* __restrict__ out)
+{
+    __shared__ double table[kTableSize];
+    table_fill(table, begin, za);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t step = gridDim.x * (kTableWG / 64), nseg = (uint32_t)za.nseg, segments = (rows_a + rows_b) * nseg;
+    for (uint32_t k = blockIdx.x * (kTableWG / 64) + wave; k < segments; k += step) {
+        const uint32_t i = k / nseg;
+        const int g = (int)(k - i * nseg);
+        if (uniform && !in_unit(uniform[i])) continue;
+        const __bf16* row = i < rows_a ? a + i * za.stride : b + (i - rows_a) * zb.stride;
+        const RowSum r = seg_sum_table(seg_load<SF_BF16>(row, g, za.V, lane), seg_live<SF_BF16>(g, za.V), za, table, begin);
+        if (lane == 0) out[k] = r;
+    }
+}
+
+// Whether rows' sums go by a table: many of bfloat16, at a temperature not too far
+// from 1.  (us by the kernels without / with it: 128 rows of 131072, 8192 segments,
+// 19.1 / 15.2; 1000 rows 84 / 55; 32 x 4 drafts of 65536, 3072 + 2048 segments, 22 / 26;
+// 128 x 4 drafts of 65536 49 / 43; 256 x 4 drafts of 131072 224 / 147.)
+static inline bool by_table(int32_t dtype, int64_t rows, const RowArg& z)
+{
+    return dtype == SF_BF16 && rows * z.nseg >= kTableSegments && rows * z.nseg < (int64_t)1 << 30 && table_begin(z.c) >= 0;
+}
+
+static int sum_by_table(const void* a, int64_t rows_a, RowArg za, const void* b, int64_t rows_b, RowArg zb, const float* uniform,
+                        RowSum* out, sf_stream_t stream)
+{
+    if (rows_b > 0 && za.c != zb.c) {  // a table each
+        const int rc = sum_by_table(a, rows_a, za, nullptr, 0, za, uniform, out, stream);
+        return rc != SF_OK ? rc : sum_by_table(b, rows_b, zb, nullptr, 0, zb, nullptr, out + rows_a * za.nseg, stream);
+    }
+    uint32_t first = (uint32_t)rows_a, others = (uint32_t)rows_b, begin = (uint32_t)table_begin(za.c);
+    int cus;
+    if (device_cus(stream, &cus) != SF_OK) return SF_EHIP;
+    void* args[] = {(void*)&a, (void*)&first, (void*)&za, (void*)&b, (void*)&others, (void*)&zb, (void*)&begin, (void*)&uniform, (void*)&out};
+    return launch((const void*)&k_row_table, dim3(cus), dim3(kTableWG), args, 0, stream);
+}
+
 // Workgroups that the segments of a row make.
 template <int DT>
 static unsigned segment_groups(const RowArg& z)
@@ -213,6 +258,8 @@ static int sum_segments(const void* a, int64_t rows_a, RowArg za, const void* b,
                         const float* uniform, RowSum* out, sf_stream_t stream)
 {
     const int64_t rows = rows_a + rows_b;
+    if (by_table(DT, rows_a, za) && (rows_b == 0 || by_table(DT, rows_b, zb)))
+        return sum_by_table(a, rows_a, za, b, rows_b, zb, uniform, out, stream);
     void* args[] = {(void*)&a, (void*)&rows_a, (void*)&za, (void*)&b, (void*)&rows_b, (void*)&zb, (void*)&uniform, (void*)&out};
     return launch((const void*)&k_row_segments<DT>,
                   dim3(segment_groups<DT>(za), (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
@@ -581,6 +628,45 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_residual(VerifyArg<DT> a, con
     }
 }
 
+// The same by a table, where both temperatures are the same.
+__global__ __launch_bounds__(kTableWG) void k_residual_table(VerifyArg<SF_BF16> a, uint32_t begin, const Outcome* __restrict__ outcomes)
+{
+    constexpr int E = kVec<SF_BF16>;
+    __shared__ double table[kTableSize];
+    table_fill(table, begin, a.z);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t step = gridDim.x * (kTableWG / 64), nseg = (uint32_t)a.z.nseg, all = (uint32_t)a.B * nseg;
+    for (uint32_t u = blockIdx.x * (kTableWG / 64) + wave; u < all; u += step) {
+        const int64_t b = u / nseg;
+        const Outcome& o = outcomes[b];
+        if (o.v.what != ROW_RESIDUAL) continue;
+        const int g = (int)(u - (uint32_t)b * nseg), live = seg_live<SF_BF16>(g, a.z.V);
+        const SegData<SF_BF16> x = seg_load<SF_BF16>(a.target + o.at * a.z.stride, g, a.z.V, lane);
+        const SegData<SF_BF16> y = seg_load<SF_BF16>(a.drafts + (o.at - b) * a.zq.stride, g, a.z.V, lane);
+        const Residual residual(o.v, a.z, a.zq);
+        double sum = __any(x.edge != -INFINITY) ? residual(x.edge, y.edge) : 0.0;
+#pragma unroll
+        for (int k = 0; k < kSegU; ++k) {
+            if (k >= live) break;
+            if (!residual.plain) {
+                sum += residual.template sum<SF_BF16>(x.y[k], y.y[k]);
+                continue;
+            }
+            const Words4 p = __builtin_bit_cast(Words4, (VecU<SF_BF16>)x.y[k]), q = __builtin_bit_cast(Words4, (VecU<SF_BF16>)y.y[k]);
+            double own = 0.0;
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) {
+                const Two at = table_places(p[j], begin), to = table_places(q[j], begin);
+                own += residual.left(table[at[0]], table[to[0]]);
+                own += residual.left(table[at[1]], table[to[1]]);
+            }
+            sum += own;
+        }
+        sum = residual.segment(sum);
+        if (lane == 0) a.residual[b * a.z.nseg + g] = sum;
+    }
+}
+
 // Draws the last tokens of sequences whose residuals were summed by parts: a
 // workgroup each.
 template <int DT>
@@ -615,8 +701,9 @@ static inline unsigned up_to(int64_t n, int64_t most) { return (unsigned)(n < mo
 
 // Threads that a row has to itself: 64, kRowsWG or 1024, or 0 where rows are split
 // over workgroups.
-static inline int sample_threads(int64_t N, int64_t nseg)
+static inline int sample_threads(int32_t dtype, int64_t N, int64_t nseg)
 {
+    if (dtype == SF_BF16 && nseg >= 16 && N * nseg >= kTableSegments) return 0;
     if (nseg == 1 || (N >= 4096 && nseg <= kLdsSegs / kRowsWaves)) return 64;
     if (N >= 512) return nseg <= kLdsSegs ? kRowsWG : 0;
     return nseg <= 32 ? 1024 : 0;
@@ -630,7 +717,7 @@ SF_API int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V)
 {
     if (!rows_ok(dtype, N, V, V, 1.0f)) return -1;
     const int64_t nseg = seg_count(dtype, V);
-    return N == 0 || sample_threads(N, nseg) ? 0 : N * nseg * (int64_t)sizeof(RowSum);
+    return N == 0 || sample_threads(dtype, N, nseg) ? 0 : N * nseg * (int64_t)sizeof(RowSum);
 }
 
 SF_API int sf_token_sample(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t row_stride,
@@ -655,7 +742,7 @@ SF_API int sf_token_sample(const void* logits, int32_t dtype, int64_t N, int64_t
             if (sizes[j] > 0 && !disjoint(outs[i], sizes[i], outs[j], sizes[j])) return SF_EINVAL;
     }
     RowArg z = row_arg(dtype, V, row_stride, inv_temperature);
-    const int threads = sample_threads(N, z.nseg);
+    const int threads = sample_threads(dtype, N, z.nseg);
     void* args[] = {(void*)&logits, (void*)&N, (void*)&uniform, (void*)&z, (void*)&out_token, (void*)&out_logp};
     if (z.nseg == 1) {
         const int live = seg_live(dtype, V);
@@ -716,7 +803,7 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     const int64_t rows = D + B, more = drafts ? D : 0;
     VerifyArg<DT> a = {(const T*)target, (const T*)drafts, draft, start, uniform, D, B, z, zq, sums, residual, accepted, token, logp};
     int rc;
-    if (D >= 2 * B && (rows + more) * z.nseg > (drafts ? kManySegments : kManySegments / 4)) {
+    if (D >= 2 * B && !(drafts && by_table(DT, D, zq)) && (rows + more) * z.nseg > (drafts ? kManySegments : kManySegments / 4)) {
         // the first rows, then those behind accepted drafts
         int64_t k0 = 0, k1 = drafts ? 1 + D / B / 3 : 1, all = (int64_t)1 << 31;
         const int64_t kinds = drafts ? 2 : 1, rest = kinds * (D / B - k1 + 1);
@@ -724,11 +811,11 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
         void* alive[] = {(void*)&a, (void*)&k1, (void*)&outcomes};
         void* others[] = {(void*)&a, (void*)&k1, (void*)&all, (void*)&outcomes, (void*)&sums};
         const unsigned gx = segment_groups<DT>(z), gy = up_to(B, 65535);
-        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, (unsigned)(kinds * k1 < 64 ? kinds * k1 : 64)), dim3(kRowsWG), first, 0, stream);
+        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, up_to(kinds * k1, 64)), dim3(kRowsWG), first, 0, stream);
         if (rc != SF_OK) return rc;
         rc = launch((const void*)&k_draft_alive<DT>, dim3(up_to(B, 1 << 21)), dim3(kRowsWG), alive, 0, stream);
         if (rc != SF_OK) return rc;
-        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, (unsigned)(rest < 6 ? rest : 6)), dim3(kRowsWG), others, 0, stream);
+        rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, up_to(rest, 6)), dim3(kRowsWG), others, 0, stream);
     } else {
         rc = sum_segments<DT>(target, rows, z, drafts, more, zq, nullptr, sums, stream);
     }
@@ -744,8 +831,16 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     } else {
         rc = launch((const void*)&k_draft_judge<DT, false>, draws, dim3(kVerifyWG), args, 0, stream);
         if (rc != SF_OK) return rc;
-        rc = launch((const void*)&k_draft_residual<DT>, dim3((z.nseg + kRowsWaves - 1) / kRowsWaves, up_to(B, 65535)),
-                    dim3(kRowsWG), args, 0, stream);
+        if (z.c == zq.c && by_table(DT, B, z)) {
+            uint32_t begin = (uint32_t)table_begin(z.c);
+            int cus;
+            if (device_cus(stream, &cus) != SF_OK) return SF_EHIP;
+            void* by_args[] = {(void*)&a, (void*)&begin, (void*)&outcomes};
+            rc = launch((const void*)&k_residual_table, dim3(cus), dim3(kTableWG), by_args, 0, stream);
+        } else {
+            rc = launch((const void*)&k_draft_residual<DT>, dim3((z.nseg + kRowsWaves - 1) / kRowsWaves, up_to(B, 65535)),
+                        dim3(kRowsWG), args, 0, stream);
+        }
     }
     if (rc != SF_OK) return rc;
     return launch((const void*)&k_draft_draw<DT>, draws, dim3(kRowsWG), args, 0, stream);

@@ -48,11 +48,16 @@ def fits(got):
     (1, 1, BF16, ["short<1, 1>"]), (1, 519, BF16, ["short<1, 1>"]), (1, 520, BF16, ["short<1, 2>"]),
     (1, 1031, F16, ["short<2, 2>"]), (1, 1032, F16, ["short<2, 4>"]), (9, 2048, F16, ["short<2, 4>"]),
     (9, 259, F32, ["short<0, 1>"]), (9, 1024, F32, ["short<0, 4>"]), (9, 1025, F32, ["sample<0, 1024, 16>"]),
-    (1, 2049, BF16, ["sample<1, 1024, 16>"]), (511, 65536, BF16, ["sample<1, 1024, 16>"]),
-    (511, 65537, BF16, ["row_segments<1>", "draw<1>"]), (512, 65537, BF16, ["sample<1, 256, 4>"]),
-    (512, 2097152, BF16, ["sample<1, 256, 4>"]), (512, 2097153, BF16, ["row_segments<1>", "draw<1>"]),
-    (4095, 524288, BF16, ["sample<1, 256, 4>"]), (4096, 524288, BF16, ["sample<1, 256, 1>"]),
-    (4096, 524289, BF16, ["sample<1, 256, 4>"])])
+    (1, 2049, BF16, ["sample<1, 1024, 16>"]), (255, 65536, BF16, ["sample<1, 1024, 16>"]),
+    (256, 65536, BF16, ["row_table", "draw<1>"]), (255, 65537, BF16, ["row_table", "draw<1>"]),
+    (248, 65537, BF16, ["row_segments<1>", "draw<1>"]), (1024, 30720, BF16, ["sample<1, 256, 4>"]),
+    (1024, 30721, BF16, ["row_table", "draw<1>"]), (512, 30721, BF16, ["row_table", "draw<1>"]),
+    (511, 30721, BF16, ["sample<1, 1024, 16>"]), (9000, 30720, BF16, ["sample<1, 256, 1>"]),
+    (511, 65536, F16, ["sample<2, 1024, 16>"]), (511, 65537, F16, ["row_segments<2>", "draw<2>"]),
+    (512, 65537, F16, ["sample<2, 256, 4>"]), (512, 2097152, F16, ["sample<2, 256, 4>"]),
+    (512, 2097153, F16, ["row_segments<2>", "draw<2>"]), (4095, 524288, F16, ["sample<2, 256, 4>"]),
+    (4096, 524288, F16, ["sample<2, 256, 1>"]), (4096, 524289, F16, ["sample<2, 256, 4>"]),
+    (1 << 20, 1 << 22, BF16, ["row_segments<1>", "draw<1>"])])
 def test_sample_launches(run, N, V, dtype, kernels):
     got = run([sample(N, V, dtype)])[0]
     assert [g[0].split("k_", 1)[1].replace("token_", "") for g in got] == kernels
@@ -64,17 +69,42 @@ def test_sample_launches(run, N, V, dtype, kernels):
     (5, 1, 65536, True, ["row_segments<1>", "draft_judge<1, true>"]),
     (32, 32, 65536, False, ["row_segments<1>", "draft_few<1>", "draft_draw<1>"]),
     (32, 33, 65536, False, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (1024, 256, 131072, False, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, false>",
-                                "draft_residual<1>", "draft_draw<1>"]),
-    (511, 256, 131072, False, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (512, 256, 105000, False, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, false>",
-                               "draft_residual<1>", "draft_draw<1>"]),
-    (512, 256, 104000, False, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (1024, 256, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
+    (511, 256, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
+    (128, 128, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
+    (128, 127, 131072, False, ["row_table", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (127, 128, 131072, False, ["row_segments<1>", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
     (900, 200, 50001, True, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, true>"]),
-    (900, 200, 20000, True, ["row_segments<1>", "draft_judge<1, true>"])])
+    (900, 200, 20000, True, ["row_table", "draft_judge<1, true>"]),
+    (300, 200, 50001, True, ["row_table", "draft_judge<1, true>"])])
 def test_verify_launches(run, D, B, V, lookup, kernels):
     got = run([verify(D, B, V, BF16, lookup)])[0]
     assert [g[0].split("k_", 1)[1] for g in got] == kernels
+
+
+@pytest.mark.parametrize("D,B,V,kernels", [
+    (1024, 256, 131072, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_judge<2, false>",
+                         "draft_residual<2>", "draft_draw<2>"]),
+    (511, 256, 131072, ["row_segments<2>", "draft_judge<2, false>", "draft_residual<2>", "draft_draw<2>"]),
+    (512, 256, 105000, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_judge<2, false>",
+                        "draft_residual<2>", "draft_draw<2>"]),
+    (512, 256, 104000, ["row_segments<2>", "draft_judge<2, false>", "draft_residual<2>", "draft_draw<2>"])])
+def test_verify_launches_without_a_table(run, D, B, V, kernels):
+    assert [g[0].split("k_", 1)[1] for g in run([verify(D, B, V, F16)])[0]] == kernels
+
+
+@pytest.mark.parametrize("inv_t,iq,kernels", [
+    (1.0, 1.0, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
+    (1.0, 0.5, ["row_table", "row_table", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (2.0 ** 100, 1.0, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (2.0 ** -110, 2.0 ** -110, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
+    (2.0 ** -120, 2.0 ** -120, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, false>",
+                                "draft_residual<1>", "draft_draw<1>"])])
+def test_tables_of_temperatures(run, inv_t, iq, kernels):
+    """A table serves one temperature, whose range of powers a bfloat16 has."""
+    call = verify(1024, 256, 131072)
+    call[1][11:13] = [["f", inv_t], ["f", iq]]
+    assert [g[0].split("k_", 1)[1] for g in run([call])[0]] == kernels
 
 
 @pytest.mark.parametrize("N,C,kw,far,grid", [
@@ -94,11 +124,12 @@ def test_largest(run):
               for d in (F32, BF16)]))
     fits(run([verify(D, B, V, d, lookup) for D, B, V in ((0, 1, 1 << 30), (1 << 12, 1, 1 << 30), (1 << 12, 1 << 12, 1 << 30),
                                                         ((1 << 31) - 1, (1 << 31) - 1, 5), ((1 << 31) - 1, 1, 1000),
-                                                        ((1 << 31) - 1, 1 << 20, 1000), (0, (1 << 31) - 1, 100))
+                                                        ((1 << 31) - 1, 1 << 20, 1000), (0, (1 << 31) - 1, 100),
+                                                        (1 << 19, 1 << 19, 1 << 20))
               for d in (F32, BF16) for lookup in (False, True)]))
 
 
 def test_kernels_spill_nothing(tmp_path):
     mine = {k: n for k, n in spilled_vgprs(tmp_path).items()
-            if k.startswith(("k_uniform", "k_dropout", "k_token_short", "k_token_sample", "k_token_draw", "k_row_seg", "k_draft"))}
+            if k.startswith(("k_uniform", "k_dropout", "k_token_short", "k_token_sample", "k_token_draw", "k_row_", "k_draft", "k_residual"))}
     assert len(mine) >= 50 and not any(mine.values()), mine

@@ -285,6 +285,38 @@ def test_sample_rows_far_from_zero(dr, kind, V):
     assert torch.equal(many[0].view(50, 12), one[0].expand(50, 12)) and torch.equal(many[1].view(50, 12), one[1].expand(50, 12))
 
 
+@pytest.mark.parametrize("inv_t", [1.0, 0.6, 1e-3, 37.0, 2.0 ** -100, 2.0 ** -120, 2.0 ** 20, 2.0 ** 100])
+def test_sample_many_bfloat16_rows(dr, inv_t):
+    """Powers from a table: numbers of every binade and both signs, denormals, zeros,
+    masked entries and NaN of either sign, against the definition and against the
+    same rows in a small call."""
+    V = 32771
+    every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    finite = every[torch.isfinite(every)]
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randn(10, V, generator=g) * 3.0).to(torch.bfloat16)
+    x[0] = finite[torch.randint(0, len(finite), (V,), generator=g)]     # any number
+    small = finite[(finite.float().abs() * inv_t) < 300.0]
+    x[1] = small[torch.randint(0, len(small), (V,), generator=g)]       # any that is not far
+    x[2] = finite[finite.float().abs() < 1e-20][torch.randint(0, 15000, (V,), generator=g)]
+    x[3] = 0.0
+    x[3, 1::2] = -0.0
+    x[4, ::2] = -INF
+    x[5, 4096:20000] = -INF                                              # whole segments
+    x[6, 32770] = NAN
+    x[7, 5] = torch.tensor(-1, dtype=torch.int16).view(torch.bfloat16)   # NaN with its sign set
+    x[8] += (700.0 / inv_t if inv_t >= 0.6 else 0.0)
+    x[9] -= (700.0 / inv_t if inv_t >= 0.6 else 0.0)
+    u = torch.tensor([0.5, 0.3, 0.7, 0.2, 0.9, 0.1, 0.5, 0.5, 0.6, 1 - 2.0 ** -24])
+    x, u = x.to(DEV), u.to(DEV)
+    one = check_sample(dr, x, u, inv_t)
+    many = dr.sf_token_sample(x.repeat(60, 1), u.repeat(60), inv_temperature=inv_t)
+    assert torch.equal(many[0].view(60, 10), one[0].expand(60, 10))
+    # (what a table takes for 1 is off by 2^-41)
+    assert (many[1].view(60, 10).nan_to_num(7.0) - one[1].nan_to_num(7.0)).abs().max() <= 2 * ref.U * 200
+    assert one[0][[6, 7]].tolist() == [-1, -1] and torch.isnan(many[1].view(60, 10)[:, 6:8]).all()
+
+
 def test_sample_greedy(dr):
     """The first of the largest logits at a temperature near 0 and u = 0."""
     x = rows(40, 5003, "bf16", 5)
@@ -398,7 +430,7 @@ def test_verify(dr, kind, lookup, counts, V, pad, shift):
 @pytest.mark.parametrize("lookup", [False, True])
 @pytest.mark.parametrize("counts,V,times", [
     ([3, 2, 4, 0, 1, 9, 5], 130, 200), ([3, 2, 4, 0, 1, 9, 5], 130, 2500), ([8, 3, 5], 2500, 150), ([8, 3, 5], 2500, 1000),
-    ([4, 4], 70003, 6), ([4, 4], 70003, 130), ([3, 1, 2], 20000, 40), ([2, 2, 2], 300, 7000)])
+    ([4, 4], 70003, 6), ([4, 4], 70003, 130), ([1, 2, 0], 70003, 130), ([3, 1, 2], 20000, 40), ([2, 2, 2], 300, 7000)])
 def test_verify_in_large_batches(dr, kind, lookup, counts, V, times):
     """The same sequences, few and many: sums all at once, rounds of them that leave
     rows out, residuals by part and by segment."""
