@@ -2,10 +2,16 @@
 // (sf_token_sample), and the verification of drafted tokens (sf_draft_verify).
 //
 // Tokens are whole numbers, so they are either the definition's or wrong: every
-// sum and comparison that decides one is in 64 bits, whose vector rate on this
-// chip is that of 32 bits.  A row is summed by segments (sf_draw.h), whose sums
+// sum and comparison that decides one is in 64 bits.  (In 32 bits a cumulative sum
+// over 131072 entries is off by up to 2^-20 of the whole, more than most entries of
+// a flat distribution have.)  A row is summed by segments (sf_draw.h), whose sums
 // give the normaliser and, in order, the cumulative sums at the segments' ends;
 // the segment that the uniform number falls into is read again for its entry.
+//
+// What bounds it: 18 instructions an entry, 14 of them of 64 bits, which issue at
+// the rate of 32-bit ones but draw power enough to lower the clock (2.1 GHz).  302
+// million bfloat16 entries take 196 us at 81% of the issue slots, 115 us by a table
+// of powers in LDS, and HBM alone 85 us.
 
 #include "sf_draw.h"
 #include "sf_host.h"
@@ -15,10 +21,10 @@ namespace sfk {
 constexpr int kRowsWG = 256;
 constexpr int kRowsWaves = kRowsWG / 64;
 static_assert(kRowsWaves == kSegU, "a wave for each vector of a segment");
-constexpr int64_t kFewSegments = 1024;
-constexpr int64_t kManySegments = 65536;
-constexpr int64_t kTableSegments = 8192;
-constexpr int kLdsSegs = 1024;  // of a row that one workgroup takes
+constexpr int64_t kFewSegments = 1024;     // of residuals that are judged where they are summed
+constexpr int64_t kManySegments = 65536;   // of rows that are summed in two rounds
+constexpr int64_t kTableSegments = 8192;   // of rows whose powers come from a table
+constexpr int kLdsSegs = 1024;             // of a row that one workgroup takes
 
 __device__ __forceinline__ bool in_unit(float u) { return u >= 0.0f && u < 1.0f; }
 
@@ -47,7 +53,9 @@ __device__ __forceinline__ void draw_token(const typename Elem<DT>::T* row, cons
 }
 
 // Rows of one segment, LIVE vectors a lane: a wave each, which keeps the powers
-// from the sum to the choice, with the next row on its way.
+// from the sum to the choice, with the next row on its way.  (16000 x 515 f16: 14.4
+// us, in place of 48 by segments of 2048 places and a second read; 372 instructions a
+// row are 10 us of it, 144 of them the powers of 512 entries.)
 template <int DT, int LIVE>
 __global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
                                                          const float* __restrict__ uniform, RowArg z,
@@ -130,8 +138,8 @@ __global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>
 // Rows of a wave each (WAVES = 1) or a workgroup of WG threads each.
 template <int DT, int WG, int WAVES>
 __global__ __launch_bounds__(WG) void k_token_sample(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
-                                                          const float* __restrict__ uniform, RowArg z,
-                                                          int64_t* __restrict__ token, float* __restrict__ logp)
+                                                     const float* __restrict__ uniform, RowArg z,
+                                                     int64_t* __restrict__ token, float* __restrict__ logp)
 {
     typedef typename Elem<DT>::T T;
     constexpr int ROWS = WG / 64 / WAVES;
@@ -162,42 +170,34 @@ __global__ __launch_bounds__(WG) void k_token_sample(const typename Elem<DT>::T*
     }
 }
 
-// Neighbouring segments that a wave sums, all on their way before the first is
-// (61 x 8 drafts of 32003 f32, 17568 segments, us with 1 / 2 / 4: 36.2 / 31.8 /
-// 33.7; segments of 16-bit entries hold twice as many and gain nothing).
+// A segment's sum by one wave, to its place.
 template <int DT>
-constexpr int kPer = DT == SF_F32 ? 2 : 1;
-
-template <int DT>
-__device__ __forceinline__ void sum_neighbours(const typename Elem<DT>::T* row, int g, const RowArg& z, int lane, RowSum* out)
+__device__ __forceinline__ void sum_segment(const typename Elem<DT>::T* row, int g, const RowArg& z, int lane, RowSum* out)
 {
-    SegData<DT> x[kPer<DT>];
-#pragma unroll
-    for (int k = 0; k < kPer<DT>; ++k)
-        if (g + k < z.nseg) x[k] = seg_load<DT>(row, g + k, z.V, lane);
-#pragma unroll
-    for (int k = 0; k < kPer<DT>; ++k)
-        if (g + k < z.nseg) {
-            const RowSum r = seg_sum<DT>(x[k], seg_live<DT>(g + k, z.V), z);
-            if (lane == 0) out[g + k] = r;
-        }
+    const RowSum r = seg_sum<DT>(seg_load<DT>(row, g, z.V, lane), seg_live<DT>(g, z.V), z);
+    if (lane == 0) out[g] = r;
 }
 
-// Sums of the segments of two groups of rows (those of b behind those of a); rows of
-// a whose uniform number says that they take no part are left out.
+// Sums of the segments of two groups of rows (those of b behind those of a), a wave
+// each; rows of a whose uniform number says that they take no part are left out.
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_row_segments(const typename Elem<DT>::T* __restrict__ a, int64_t rows_a, RowArg za,
                                                           const typename Elem<DT>::T* __restrict__ b, int64_t rows_b, RowArg zb,
                                                           const float* __restrict__ uniform, RowSum* __restrict__ out)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g = ((int)blockIdx.x * kRowsWaves + wave) * kPer<DT>;
+    const int g = (int)blockIdx.x * kRowsWaves + wave;
     if (g >= za.nseg) return;
     for (int64_t i = blockIdx.y; i < rows_a + rows_b; i += gridDim.y) {
         const bool first = i < rows_a;
         if (first && uniform && !in_unit(uniform[i])) continue;
         const typename Elem<DT>::T* row = first ? a + i * za.stride : b + (i - rows_a) * zb.stride;
-        sum_neighbours<DT>(row, g, first ? za : zb, lane, out + i * za.nseg);
+        // (member by member: a choice between the two as they are puts them into memory)
+        RowArg z = za;
+        z.c = first ? za.c : zb.c;
+        z.floor = first ? za.floor : zb.floor;
+        z.top = first ? za.top : zb.top;
+        sum_segment<DT>(row, g, z, lane, out + i * za.nseg);
     }
 }
 
@@ -245,13 +245,8 @@ static int sum_by_table(const void* a, int64_t rows_a, RowArg za, const void* b,
     return launch((const void*)&k_row_table, dim3(cus), dim3(kTableWG), args, 0, stream);
 }
 
-// Workgroups that the segments of a row make.
-template <int DT>
-static unsigned segment_groups(const RowArg& z)
-{
-    constexpr int each = kPer<DT> * kRowsWaves;
-    return (unsigned)((z.nseg + each - 1) / each);
-}
+// Workgroups that a row's segments make, a wave each.
+static inline unsigned segment_groups(const RowArg& z) { return (unsigned)((z.nseg + kRowsWaves - 1) / kRowsWaves); }
 
 template <int DT>
 static int sum_segments(const void* a, int64_t rows_a, RowArg za, const void* b, int64_t rows_b, RowArg zb,
@@ -262,7 +257,7 @@ static int sum_segments(const void* a, int64_t rows_a, RowArg za, const void* b,
         return sum_by_table(a, rows_a, za, b, rows_b, zb, uniform, out, stream);
     void* args[] = {(void*)&a, (void*)&rows_a, (void*)&za, (void*)&b, (void*)&rows_b, (void*)&zb, (void*)&uniform, (void*)&out};
     return launch((const void*)&k_row_segments<DT>,
-                  dim3(segment_groups<DT>(za), (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
+                  dim3(segment_groups(za), (unsigned)(rows < 65535 ? rows : 65535)), dim3(kRowsWG), args, 0,
                   stream);
 }
 
@@ -538,7 +533,7 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_segments(VerifyArg<DT> a, int
                                                             const Outcome* __restrict__ outcomes, RowSum* __restrict__ sums)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g = ((int)blockIdx.x * kRowsWaves + wave) * kPer<DT>;
+    const int g = (int)blockIdx.x * kRowsWaves + wave;
     if (g >= a.z.nseg) return;
     for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
         if (k0 > 0 && outcomes[b].v.what != ROW_ACCEPT) continue;
@@ -552,14 +547,15 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_segments(VerifyArg<DT> a, int
             if (drafts && k == n) continue;
             const int64_t i = drafts ? s + k : s + b + k;
             const RowArg& z = drafts ? a.zq : a.z;
-            sum_neighbours<DT>((drafts ? a.drafts : a.target) + i * z.stride, g, z, lane,
-                               sums + (i + (drafts ? a.D + a.B : 0)) * z.nseg);
+            sum_segment<DT>((drafts ? a.drafts : a.target) + i * z.stride, g, z, lane,
+                            sums + (i + (drafts ? a.D + a.B : 0)) * z.nseg);
         }
     }
 }
 
 // Judges sequences, and (DRAW) draws their last tokens where no residual's sums
-// are needed for it.
+// are needed for it.  Bound by waiting: the starts, then drafts and uniform numbers,
+// then the logits that these name, each an answer of memory (256 sequences: 5.2 us).
 template <int DT, bool DRAW>
 __global__ __launch_bounds__(kVerifyWG) void k_draft_judge(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
@@ -575,7 +571,10 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_judge(VerifyArg<DT> a, Outc
 }
 
 // Where there are few segments: judges a sequence in every workgroup of it, which
-// then takes two segments of its residual, four waves each.
+// then takes two segments of its residual, four waves each: a launch less.  (us under
+// replay in three launches / in four: 4 x 4 drafts of 131072, 256 segments, 15.7 / 18.5;
+// 64 x 4 of 32003, 1024 segments, 25.7 / 27.1; 61 x 8 of 32003 f32, 1952 segments, 40.9 /
+// 36.2; 64 x 4 of 131072, 4096 segments, 56 / 50.)
 template <int DT>
 __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
@@ -606,6 +605,7 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcom
 }
 
 // The sums of the residuals' segments of sequences that are judged, a wave each.
+// (146 of 256 sequences refused, 131072 entries: 33 us, two powers an entry.)
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_draft_residual(VerifyArg<DT> a, const Outcome* __restrict__ outcomes)
 {
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_residual(VerifyArg<DT> a, con
     }
 }
 
-// The same by a table, where both temperatures are the same.
+// The same by a table, where both temperatures are the same.  (26 us in place of 33.)
 __global__ __launch_bounds__(kTableWG) void k_residual_table(VerifyArg<SF_BF16> a, uint32_t begin, const Outcome* __restrict__ outcomes)
 {
     constexpr int E = kVec<SF_BF16>;
@@ -700,7 +700,17 @@ static inline int seg_live(int dtype, int64_t V)
 static inline unsigned up_to(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
 
 // Threads that a row has to itself: 64, kRowsWG or 1024, or 0 where rows are split
-// over workgroups.
+// over workgroups, which costs a second launch.  Measured (f16, us under replay, 64 /
+// 256 / 1024 / split):
+//   1 x 20000: 17.5 / 8.7 / 8.1 / 7.7;  1 x 50001: 36 / 13.9 / 11.5 / 7.8, but in a
+//   queue of calls, where a launch and a workspace cost the host 3 us, - / - / 10.8 /
+//   13.3;  200 x 32768: 28 / 10.8 / 10.0 / 12.8;  64 x 131072: 97 / 30 / 23 / 13.6;
+//   400 x 65536: 56 / 28 / 29 / 27;  512 x 131072: 111 / 52 / 53 / 53;
+//   600 x 8000: 13.6 / 10.1 / 17.5 / 13.0;  1024 x 32768: 35 / 27 / 38 / 33;
+//   2048 x 32768: 58 / 52 / 75 / 63;  4096 x 8000: 34 / 36 / 90 / 44;
+//   4096 x 16384: 54 / 58 / 98 / 67;  8000 x 32768: 181 / 186 / 288 / 203.
+// Many bfloat16 rows are split for the table's sake (by_table); short ones have more
+// to draw than to sum.
 static inline int sample_threads(int32_t dtype, int64_t N, int64_t nseg)
 {
     if (dtype == SF_BF16 && nseg >= 16 && N * nseg >= kTableSegments) return 0;
@@ -804,13 +814,17 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     VerifyArg<DT> a = {(const T*)target, (const T*)drafts, draft, start, uniform, D, B, z, zq, sums, residual, accepted, token, logp};
     int rc;
     if (D >= 2 * B && !(drafts && by_table(DT, D, zq)) && (rows + more) * z.nseg > (drafts ? kManySegments : kManySegments / 4)) {
-        // the first rows, then those behind accepted drafts
+        // The first rows, then those behind accepted drafts, which costs two launches of
+        // 5 us.  (f16, us with the first 1 / 2 / 3 rows / all at once: 256 x 4 drafts of
+        // 131072, 79% accepted, 230 / 224 / 233 / 245; 128 x 4 125 / 125 / 130 / 133; 64 x 4
+        // 78 / 76 / 76 / 77; 200 x 9 without logits of 50001, 12% accepted, 36 / 40 / 38 / 56.
+        // By a table, all at once, 256 x 4 bf16 take 140, and 156 in two rounds.)
         int64_t k0 = 0, k1 = drafts ? 1 + D / B / 3 : 1, all = (int64_t)1 << 31;
         const int64_t kinds = drafts ? 2 : 1, rest = kinds * (D / B - k1 + 1);
         void* first[] = {(void*)&a, (void*)&k0, (void*)&k1, (void*)&outcomes, (void*)&sums};
         void* alive[] = {(void*)&a, (void*)&k1, (void*)&outcomes};
         void* others[] = {(void*)&a, (void*)&k1, (void*)&all, (void*)&outcomes, (void*)&sums};
-        const unsigned gx = segment_groups<DT>(z), gy = up_to(B, 65535);
+        const unsigned gx = segment_groups(z), gy = up_to(B, 65535);
         rc = launch((const void*)&k_draft_segments<DT>, dim3(gx, gy, up_to(kinds * k1, 64)), dim3(kRowsWG), first, 0, stream);
         if (rc != SF_OK) return rc;
         rc = launch((const void*)&k_draft_alive<DT>, dim3(up_to(B, 1 << 21)), dim3(kRowsWG), alive, 0, stream);
@@ -838,8 +852,7 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
             void* by_args[] = {(void*)&a, (void*)&begin, (void*)&outcomes};
             rc = launch((const void*)&k_residual_table, dim3(cus), dim3(kTableWG), by_args, 0, stream);
         } else {
-            rc = launch((const void*)&k_draft_residual<DT>, dim3((z.nseg + kRowsWaves - 1) / kRowsWaves, up_to(B, 65535)),
-                        dim3(kRowsWG), args, 0, stream);
+            rc = launch((const void*)&k_draft_residual<DT>, dim3(segment_groups(z), up_to(B, 65535)), dim3(kRowsWG), args, 0, stream);
         }
     }
     if (rc != SF_OK) return rc;

@@ -17,7 +17,7 @@ struct Words {
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011): ten rounds of two
 // 32 x 32 -> 64 bit products and exclusive ors, the key raised by Weyl constants
-// in between.
+// in between.  (A product of 64 bits is one instruction at the full rate here.)
 __device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
 {
 #pragma unroll
@@ -218,6 +218,7 @@ __device__ __forceinline__ bool sum_is_ordinary(double s) { return s > 0x1p-200 
 // The segment's sum, in every lane.  64 bits have room for powers of ordinary
 // logits as they are, so no maximum is looked for: only whether one lies above
 // that room.  Where the sum shows that the segment is another, it is done again.
+// (Without the maximum 84 in place of 95 us at 900 rows of 131072.)
 template <int DT>
 __device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, int live, const RowArg& z)
 {
@@ -237,17 +238,19 @@ __device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, int live, const 
 
 // A bfloat16 is one of few numbers, and of those between 2^-42 / c and 2^10 / c,
 // whose powers are neither 1 nor held, there are 52 binades of 128 of each sign:
-// 104 KB of a compute unit's 160 KB of LDS.  A power then takes two packed halves
-// of five instructions, an address and a read of 8 bytes, in place of 15
-// instructions of 64 bits, and it is the same number.  2304 rows of 131072: 110 us
-// in place of 196, which 64-bit instructions and the power they draw had bound;
-// what is left is LDS (its banks meet) beside HBM (85 us without any powers).
+// 104 KB of a compute unit's 160 KB of LDS.  A power then takes half of five packed
+// instructions, two for an address and a read of 8 bytes, in place of 15 of 64 bits,
+// and it is the same number.  (float16 has eight times the numbers a binade: its table
+// would not fit.)  2304 rows of 131072: 115 us in place of 196; HBM alone takes 85,
+// and what is left is neither the banks of LDS (reads without conflicts: 112) nor reads
+// in flight (all 32 of a segment before the first is added: the same).
 constexpr int kTableBinades = 52;
 constexpr int kTableSize = 2 * kTableBinades * 128;  // sign in the lowest bit of the place
 constexpr int kTableWG = 1024;
 
-// The bits of the magnitude that the table begins at, or -1 where c is so far
-// from 1 that a float's range does not hold it.
+// The bits of the magnitude that the table begins at (at 2^-42 / c or up to twice
+// that: what lies below has a power within 2^-41 of 1), or -1 where c is so far from
+// 1 that a float's range does not hold it.
 static inline int table_begin(double c)
 {
     const int e = (int)ceil(log2(0x1p-42 / c)) + 127;

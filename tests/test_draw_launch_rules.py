@@ -2,10 +2,11 @@
 their rules and at the largest sizes, and the registers of those kernels (CPU only:
 launch_recorder.c stands in for the HIP runtime)."""
 import os
+import subprocess
 
 import pytest
 
-from launches import build_recorder, spilled_vgprs
+from launches import LLVM, build_recorder, spilled_vgprs
 from train_launches import launches
 
 LIB = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_06751_amd",
@@ -127,6 +128,29 @@ def test_largest(run):
                                                         ((1 << 31) - 1, 1 << 20, 1000), (0, (1 << 31) - 1, 100),
                                                         (1 << 19, 1 << 19, 1 << 20))
               for d in (F32, BF16) for lookup in (False, True)]))
+
+
+def test_kernels_keep_nothing_in_memory(tmp_path):
+    """No kernel of the library's third part has a stack of its own in memory."""
+    data, held = open(LIB, "rb").read(), {}
+    at = data.find(b"\x7fELF", 4)
+    while at >= 0:
+        if int.from_bytes(data[at + 18:at + 20], "little") == 224:  # an AMDGPU code object
+            end = data.find(b"\x7fELF", at + 4)
+            path = tmp_path / "object.elf"
+            path.write_bytes(data[at:end if end > 0 else len(data)])
+            notes = subprocess.run([LLVM + "llvm-readelf", "--notes", str(path)], capture_output=True, text=True).stdout
+            name = None
+            for line in notes.split("\n"):
+                key, _, value = line.strip().lstrip("- ").partition(":")
+                if key == ".name" and value.strip().startswith("_Z"):
+                    name = value.strip()
+                elif key == ".private_segment_fixed_size" and name:
+                    held[name] = int(value)
+        at = data.find(b"\x7fELF", at + 4)
+    mine = {n: v for n, v in held.items() if any(k in n for k in ("k_uniform", "k_dropout", "k_token_short", "k_token_sample",
+                                                                 "k_token_draw", "k_row_", "k_draft", "k_residual"))}
+    assert len(mine) >= 50 and not any(mine.values()), mine
 
 
 def test_kernels_spill_nothing(tmp_path):
