@@ -208,13 +208,24 @@ def sf_draft_verify(target_logits: torch.Tensor, draft_logits: torch.Tensor | No
         draft_stride = _matrix(draft_logits, "draft_logits", (D, V), target_logits)
         if draft_logits.dtype is not target_logits.dtype:
             raise TypeError("draft_logits must have the target's type")
-    _check(draft, "draft", torch.int64, (D,), target_logits)
-    _check(seq_start, "seq_start", torch.int64, (ends,), target_logits)
-    _check(uniform, "uniform", torch.float32, (rows,), target_logits)
+    index = target_logits.get_device()
+    # one chained test on the good path; which of them it is, is asked on failure
+    if not (draft.dtype is torch.int64 and seq_start.dtype is torch.int64 and uniform.dtype is torch.float32
+            and draft.get_device() == index and seq_start.get_device() == index and uniform.get_device() == index
+            and uniform.shape == (rows,) and draft.is_contiguous() and seq_start.is_contiguous()
+            and uniform.is_contiguous()):
+        _check(draft, "draft", torch.int64, (D,), target_logits)
+        _check(seq_start, "seq_start", torch.int64, (ends,), target_logits)
+        _check(uniform, "uniform", torch.float32, (rows,), target_logits)
     given = out_accepted is not None or out_token is not None or out_logp is not None
-    out_accepted = _out(out_accepted, "out_accepted", torch.int64, (B,), target_logits, stream)
-    out_token = _out(out_token, "out_token", torch.int64, (rows,), target_logits, stream)
-    out_logp = _out(out_logp, "out_logp", torch.float32, (rows,), target_logits, stream)
+    if given:
+        out_accepted = _out(out_accepted, "out_accepted", torch.int64, (B,), target_logits, stream)
+        out_token = _out(out_token, "out_token", torch.int64, (rows,), target_logits, stream)
+        out_logp = _out(out_logp, "out_logp", torch.float32, (rows,), target_logits, stream)
+    else:
+        out_accepted = _new((B,), torch.int64, dev, stream)
+        out_token = _new((rows,), torch.int64, dev, stream)
+        out_logp = _new((rows,), torch.float32, dev, stream)
     dtype = _DTYPES[target_logits.dtype]
     need = _lib.sf_draft_verify_workspace(dtype, D, B, V)
     if need != 0:
