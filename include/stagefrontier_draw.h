@@ -67,9 +67,9 @@ int sf_uniform(const int64_t* key, uint32_t site, int64_t first, int64_t n, floa
  *     out[r][j] = residual[r][j] + (keep ? scale x[r][j] : 0)
  * The entry's index is e = first + r index_stride + j; it is kept where bits
  * 16 (e mod 2) and up of word (e mod 8) div 2 of block e div 8, 16 bits, are at
- * least t = floor(65536 p + 1/2), and scale = 65536 / (65536 - t): p is taken to
- * the next multiple of 2^-16, and the expectation is x exactly.  (16 bits an
- * entry: the generator is what bounds the kernel beside HBM.)
+ * least t = floor(65536 p + 1/2), and scale = 65536 / (65536 - t), 0 where t =
+ * 65536: p is taken to the nearest multiple of 2^-16, and the expectation is x,
+ * but for the scale's rounding to a float.
  * The product is added in 32 bits with one rounding, and rounded once to the
  * output's type.  What is dropped counts as 0, also where x is not finite.
  *
@@ -81,8 +81,10 @@ int sf_uniform(const int64_t* key, uint32_t site, int64_t first, int64_t n, floa
  *   x               [N][x_stride] of type dtype, the first C entries of each
  *                   row used.
  *   out             [N][out_stride] of type out_dtype.  May be x or the
- *                   residual (same pointer, stride and type); must not overlap
- *                   them in any other way.  Entries from C on are left alone.
+ *                   residual (same pointer, stride and type); else the memory
+ *                   from its first to its last entry must hold none of theirs,
+ *                   nor the gaps between their rows.  Entries from C on are
+ *                   left alone.
  *   residual        [N][residual_stride] of type out_dtype, or NULL.
  *   dtype, out_dtype  SF_F32, SF_BF16 or SF_F16.
  *   N, C            N >= 0, C >= 0; with one of them 0 a no-op.  Each, and each
@@ -170,6 +172,8 @@ int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V);
  *                    they were.
  *   workspace        sf_draft_verify_workspace(dtype, D, B, V) bytes, 16-byte
  *                    aligned.
+ *
+ * Rows behind the draft that is refused may be read or not.
  *
  * A sequence ends without a token drawn (-1) at a row that is reached where the
  * uniform number lies outside [0, 1) (logp 0), the target's logits are all -inf

@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kTableWG) void k_row_table(const __bf16* __restrict
 
 // Whether rows' sums go by a table: many of bfloat16, at a temperature not too far
 // from 1.  (us by the kernels without / with it: 128 rows of 131072, 8192 segments,
-// 19.1 / 15.2; 1000 rows 84 / 55; 32 x 4 drafts of 65536, 3072 + 2048 segments, 22 / 26;
+// 19.1 / 15.2; 1000 rows 84 / 55; 32 x 4 drafts of 65536 22 / 26;
 // 128 x 4 drafts of 65536 49 / 43; 256 x 4 drafts of 131072 224 / 147.)
 static inline bool by_table(int32_t dtype, int64_t rows, const RowArg& z)
 {

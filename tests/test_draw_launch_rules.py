@@ -51,9 +51,9 @@ def fits(got):
     (9, 259, F32, ["short<0, 1>"]), (9, 1024, F32, ["short<0, 4>"]), (9, 1025, F32, ["sample<0, 1024, 16>"]),
     (1, 2049, BF16, ["sample<1, 1024, 16>"]), (255, 65536, BF16, ["sample<1, 1024, 16>"]),
     (256, 65536, BF16, ["row_table", "draw<1>"]), (255, 65537, BF16, ["row_table", "draw<1>"]),
-    (248, 65537, BF16, ["row_segments<1>", "draw<1>"]), (1024, 30720, BF16, ["sample<1, 256, 4>"]),
-    (1024, 30721, BF16, ["row_table", "draw<1>"]), (512, 30721, BF16, ["row_table", "draw<1>"]),
-    (511, 30721, BF16, ["sample<1, 1024, 16>"]), (9000, 30720, BF16, ["sample<1, 256, 1>"]),
+    (248, 65537, BF16, ["row_segments<1>", "draw<1>"]), (1024, 30700, BF16, ["sample<1, 256, 4>"]),
+    (1024, 30750, BF16, ["row_table", "draw<1>"]), (512, 30750, BF16, ["row_table", "draw<1>"]),
+    (511, 30750, BF16, ["sample<1, 1024, 16>"]), (9000, 30700, BF16, ["sample<1, 256, 1>"]),
     (511, 65536, F16, ["sample<2, 1024, 16>"]), (511, 65537, F16, ["row_segments<2>", "draw<2>"]),
     (512, 65537, F16, ["sample<2, 256, 4>"]), (512, 2097152, F16, ["sample<2, 256, 4>"]),
     (512, 2097153, F16, ["row_segments<2>", "draw<2>"]), (4095, 524288, F16, ["sample<2, 256, 4>"]),

@@ -160,7 +160,7 @@ def test_dropout_gradient(dr):
     check_dropout(g, dr.sf_dropout(g, p, k, site=1, out_dtype=torch.bfloat16), keep, p, None, "bf16")
 
 
-@pytest.mark.parametrize("N,C", [(70000, 3), (3, 3000001), (131073, 9)])
+@pytest.mark.parametrize("N,C", [(70000, 3), (3, 3000001), (131073, 9), (9000001, 1)])
 def test_dropout_more_than_a_launch(dr, N, C):
     """More rows than a grid holds, rows of many turns: the mask's share, ends of
     rows and equal parts."""
@@ -362,6 +362,36 @@ def test_sample_does_not_depend_on_split_or_address(dr):
         assert got[0] == many[0][7] and got[1] == many[1][7]
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_sample_long_rows(dr, kind):
+    """Rows of many more segments than a wave has lanes."""
+    check_sample(dr, rows(2, 3000001, kind, 3, 0, 1), torch.tensor([0.4, 0.99999], device=DEV), 1.0)
+    x = rows(3, 2200000, kind, 5)
+    one = dr.sf_token_sample(x, uniforms(3, 9))
+    many = dr.sf_token_sample(x.repeat(173, 1), uniforms(3, 9).repeat(173))
+    assert torch.equal(many[0].view(173, 3), one[0].expand(173, 3)) and torch.equal(many[1].view(173, 3), one[1].expand(173, 3))
+
+
+def test_calls_without_anything(dr):
+    """No rows, no entries, no sequences, no drafts: nothing is done, nothing fails."""
+    key, none = key_of(1, 1), torch.zeros(0, dtype=torch.int64, device=DEV)
+    assert dr.sf_uniform(0, key).shape == (0,)
+    for shape in ((0, 5), (5, 0), (0, 0)):
+        x = torch.zeros(shape, device=DEV)
+        assert dr.sf_dropout(x, 0.5, key, residual=x).shape == shape
+    token, logp = dr.sf_token_sample(torch.zeros(0, 9, device=DEV), torch.zeros(0, device=DEV))
+    assert token.shape == logp.shape == (0,)
+    acc, token, logp = dr.sf_draft_verify(torch.zeros(0, 9, device=DEV), None, none, torch.zeros(1, dtype=torch.int64, device=DEV),
+                                          torch.zeros(0, device=DEV))
+    assert acc.shape == token.shape == logp.shape == (0,)
+    # drafts that are in no sequence
+    x = rows(4, 9, "f32", 1)
+    acc, _, _ = dr.sf_draft_verify(x, x, torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV),
+                                   torch.zeros(4, device=DEV))
+    assert acc.shape == (0,)
+    torch.cuda.synchronize()
+
+
 def test_sample_frequencies(dr):
     """Tokens come with their probabilities (5 standard deviations of each)."""
     N, p = 400000, torch.tensor([0.5, 0.25, 0.0, 0.125, 0.1, 0.02, 0.005])
@@ -424,6 +454,28 @@ def check_verify(dr, target, q, draft, start, u, inv_t=1.0, iq=1.0, **kw):
 def test_verify(dr, kind, lookup, counts, V, pad, shift):
     target, q, draft, start, u = batch(counts, V, kind, 11 * len(counts) + V, pad=pad, shift=shift, lookup=lookup)
     check_verify(dr, target, q, draft, start, u, float(np.float32(1 / 0.8)), float(np.float32(1 / 1.1)))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("V", [130, 60001])
+def test_verify_a_long_sequence(dr, kind, V):
+    """Hundreds of drafts of one sequence, most of them accepted, in rounds of eight
+    and with rows that are left out."""
+    counts = [700, 0, 650]
+    target, q, draft, start, u = batch(counts, V, kind, 3, noise=0.004)
+    accepted, token, logp = dr.sf_draft_verify(target, q, draft, start, u)
+    assert (accepted[[0, 2]] > 20).all() and accepted[1] == 0
+    if V < 1000:
+        check_verify(dr, target, q, draft, start, u)
+    # the same from the first draft that is refused, or a few before it
+    for b, s in ((0, 0), (2, 702)):
+        k0, n = max(0, int(accepted[b]) - 5), counts[b]
+        i, d = s + k0, s + k0 - b
+        part = torch.tensor([0, n - k0], device=DEV)
+        got = dr.sf_draft_verify(target[i:i + n - k0 + 1], q[d:d + n - k0], draft[d:d + n - k0].contiguous(), part,
+                                 u[i:i + n - k0 + 1].contiguous())
+        assert got[0].item() + k0 == accepted[b].item()
+        assert torch.equal(got[1], token[i:i + n - k0 + 1]) and torch.equal(got[2], logp[i:i + n - k0 + 1])
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
