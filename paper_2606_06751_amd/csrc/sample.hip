@@ -21,7 +21,7 @@ namespace sfk {
 constexpr int kRowsWG = 256;
 constexpr int kRowsWaves = kRowsWG / 64;
 static_assert(kRowsWaves == kSegU, "a wave for each vector of a segment");
-constexpr int64_t kFewSegments = 1024;     // of residuals that are judged where they are summed
+constexpr int64_t kFewSegments = 1024;     // of residuals that are decided where they are summed
 constexpr int64_t kManySegments = 65536;   // of rows that are summed in two rounds
 constexpr int64_t kTableSegments = 8192;   // of rows whose powers come from a table
 constexpr int kLdsSegs = 1024;             // of a row that one workgroup takes
@@ -332,12 +332,12 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     const int64_t i = s + b + k;
     const int64_t d = k < n ? a.draft[s + k] : -1;
     const float u = a.uniform[i];
-    const bool some = d >= 0 && d < a.z.V, judged = some && a.drafts;
+    const bool some = d >= 0 && d < a.z.V, has_q = some && a.drafts;
     const float x = some ? (float)a.target[i * a.z.stride + d] : 0.0f;
-    const float y = judged ? (float)a.drafts[(s + k) * a.zq.stride + d] : 0.0f;
+    const float y = has_q ? (float)a.drafts[(s + k) * a.zq.stride + d] : 0.0f;
     Verdict v = {};
     v.p = row_sum(a.sums + i * a.z.nseg, a.z.nseg, a.z.c, lane);
-    if (judged) v.q = row_sum(a.sums + (a.D + a.B + s + k) * a.z.nseg, a.z.nseg, a.zq.c, lane);
+    if (has_q) v.q = row_sum(a.sums + (a.D + a.B + s + k) * a.z.nseg, a.z.nseg, a.zq.c, lane);
     v.what = ROW_END;
     if (!in_unit(u)) return v;
     if (!(v.p.s > 0.0)) {
@@ -348,7 +348,7 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     if (!some) return v;
     const double pd = pow2_any((double)x - (double)v.p.m, a.z.c) / v.p.s;
     double qd = 1.0;
-    if (judged) {
+    if (has_q) {
         if (v.q.s != v.q.s) {
             v.what = ROW_END;
             v.logp = NAN;
@@ -359,7 +359,7 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     if ((double)u * qd < pd) {
         v.what = ROW_ACCEPT;
         v.logp = row_logp(x, v.p, a.z.inv_t);
-    } else if (!judged) {
+    } else if (!has_q) {
         v.what = ROW_OTHER;
     } else if (v.q.s > 0.0) {
         v.what = ROW_RESIDUAL;
@@ -467,7 +467,7 @@ constexpr int kVerifyWaves = kVerifyWG / 64;
 // Where sequence b ends, found by a workgroup: its rows eight at a time.  One of the
 // workgroups that do the same (`writes`) writes what is accepted.
 template <int DT>
-__device__ __forceinline__ Outcome judge(const VerifyArg<DT>& a, int64_t b, Verdict (&row)[kVerifyWaves], bool writes)
+__device__ __forceinline__ Outcome decide(const VerifyArg<DT>& a, int64_t b, Verdict (&row)[kVerifyWaves], bool writes)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
@@ -553,16 +553,16 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_segments(VerifyArg<DT> a, int
     }
 }
 
-// Judges sequences, and (DRAW) draws their last tokens where no residual's sums
+// Decides sequences, and (DRAW) draws their last tokens where no residual's sums
 // are needed for it.  Bound by waiting: the starts, then drafts and uniform numbers,
 // then the logits that these name, each an answer of memory (256 sequences: 5.2 us).
 template <int DT, bool DRAW>
-__global__ __launch_bounds__(kVerifyWG) void k_draft_judge(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
+__global__ __launch_bounds__(kVerifyWG) void k_draft_decide(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
     __shared__ Verdict row[kVerifyWaves];
     __shared__ PickShared shared;
     for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const Outcome o = judge<DT>(a, b, row, true);
+        const Outcome o = decide<DT>(a, b, row, true);
         if (DRAW)
             draw_last<DT>(a, b, o, shared);
         else if (threadIdx.x == 0)
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_judge(VerifyArg<DT> a, Outc
     }
 }
 
-// Where there are few segments: judges a sequence in every workgroup of it, which
+// Where there are few segments: decides a sequence in every workgroup of it, which
 // then takes two segments of its residual, four waves each: a launch less.  (us under
 // replay in three launches / in four: 4 x 4 drafts of 131072, 256 segments, 15.7 / 18.5;
 // 64 x 4 of 32003, 1024 segments, 25.7 / 27.1; 61 x 8 of 32003 f32, 1952 segments, 40.9 /
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcom
     const int g = (int)blockIdx.x * (kVerifyWaves / kSegU) + wave / kSegU, k = wave % kSegU;
     const int at = g * kSeg<DT> + (k * 64 + lane) * E, tail = a.z.V - a.z.V % E + lane;
     for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
-        const Outcome o = judge<DT>(a, b, row, blockIdx.x == 0);
+        const Outcome o = decide<DT>(a, b, row, blockIdx.x == 0);
         if (blockIdx.x == 0 && threadIdx.x == 0) outcomes[b] = o;
         if (o.v.what != ROW_RESIDUAL) continue;
         const typename Elem<DT>::T* xp = a.target + o.at * a.z.stride;
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcom
         const Residual residual(o.v, a.z, a.zq);
         double sum = 0.0;
         if (at + E <= a.z.V) sum = residual.template sum<DT>(*(const VecU<DT>*)(xp + at), *(const VecU<DT>*)(xq + at));
-        part[wave][lane] = sum;  // (a former sequence's are read: judge waits)
+        part[wave][lane] = sum;  // (a former sequence's are read: decide waits)
         __syncthreads();
         if (k == 0 && g < a.z.nseg) {
             sum = g == a.z.nseg - 1 && tail < a.z.V ? residual((float)xp[tail], (float)xq[tail]) : 0.0;
@@ -604,7 +604,7 @@ __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcom
     }
 }
 
-// The sums of the residuals' segments of sequences that are judged, a wave each.
+// The sums of the residuals' segments of sequences that are decided, a wave each.
 // (146 of 256 sequences refused, 131072 entries: 33 us, two powers an entry.)
 template <int DT>
 __global__ __launch_bounds__(kRowsWG) void k_draft_residual(VerifyArg<DT> a, const Outcome* __restrict__ outcomes)
@@ -837,13 +837,13 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
     void* args[] = {(void*)&a, (void*)&outcomes};
     const dim3 draws(up_to(B, 1 << 21));
     if (!drafts)
-        return launch((const void*)&k_draft_judge<DT, true>, draws, dim3(kVerifyWG), args, 0, stream);
+        return launch((const void*)&k_draft_decide<DT, true>, draws, dim3(kVerifyWG), args, 0, stream);
     if (B * z.nseg <= kFewSegments) {
         constexpr int each = kVerifyWaves / kSegU;
         rc = launch((const void*)&k_draft_few<DT>, dim3((z.nseg + each - 1) / each, up_to(B, 65535)), dim3(kVerifyWG), args, 0,
                     stream);
     } else {
-        rc = launch((const void*)&k_draft_judge<DT, false>, draws, dim3(kVerifyWG), args, 0, stream);
+        rc = launch((const void*)&k_draft_decide<DT, false>, draws, dim3(kVerifyWG), args, 0, stream);
         if (rc != SF_OK) return rc;
         if (z.c == zq.c && by_table(DT, B, z)) {
             uint32_t begin = (uint32_t)table_begin(z.c);

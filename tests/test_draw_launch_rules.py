@@ -67,39 +67,39 @@ def test_sample_launches(run, N, V, dtype, kernels):
 @pytest.mark.parametrize("D,B,V,lookup,kernels", [
     (0, 1, 5, False, ["row_segments<1>", "draft_few<1>", "draft_draw<1>"]),
     (5, 1, 65536, False, ["row_segments<1>", "draft_few<1>", "draft_draw<1>"]),
-    (5, 1, 65536, True, ["row_segments<1>", "draft_judge<1, true>"]),
+    (5, 1, 65536, True, ["row_segments<1>", "draft_decide<1, true>"]),
     (32, 32, 65536, False, ["row_segments<1>", "draft_few<1>", "draft_draw<1>"]),
-    (32, 33, 65536, False, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (1024, 256, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (511, 256, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (128, 128, 131072, False, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (128, 127, 131072, False, ["row_table", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (127, 128, 131072, False, ["row_segments<1>", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (900, 200, 50001, True, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, true>"]),
-    (900, 200, 20000, True, ["row_table", "draft_judge<1, true>"]),
-    (300, 200, 50001, True, ["row_table", "draft_judge<1, true>"])])
+    (32, 33, 65536, False, ["row_segments<1>", "draft_decide<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (1024, 256, 131072, False, ["row_table", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (511, 256, 131072, False, ["row_table", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (128, 128, 131072, False, ["row_table", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (128, 127, 131072, False, ["row_table", "draft_decide<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (127, 128, 131072, False, ["row_segments<1>", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (900, 200, 50001, True, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_decide<1, true>"]),
+    (900, 200, 20000, True, ["row_table", "draft_decide<1, true>"]),
+    (300, 200, 50001, True, ["row_table", "draft_decide<1, true>"])])
 def test_verify_launches(run, D, B, V, lookup, kernels):
     got = run([verify(D, B, V, BF16, lookup)])[0]
     assert [g[0].split("k_", 1)[1] for g in got] == kernels
 
 
 @pytest.mark.parametrize("D,B,V,kernels", [
-    (1024, 256, 131072, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_judge<2, false>",
+    (1024, 256, 131072, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_decide<2, false>",
                          "draft_residual<2>", "draft_draw<2>"]),
-    (511, 256, 131072, ["row_segments<2>", "draft_judge<2, false>", "draft_residual<2>", "draft_draw<2>"]),
-    (512, 256, 105000, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_judge<2, false>",
+    (511, 256, 131072, ["row_segments<2>", "draft_decide<2, false>", "draft_residual<2>", "draft_draw<2>"]),
+    (512, 256, 105000, ["draft_segments<2>", "draft_alive<2>", "draft_segments<2>", "draft_decide<2, false>",
                         "draft_residual<2>", "draft_draw<2>"]),
-    (512, 256, 104000, ["row_segments<2>", "draft_judge<2, false>", "draft_residual<2>", "draft_draw<2>"])])
+    (512, 256, 104000, ["row_segments<2>", "draft_decide<2, false>", "draft_residual<2>", "draft_draw<2>"])])
 def test_verify_launches_without_a_table(run, D, B, V, kernels):
     assert [g[0].split("k_", 1)[1] for g in run([verify(D, B, V, F16)])[0]] == kernels
 
 
 @pytest.mark.parametrize("inv_t,iq,kernels", [
-    (1.0, 1.0, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (1.0, 0.5, ["row_table", "row_table", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (2.0 ** 100, 1.0, ["row_segments<1>", "draft_judge<1, false>", "draft_residual<1>", "draft_draw<1>"]),
-    (2.0 ** -110, 2.0 ** -110, ["row_table", "draft_judge<1, false>", "residual_table", "draft_draw<1>"]),
-    (2.0 ** -120, 2.0 ** -120, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_judge<1, false>",
+    (1.0, 1.0, ["row_table", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (1.0, 0.5, ["row_table", "row_table", "draft_decide<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (2.0 ** 100, 1.0, ["row_segments<1>", "draft_decide<1, false>", "draft_residual<1>", "draft_draw<1>"]),
+    (2.0 ** -110, 2.0 ** -110, ["row_table", "draft_decide<1, false>", "residual_table", "draft_draw<1>"]),
+    (2.0 ** -120, 2.0 ** -120, ["draft_segments<1>", "draft_alive<1>", "draft_segments<1>", "draft_decide<1, false>",
                                 "draft_residual<1>", "draft_draw<1>"])])
 def test_tables_of_temperatures(run, inv_t, iq, kernels):
     """A table serves one temperature, whose range of powers a bfloat16 has."""

@@ -566,7 +566,7 @@ def test_verify_far_temperatures(dr, kind, inv_t, iq):
 
 
 def test_verify_leaves_rows_of_no_sequence(dr):
-    """Rows before the first and behind the last sequence are neither judged nor
+    """Rows before the first and behind the last sequence are neither decided nor
     written."""
     target, q, draft, _, u = batch([8, 0, 0], 700, "bf16", 2)
     start = torch.tensor([2, 4, 4, 6], device=DEV)
@@ -749,6 +749,35 @@ def test_two_graphs(dr):
         for g, w in zip(got, want):
             assert torch.equal(g, w)
         torch.rand(1000, device=DEV).sum().item()
+
+
+def test_large_calls_in_a_graph(dr):
+    """Sums by table and in rounds, captured, replayed on new inputs and another
+    stream's work between."""
+    key = key_of(8, 0)
+    x = rows(300, 65536, "bf16", 2)
+    target, q, draft, start, u = batch([4, 0, 3], 70003, "bf16", 3)
+    big = [target.repeat(60, 1), q.repeat(60, 1), draft.repeat(60),
+           torch.cat([(start[:-1][None, :] + 7 * torch.arange(60, device=DEV)[:, None]).reshape(-1), torch.tensor([420], device=DEV)])]
+    half = [big[0].half(), None, big[2], big[3]]
+
+    def calls(key):
+        v = dr.sf_uniform(600, key, site=2)
+        out = list(dr.sf_token_sample(x, dr.sf_uniform(300, key, site=1))) + list(dr.sf_draft_verify(*big, v))
+        return out + list(dr.sf_draft_verify(*half, v))
+
+    calls(key)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        key[1] += 1
+        got = calls(key)
+    for step in range(1, 5):
+        graph.replay()
+        torch.rand(1 << 20, device=DEV).sort()
+        torch.cuda.synchronize()
+        for a, b in zip(got, calls(key_of(8, step))):
+            assert torch.equal(a, b)
 
 
 def test_device_that_is_not_the_current_one(dr, monkeypatch):
