@@ -298,7 +298,7 @@ enum {
 // Sums of max(p - q, 0) below this are rounding's.
 constexpr double kLeastResidual = 0x1p-30;
 
-struct Verdict {
+struct Fate {
     RowSum p, q;
     int what;
     float logp;  // of the draft, or what stands in place of one
@@ -327,7 +327,7 @@ __device__ __forceinline__ int64_t held(int64_t v, int64_t lo, int64_t hi) { ret
 // is asked for before it is known to be needed: a wave waits for two answers of
 // memory, not five.
 template <int DT>
-__device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b, int64_t s, int64_t n, int64_t k, int lane)
+__device__ __forceinline__ Fate row_fate(const VerifyArg<DT>& a, int64_t b, int64_t s, int64_t n, int64_t k, int lane)
 {
     const int64_t i = s + b + k;
     const int64_t d = k < n ? a.draft[s + k] : -1;
@@ -335,7 +335,7 @@ __device__ __forceinline__ Verdict row_verdict(const VerifyArg<DT>& a, int64_t b
     const bool some = d >= 0 && d < a.z.V, has_q = some && a.drafts;
     const float x = some ? (float)a.target[i * a.z.stride + d] : 0.0f;
     const float y = has_q ? (float)a.drafts[(s + k) * a.zq.stride + d] : 0.0f;
-    Verdict v = {};
+    Fate v = {};
     v.p = row_sum(a.sums + i * a.z.nseg, a.z.nseg, a.z.c, lane);
     if (has_q) v.q = row_sum(a.sums + (a.D + a.B + s + k) * a.z.nseg, a.z.nseg, a.zq.c, lane);
     v.what = ROW_END;
@@ -373,7 +373,7 @@ struct Residual {
     RowArg z, zq;
     double mp, mq, p_of, q_of;
     bool plain;
-    __device__ Residual(const Verdict& v, const RowArg& z, const RowArg& zq)
+    __device__ Residual(const Fate& v, const RowArg& z, const RowArg& zq)
         : z(z), zq(zq), mp(v.p.m), mq(v.q.m), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s), plain(v.p.m == 0.0f && v.q.m == 0.0f)
     {
     }
@@ -405,7 +405,7 @@ struct Residual {
 
 // Where a sequence ends, for the launch that draws its token.
 struct Outcome {
-    Verdict v;
+    Fate v;
     int64_t at, last;  // the row of the target, and its last, with the sequence's uniform number
     int64_t draft;     // the draft refused
 };
@@ -416,7 +416,7 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
 {
     typedef typename Elem<DT>::T T;
     const int lane = threadIdx.x & 63;
-    const Verdict& v = o.v;
+    const Fate& v = o.v;
     const float u = a.uniform[o.last];
     if (v.what == ROW_END || !in_unit(u)) {
         if (threadIdx.x == 0) {
@@ -467,16 +467,16 @@ constexpr int kVerifyWaves = kVerifyWG / 64;
 // Where sequence b ends, found by a workgroup: its rows eight at a time.  One of the
 // workgroups that do the same (`writes`) writes what is accepted.
 template <int DT>
-__device__ __forceinline__ Outcome decide(const VerifyArg<DT>& a, int64_t b, Verdict (&row)[kVerifyWaves], bool writes)
+__device__ __forceinline__ Outcome decide(const VerifyArg<DT>& a, int64_t b, Fate (&row)[kVerifyWaves], bool writes)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
     int64_t end;
     for (int64_t k0 = 0;; k0 += kVerifyWaves) {
         const int64_t k = k0 + wave;
-        Verdict v = {};
+        Fate v = {};
         v.what = ROW_PLAIN;
-        if (k <= n) v = row_verdict<DT>(a, b, s, n, k, lane);
+        if (k <= n) v = row_fate<DT>(a, b, s, n, k, lane);
         __syncthreads();  // former ones are read
         if (lane == 0) row[wave] = v;
         __syncthreads();
@@ -514,7 +514,7 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_alive(VerifyArg<DT> a, int64_
         const int64_t s = held(a.start[b], 0, a.D), n = held(a.start[b + 1], s, a.D) - s;
         bool alive = n >= k1;
         for (int64_t k = wave; alive && k - wave < k1; k += kRowsWaves) {
-            const int is = k < k1 ? row_verdict<DT>(a, b, s, n, k, lane).what : ROW_ACCEPT;
+            const int is = k < k1 ? row_fate<DT>(a, b, s, n, k, lane).what : ROW_ACCEPT;
             __syncthreads();  // former ones are read
             if (lane == 0) what[wave] = is;
             __syncthreads();
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(kRowsWG) void k_draft_segments(VerifyArg<DT> a, int
 template <int DT, bool DRAW>
 __global__ __launch_bounds__(kVerifyWG) void k_draft_decide(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
-    __shared__ Verdict row[kVerifyWaves];
+    __shared__ Fate row[kVerifyWaves];
     __shared__ PickShared shared;
     for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
         const Outcome o = decide<DT>(a, b, row, true);
@@ -579,7 +579,7 @@ template <int DT>
 __global__ __launch_bounds__(kVerifyWG) void k_draft_few(VerifyArg<DT> a, Outcome* __restrict__ outcomes)
 {
     constexpr int E = kVec<DT>;
-    __shared__ Verdict row[kVerifyWaves];
+    __shared__ Fate row[kVerifyWaves];
     __shared__ double part[kVerifyWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = (int)blockIdx.x * (kVerifyWaves / kSegU) + wave / kSegU, k = wave % kSegU;
