@@ -9,8 +9,9 @@ namespace sfk {
 constexpr int kDrawWG = 256;
 constexpr int64_t kLastCache = 256 << 20;  // bytes that the chip's last cache holds
 
-// One block of four numbers a lane and turn.  Bound by the writes: 20480007 numbers
-// 15.5 us, 5.3 TB/s; the same without the generator's ten rounds takes 13 us.
+// One block of four numbers a lane and turn.  Bound by the writes and, close behind,
+// the generator's 60 instructions a block: 20480007 numbers 14.8 us, 5.5 TB/s; without
+// its rounds 13 us.
 __global__ __launch_bounds__(kDrawWG) void k_uniform(const int64_t* __restrict__ key, uint32_t site, int64_t first,
                                                      int64_t n, float* __restrict__ out)
 {
@@ -51,11 +52,11 @@ __device__ __forceinline__ V load_eight(const V* p)
 
 // A lane takes the eight entries of one block of the generator, whose place in
 // the row depends on the row's first index, so that equal indexes keep equal
-// entries at any alignment.  Bound by HBM: 16384 x 8192 bf16 onto a residual 127 us,
-// 6.3 TB/s read + write, the same without the generator (16 bits an entry: a block
-// of 10 rounds for eight).  Loads and stores go past the caches where the call moves
-// more than the last of them holds (127 against 135 us; loads alone 131), else not
-// (4099 x 2048 f32 to bf16, 50 MB: 10.2 against 11.8 us).
+// entries at any alignment.  Bound by HBM: 16384 x 8192 bf16 onto a residual 130 us,
+// 6.2 TB/s read + write, the same without the generator (16 bits an entry: a block
+// of 10 rounds for eight).  Loads go past the caches where the call moves more than
+// the last of them holds (130 against 135 us; stores, too: 134), else not (4099 x 2048
+// f32 to bf16, 50 MB: 9.6 against 11.8 us).
 template <int XT, int OT, bool FAR>
 __global__ __launch_bounds__(kDrawWG) void k_dropout(const typename Elem<XT>::T* x, const int64_t* __restrict__ key,
                                                      const typename Elem<OT>::T* residual, typename Elem<OT>::T* out,
@@ -94,10 +95,7 @@ __global__ __launch_bounds__(kDrawWG) void k_dropout(const typename Elem<XT>::T*
                 w[j] = (O)(residual ? fmaf(xv, s, (float)w[j]) : xv * s);
             }
             if (whole) {
-                if (FAR)
-                    __builtin_nontemporal_store(w, (Eight<OT>*)(o + at));
-                else
-                    *(Eight<OT>*)(o + at) = w;
+                *(Eight<OT>*)(o + at) = w;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
