@@ -367,6 +367,11 @@ __device__ __forceinline__ Fate row_fate(const VerifyArg<DT>& a, int64_t b, int6
     return v;
 }
 
+// What the entries of a segment of residuals that hold nothing may add up to is below
+// this: powers held at 2^-1000, over the sum of an ordinary row, 2^-200 at least.  A
+// segment above it has an entry whose own difference is not 0.
+constexpr double kNoResidual = 0x1p-700;
+
 // max(p - q, 0) of entries.  Of two rows of ordinary logits powers are taken as they
 // are; what is held at 2^-1000 counts in no sum.
 struct Residual {
@@ -399,7 +404,7 @@ struct Residual {
     __device__ __forceinline__ double segment(double s) const
     {
         s = wave_sum_f64(s);
-        return s > 0x1p-900 ? s : 0.0;
+        return s > kNoResidual ? s : 0.0;
     }
 };
 
