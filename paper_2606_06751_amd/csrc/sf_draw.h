@@ -69,13 +69,14 @@ __device__ __forceinline__ double pow2_rest(double f)
 // it in its low word.
 constexpr double kWhole = 6755399441055744.0;  // 1.5 * 2^52
 
-// 2^(x c) for |x c| < 2^31: x c = whole + f by two multiply-adds, each rounded once.
-__device__ __forceinline__ double pow2(double x, double c)
+// s 2^(x c) for |x c| < 2^31: x c = whole + f by two multiply-adds, each rounded once.
+__device__ __forceinline__ double pow2_times(double s, double x, double c)
 {
     const double whole = fma(x, c, kWhole);
     const double p = pow2_rest(fma(x, c, kWhole - whole));
-    return ldexp(p, (int)(uint32_t)(uint64_t)__double_as_longlong(whole));
+    return ldexp(s * p, (int)(uint32_t)(uint64_t)__double_as_longlong(whole));
 }
+__device__ __forceinline__ double pow2(double x, double c) { return pow2_times(1.0, x, c); }
 
 // 2^(d c) for any d c up to 0 (or somewhat above): 0 below 2^-1000, NaN for NaN.
 // (Chosen, not branched for: the power of 0 in its place.)
@@ -318,10 +319,18 @@ __device__ __forceinline__ RowSum seg_sum_table(const SegData<SF_BF16>& a, int l
     return seg_sum_any<SF_BF16>(a, z.c);
 }
 
-// A segment's weight relative to the row's reference.
+// A segment's weight relative to the row's reference, whose own entry weighs 1 (the
+// sums of ordinary rows, relative to 0, 2^-200 at least).  The power is scaled with
+// the sum, which may be up to 2^900, and what is left below 2^-900 counts as 0: a
+// segment that weighs something has an entry within 2^-1000, which weighs something by
+// itself (pow2_any), so the choice that a segment is given finds one.
 __device__ __forceinline__ double seg_weight(const RowSum& a, float top, double c)
 {
-    return a.m == top ? a.s : a.m == -INFINITY ? a.s : a.s * pow2_any((double)a.m - (double)top, c);
+    if (a.m == top || a.m == -INFINITY) return a.s;
+    const double d = (double)a.m - (double)top;
+    const bool far = d * c < -2000.0;
+    const double s = pow2_times(far ? a.s * 0.0 : a.s, far ? 0.0 : d, c);
+    return s < 0x1p-900 ? 0.0 : s;  // (NaN stays)
 }
 
 // Joins a row's segments by one wave, in every lane.

@@ -64,3 +64,84 @@ def test_residual_of_low_logits_at_zero(dr, kind, times):
     assert not got[0].any()
     assert (got[1] == torch.tensor([d + 1, -1], device=DEV)).all()
     assert ((got[2][:, 0].double() - logp(d + 1)).abs() <= ref.logp_bound(logp(d + 1))).all() and not got[2][:, 1].any()
+
+
+def far_rows(kind, V, what):
+    """Rows of ordinary logits beside others that lie far above them, the tokens
+    that a uniform number of 0 may draw, and the temperature's inverse."""
+    low, high, inv_t = {"beyond": (-80.0, 656.0, 1.0), "within": (620.0, 720.0, 1.0), "cold": (-8.0, 65.5, 10.0)}[what]
+    x = torch.full((6, V), -INF)
+    x[:, :2048], x[:, V - 3] = low, high
+    x[1, 2048:4096] = high                       # a whole part that is as high
+    x[2, 7] = NAN
+    x[3, 1:2048] = -INF                          # one entry alone
+    x[4, :2048], x[4, 2048:4096] = high, low     # the other way round
+    x[5, 2048:] = -INF                           # nothing above
+    # 2^-144 of the largest has its probability; 2^-1062 may count as 0
+    allowed = [{0}] * 6 if what == "within" else [{0, V - 3}, {0, 2048}, {0}, {0, V - 3}, {0}, {0}]
+    allowed[2] = {-1}
+    return x.to(DEV, KINDS[kind]), allowed, inv_t
+
+
+def check_drawn(x, inv_t, allowed, token, logp):
+    """Copies of the rows: the same token in each, one of those allowed, and its
+    log-probability."""
+    token, logp = token.view(-1, len(allowed)), logp.view(-1, len(allowed)).double()
+    assert (token == token[:1]).all()
+    for i, (t, want) in enumerate(zip(token[0].tolist(), allowed)):
+        assert t in want, (i, t)
+        if t < 0:
+            assert torch.isnan(logp[:, i]).all()
+        else:
+            v = ref.log_p(ref.softmax(f64(x[i]), inv_t)[t])
+            assert ((logp[:, i] - v).abs() <= ref.logp_bound(v)).all(), (i, logp[0, i].item(), v)
+
+
+@pytest.mark.parametrize("kind,V,copies", WAYS)
+@pytest.mark.parametrize("what", ["beyond", "within", "cold"])
+def test_sample_far_apart_at_zero(dr, kind, V, copies, what):
+    """What has 2^-144 of the largest's probability is drawn, what has 2^-1062 of it
+    or not, and neither leaves a row without a token."""
+    x, want, inv_t = far_rows(kind, V, what)
+    u = torch.zeros(6 * copies, device=DEV)
+    check_drawn(x, inv_t, want, *dr.sf_token_sample(x.repeat(copies, 1), u, inv_temperature=inv_t))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("what", ["beyond", "within", "cold"])
+@pytest.mark.parametrize("copies", [1, 60, 400])
+def test_verify_far_apart_at_zero(dr, kind, what, copies):
+    """The same as a sequence's last token: without drafts, and behind a draft
+    without logits that the target forbids."""
+    x, want, inv_t = far_rows(kind, 9000, what)
+    u, start = torch.zeros(6, device=DEV), torch.zeros(7, dtype=torch.int64, device=DEV)
+    none = torch.zeros(0, dtype=torch.int64, device=DEV)
+    for drafts in (None, x[:0]):
+        acc, token, logp = repeated(dr, x, drafts, none, start, u, copies, inv_temperature=inv_t)
+        assert not acc.any()
+        check_drawn(x, inv_t, want, token, logp)
+    # a draft of a token with no probability before each, and rows behind that are not reached
+    target = torch.stack([x, torch.zeros_like(x)], 1).view(12, 9000)
+    draft = torch.full((6,), 8999, device=DEV)
+    u = torch.tensor([0.5, 0.0], device=DEV).repeat(6)
+    acc, token, logp = repeated(dr, target, None, draft, torch.arange(7, device=DEV), u, copies, inv_temperature=inv_t)
+    token, logp = token.view(-1, 6, 2), logp.view(-1, 6, 2)
+    assert not acc.any() and (token[:, :, 1] == -1).all() and not logp[:, :, 1].any()
+    check_drawn(x, inv_t, want, token[:, :, 0], logp[:, :, 0])
+
+
+@pytest.mark.parametrize("kind,V,copies", WAYS)
+def test_sample_any_distance_at_zero(dr, kind, V, copies):
+    """Between what is drawn and what counts as 0 either is right; a token is."""
+    g = torch.Generator().manual_seed(V + copies)
+    x = torch.full((60, V), -INF)
+    at = torch.rand(60, generator=g) * -130.0 - 10.0
+    x[:, :2048] = at[:, None]
+    x[:, V - 3] = at + torch.linspace(100.0, 800.0, 60)
+    x = x.to(DEV, KINDS[kind])
+    rows = (copies * 6 + 59) // 60
+    token, logp = dr.sf_token_sample(x.repeat(rows, 1), torch.zeros(60 * rows, device=DEV))
+    token, logp = token.view(rows, 60), logp.view(rows, 60)
+    apart = (x[:, V - 3].double() - x[:, 0].double()) * math.log2(math.e)
+    assert ((token == 0) | (token == V - 3)).all() and torch.isfinite(logp).all()
+    assert (token[:, apart < 700] == 0).all()
