@@ -373,13 +373,15 @@ __device__ __forceinline__ Fate row_fate(const VerifyArg<DT>& a, int64_t b, int6
 constexpr double kNoResidual = 0x1p-700;
 
 // max(p - q, 0) of entries.  Of two rows of ordinary logits powers are taken as they
-// are; what is held at 2^-1000 counts in no sum.
+// are; what is held at 2^-1000 counts in no sum.  (Not at temperatures so high that no
+// float but -inf is that far: it would be held as itself, whose power is NaN.)
 struct Residual {
     RowArg z, zq;
     double mp, mq, p_of, q_of;
     bool plain;
     __device__ Residual(const Fate& v, const RowArg& z, const RowArg& zq)
-        : z(z), zq(zq), mp(v.p.m), mq(v.q.m), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s), plain(v.p.m == 0.0f && v.q.m == 0.0f)
+        : z(z), zq(zq), mp(v.p.m), mq(v.q.m), p_of(1.0 / v.p.s), q_of(1.0 / v.q.s),
+          plain(v.p.m == 0.0f && v.q.m == 0.0f && z.floor > -INFINITY && zq.floor > -INFINITY)
     {
     }
     __device__ __forceinline__ double left(double p, double q) const { return fmax(fma(p, p_of, -(q * q_of)), 0.0); }

@@ -145,3 +145,22 @@ def test_sample_any_distance_at_zero(dr, kind, V, copies):
     apart = (x[:, V - 3].double() - x[:, 0].double()) * math.log2(math.e)
     assert ((token == 0) | (token == V - 3)).all() and torch.isfinite(logp).all()
     assert (token[:, apart < 700] == 0).all()
+
+
+# -- temperatures at which masked entries alone are far -------------------------
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("inv_t,iq", [(1e-37, 1e-37), (1e-37, 1.0), (1.0, 1e-37), (2.0 ** -149, 2.0 ** -149)])
+@pytest.mark.parametrize("times", [1, 700])
+def test_residual_at_nearly_infinite_temperatures(dr, kind, inv_t, iq, times):
+    """Rows of 0 and -inf: what the draft's row masks is left to the target's."""
+    V = 3000
+    target, drafts = torch.zeros(2, V), torch.zeros(1, V)
+    target[0, 2000:], drafts[0, 1000:] = -INF, -INF
+    target, drafts = target.to(DEV, KINDS[kind]), drafts.to(DEV, KINDS[kind])
+    for v, want in ((0.0, 1000), (0.3003, 1300), (0.9999, 1999)):
+        u = torch.tensor([0.9, v], device=DEV)
+        got = repeated(dr, target, drafts, torch.tensor([3], device=DEV), torch.tensor([0, 1], device=DEV), u, times,
+                       inv_temperature=inv_t, draft_inv_temperature=iq)
+        assert not got[0].any() and (got[1] == torch.tensor([want, -1], device=DEV)).all(), got[1][0].tolist()
+        assert ((got[2][:, 0].double() + math.log(2000)).abs() <= ref.logp_bound(math.log(2000))).all()
