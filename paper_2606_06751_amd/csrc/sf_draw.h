@@ -244,24 +244,25 @@ __device__ __forceinline__ RowSum seg_sum(const SegData<DT>& a, int live, const 
 
 // -- the same of many bfloat16 rows: powers from a table ----------------------
 
-// A bfloat16 is one of few numbers, and of those between 2^-42 / c and 2^10 / c,
-// whose powers are neither 1 nor held, there are 52 binades of 128 of each sign:
-// 104 KB of a compute unit's 160 KB of LDS.  A power then takes half of five packed
+// A bfloat16 is one of few numbers, and of those between 2^-55 / c and 2^10 / c,
+// whose powers are neither 1 nor held, there are 65 binades of 128 of each sign:
+// 130 KB of a compute unit's 160 KB of LDS.  A power then takes half of five packed
 // instructions, two for an address and a read of 8 bytes, in place of 15 of 64 bits,
-// and it is the same number.  (float16 has eight times the numbers a binade: its table
-// would not fit.)  2304 rows of 131072: 115 us in place of 196; HBM alone takes 85,
-// and what is left is neither the banks of LDS (reads without conflicts: 112) nor reads
-// in flight (all 32 of a segment before the first is added: the same).
-constexpr int kTableBinades = 52;
+// and it is the same number, bit for bit.  (float16 has eight times the numbers a
+// binade: its table would not fit.)  2304 rows of 131072: 115 us in place of 196; HBM
+// alone takes 85, and what is left is neither the banks of LDS (reads without
+// conflicts: 112) nor reads in flight (all 32 of a segment before the first is added:
+// the same).
+constexpr int kTableBinades = 65;
 constexpr int kTableSize = 2 * kTableBinades * 128;  // sign in the lowest bit of the place
 constexpr int kTableWG = 1024;
 
-// The bits of the magnitude that the table begins at (at 2^-42 / c or up to twice
-// that: what lies below has a power within 2^-41 of 1), or -1 where c is so far from
-// 1 that a float's range does not hold it.
+// The bits of the magnitude that the table begins at, or -1 where c is so far from 1
+// that a float's range does not hold it.  At 2^-55 / c or up to twice that, so that
+// what lies below has a power within 2^-54.5 of 1, which rounds to 1.
 static inline int table_begin(double c)
 {
-    const int e = (int)ceil(log2(0x1p-42 / c)) + 127;
+    const int e = (int)ceil(log2(0x1p-55 / c)) + 127;
     return e >= 1 && e + kTableBinades <= 254 ? e * 128 : -1;
 }
 

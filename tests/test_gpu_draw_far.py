@@ -164,3 +164,19 @@ def test_residual_at_nearly_infinite_temperatures(dr, kind, inv_t, iq, times):
                        inv_temperature=inv_t, draft_inv_temperature=iq)
         assert not got[0].any() and (got[1] == torch.tensor([want, -1], device=DEV)).all(), got[1][0].tolist()
         assert ((got[2][:, 0].double() + math.log(2000)).abs() <= ref.logp_bound(math.log(2000))).all()
+
+
+def test_powers_from_a_table_are_the_same_numbers(dr):
+    """Rows of many bfloat16 numbers near 0, whose powers are all but 1, and of one
+    such number alone: the same bits as of a few rows."""
+    V, N = 33000, 30
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(N, V, generator=g) * 2.0 ** (-60.0 + torch.arange(N)[:, None])
+    at = torch.randint(0, V, (N,), generator=g)
+    x[::2] = -INF
+    x[torch.arange(N), at] = torch.randn(N, generator=g) * 2.0 ** (-60.0 + torch.arange(N))
+    x = x.to(DEV, torch.bfloat16)
+    u = torch.rand(N, generator=g).to(DEV)
+    one = dr.sf_token_sample(x, u)
+    many = dr.sf_token_sample(x.repeat(20, 1), u.repeat(20))
+    assert (many[0].view(20, N) == one[0]).all() and (many[1].view(20, N) == one[1]).all()
