@@ -113,7 +113,9 @@ int sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t C, int64_t x_str
  *                    part (an answer that has ended): it is not read, its token
  *                    is -1 and its logp 0.
  *   out_token        [N] int64.
- *   out_logp         [N] float, rounded once.
+ *   out_logp         [N] float, at most 0: rounded once, of a number within 2^-35
+ *                    of log p, relative to it, and 2^-46 (2^-39 of rows of more
+ *                    than 2^22 entries).
  *   workspace        sf_token_sample_workspace(dtype, N, V) bytes, 16-byte
  *                    aligned; may be NULL where that is 0.
  *
@@ -167,8 +169,8 @@ int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V);
  *   out_accepted     [B] int64: drafts accepted.
  *   out_token        [D + B] int64: in a sequence's rows the accepted drafts,
  *                    the token drawn, then -1.
- *   out_logp         [D + B] float: log p of each, at the target's temperature;
- *                    0 where the token is -1.  Rows of no sequence are left as
+ *   out_logp         [D + B] float: log p of each, at the target's temperature, as
+ *                    exact as sf_token_sample's; 0 where the token is -1.  Rows of no sequence are left as
  *                    they were.
  *   workspace        sf_draft_verify_workspace(dtype, D, B, V) bytes, 16-byte
  *                    aligned.

@@ -48,7 +48,7 @@ __device__ __forceinline__ void draw_token(const typename Elem<DT>::T* row, cons
     }
     if (GROUP ? threadIdx.x == 0 : lane == 0) {
         *token = t;
-        *logp = t >= 0 ? row_logp((float)row[t], r, z.inv_t) : no_token(r);
+        *logp = t >= 0 ? row_logp((float)row[t], r, z) : no_token(r);
     }
 }
 
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>
                     const int hit = pick_scanned<1>(ve, ve[0], edges, run, target, lane, last, none);
                     t = hit >= 0 ? hit + z.V - z.V % E : last >= 0 ? last + z.V - z.V % E : t;
                 }
-                lp = t >= 0 ? row_logp((float)row[t], {s, 0.0f, 0.0f}, z.inv_t) : 0.0f;
+                lp = t >= 0 ? row_logp((float)row[t], {s, 0.0f, 0.0f}, z) : 0.0f;
             } else {
                 const RowSum r = seg_sum_any<DT>(a, z.c);
                 if (r.s > 0.0) {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>
                     t = pick_entry<DT>(row, [&](float x, int) { return pow2_any((double)x - (double)r.m, z.c); }, {0, 0.0}, z.V,
                                        target, lane);
                 }
-                lp = t >= 0 ? row_logp((float)row[t], r, z.inv_t) : no_token(r);
+                lp = t >= 0 ? row_logp((float)row[t], r, z) : no_token(r);
             }
         }
         if (lane == 0) {
@@ -358,7 +358,7 @@ __device__ __forceinline__ Fate row_fate(const VerifyArg<DT>& a, int64_t b, int6
     }
     if ((double)u * qd < pd) {
         v.what = ROW_ACCEPT;
-        v.logp = row_logp(x, v.p, a.z.inv_t);
+        v.logp = row_logp(x, v.p, a.z);
     } else if (!has_q) {
         v.what = ROW_OTHER;
     } else if (v.q.s > 0.0) {
@@ -464,7 +464,7 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
         draw_token<DT, true>(xp, seg, v.p, u, a.z, &shared, a.token + o.at, a.logp + o.at);
     } else if (threadIdx.x == 0) {
         a.token[o.at] = t;
-        a.logp[o.at] = row_logp((float)xp[t], v.p, a.z.inv_t);
+        a.logp[o.at] = row_logp((float)xp[t], v.p, a.z);
     }
 }
 

@@ -357,11 +357,18 @@ __device__ __forceinline__ double log2_of(double s)
     return (double)whole + fma(fma(d, -0.5, 1.0) * d, kLog2eD, l);
 }
 
-// log p of an entry, rounded once.
-__device__ __forceinline__ float row_logp(float x, const RowSum& r, float inv_t)
+// log p of an entry x of the row, rounded once, at most 0.  Near 0 the logarithms of the
+// sum and of the power cancel, and 2^-38.5 of error would be left: there the power e is
+// taken out of the sum s that holds it bit for bit (what has more than half of a row has
+// the row's reference), and log(e / s) = -2 artanh((s - e) / (s + e)) is as exact as what
+// is left.  The series' first term left out, v^11 / 11, is 2^-43 of it at v = 1/16.
+__device__ __forceinline__ float row_logp(float x, const RowSum& r, const RowArg& z)
 {
     constexpr double ln2 = 0.69314718055994530942;
-    return (float)fma(-ln2, log2_of(r.s), ((double)x - (double)r.m) * (double)inv_t);
+    const double d = (double)x - (double)r.m, far = fma(-ln2, log2_of(r.s), d * (double)z.inv_t);
+    if (far < -0.125) return (float)far;
+    const double e = pow2_any(d, z.c), v = fmax(r.s - e, 0.0) / (r.s + e), q = v * v;
+    return (float)(0.0 - 2.0 * v * fma(fma(fma(fma(q, 1.0 / 9, 1.0 / 7), q, 1.0 / 5), q, 1.0 / 3), q, 1.0));
 }
 
 // -- the choice of an entry --------------------------------------------------

@@ -166,6 +166,86 @@ def test_residual_at_nearly_infinite_temperatures(dr, kind, inv_t, iq, times):
         assert ((got[2][:, 0].double() + math.log(2000)).abs() <= ref.logp_bound(math.log(2000))).all()
 
 
+# -- tokens that are all but certain ----------------------------------------------
+
+def near_bound(v):
+    """One rounding; powers within 2^-39.7, farther than 1/8 from 0 the logarithm
+    within 2^-39, 2^-38.5 in all and 8 times that relative to it; and nearer the sums,
+    of at most 64 additions to the longest of these rows, 2^-53 each."""
+    return ref.U * abs(v) + 2.0 ** -35 * abs(v) + 2.0 ** -46
+
+
+def certain_rows(kind, V):
+    """Rows with one token left, or with one that takes almost all, and that token."""
+    g = torch.Generator().manual_seed(V)
+    tops = [0.0, 1.5, -7.25, 80.0, -200.0, 640.0, -640.0, 2000.0, -2000.0, 2.0 ** -46, -2.0 ** -46, 0.3, 5e-7]
+    x, at = torch.full((52, V), -INF), torch.randint(0, V, (52,), generator=g)
+    at[:4] = torch.tensor([0, V - 1, 2047, 2048]).clamp(max=V - 1)
+    for i in range(52):
+        top = tops[i % 13]
+        if i >= 13:
+            # others below it, few or many, until it is no longer the likeliest
+            gap = [40.0, 30.0, 24.0, 20.0, 16.0, 12.0, 9.0, 7.0, 5.0, 3.0, 2.5, 2.0, 1.0][(i * 5 + i // 13) % 13]
+            n = [1, 3, 200, V][i // 13]
+            if n == V:
+                x[i] = top - gap - 2.0 * torch.rand(V, generator=g)
+            else:
+                x[i, torch.randint(0, V, (n,), generator=g)] = top - gap
+        x[i, at[i]] = top
+    return x.to(KINDS[kind]), at
+
+
+@pytest.mark.parametrize("kind,V,copies", [(k, V, (c + 7) // 8) for k, V, c in WAYS] + [(k, V, 1) for k in KINDS for V in (3, 500, 900)])
+@pytest.mark.parametrize("inv_t", [1.0, 0.37, 3.0])
+def test_log_probabilities_near_0(dr, kind, V, copies, inv_t):
+    """0 where nothing else is left, never above it, and near it as exact as a
+    float is."""
+    x, at = certain_rows(kind, V)
+    u = torch.full((52 * copies,), 0.5, device=DEV)
+    token, logp = dr.sf_token_sample(x.to(DEV).repeat(copies, 1), u, inv_temperature=inv_t)
+    token, logp = token.view(copies, 52), logp.view(copies, 52)
+    assert (token >= 0).all() and (token[:, :13] == at[:13].to(DEV)).all()
+    assert (logp <= 0).all() and not logp[:, :13].any(), logp[0, :13].tolist()
+    for i in range(13, 52):
+        p = ref.softmax(f64(x[i]), inv_t)
+        for t, lp in set(zip(token[:, i].tolist(), logp[:, i].tolist())):
+            v = ref.log_p(p[t])
+            assert abs(lp - v) <= near_bound(v), (i, lp, v)
+
+
+@pytest.mark.parametrize("kind,V,times", [("f32", 900, 1), ("bf16", 900, 1), ("f16", 9000, 1), ("f32", 9000, 4), ("bf16", 9000, 4),
+                                          ("bf16", 40000, 20), ("f16", 40000, 40)])
+@pytest.mark.parametrize("lookup", [False, True])
+def test_verified_log_probabilities_near_0(dr, kind, V, times, lookup):
+    """The same of drafts that are accepted, and of the last token."""
+    x, at = certain_rows(kind, V)
+    # sequences of three drafts, each the token that takes almost all
+    start, draft = torch.arange(0, 40, 3, device=DEV), at.view(13, 4)[:, :3].reshape(-1).to(DEV)
+    drafts = None if lookup else x.view(13, 4, V)[:, :3].reshape(39, V).to(DEV)
+    u = torch.full((52,), 0.25, device=DEV)
+    acc, token, logp = repeated(dr, x.to(DEV), drafts, draft, start, u, times)
+    for b in range(13):
+        for k in range(int(acc[0, b]) + 1):
+            i = 4 * b + k
+            p = ref.softmax(f64(x[i]), 1.0)
+            for t, lp in set(zip(token[:, i].tolist(), logp[:, i].tolist())):
+                v = ref.log_p(p[t])
+                assert t >= 0 and lp <= 0 and abs(lp - v) <= near_bound(v), (i, t, lp, v)
+                assert i >= 13 or lp == 0
+    assert (acc[0] > 0).sum() > 5 and (acc == acc[:1]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_log_probability_above_0(dr, kind):
+    """One token left, of any size."""
+    N, V = 4000, 700
+    g = torch.Generator().manual_seed(9)
+    x, at = torch.full((N, V), -INF), torch.randint(0, V, (N,), generator=g)
+    x[torch.arange(N), at] = torch.randn(N, generator=g) * torch.logspace(-18, 3, N)
+    token, logp = dr.sf_token_sample(x.to(DEV, KINDS[kind]), torch.rand(N, generator=g).to(DEV))
+    assert (token == at.to(DEV)).all() and not logp.any()
+
+
 def test_powers_from_a_table_are_the_same_numbers(dr):
     """Rows of many bfloat16 numbers near 0, whose powers are all but 1, and of one
     such number alone: the same bits as of a few rows."""
