@@ -455,12 +455,11 @@ __device__ __forceinline__ void draw_last(const VerifyArg<DT>& a, int64_t b, con
         double total = 0.0;
         for (int g = lane; g < a.z.nseg; g += 64) total += weight(g);
         total = wave_sum_f64(total);
-        if (total >= kLeastResidual * v.p.s) {
-            const double target = (double)u * total;
-            t = pick_entry_group<DT>(xp, value, pick_weight(weight, a.z.nseg, target, lane), a.z.V, target, shared);
-        }
+        // (2^-24 of the row at least: what refused the draft is below 1, and no less than its share)
+        const double target = (double)u * total;
+        t = pick_entry_group<DT>(xp, value, pick_weight(weight, a.z.nseg, target, lane), a.z.V, target, shared);
     }
-    if (t < 0) {  // from p, also where rounding leaves nothing else
+    if (t < 0) {  // from p, also where next to nothing of it is left
         draw_token<DT, true>(xp, seg, v.p, u, a.z, &shared, a.token + o.at, a.logp + o.at);
     } else if (threadIdx.x == 0) {
         a.token[o.at] = t;

@@ -67,3 +67,15 @@ def test_verified_tokens_are_the_targets(lookup):
     residual = np.maximum(p - q, 0)
     got = q * accept + (1 - (q * accept).sum()) * residual / residual.sum()
     np.testing.assert_allclose(got, p, atol=1e-15)
+
+
+@pytest.mark.parametrize("share,left", [(2.0 ** -29, True), (1.01 * 2.0 ** -30, True), (0.99 * 2.0 ** -30, False), (2.0 ** -33, False)])
+def test_verify_next_to_nothing_by_hand(share, left):
+    """A refused draft's token comes from what p has more of than q, here token 3
+    alone, down to a share of 2^-30; below that from p."""
+    p = np.log([0.5, 0.25, 0.25, share, 1e-100])
+    q = np.log([0.5, 0.25, 0.25, 1e-100, share])
+    for u, t in ((0.3, 0), (0.6, 1), (0.9, 2)):
+        assert ref.verify([p, p], [q], [4], [0.5, u], 1.0, 1.0)[:2] == (0, {3 if left else t})
+    # without the draft's distribution only its own share is taken from p
+    assert ref.verify([p, p], None, [4], [0.5, 0.6], 1.0, 1.0)[:2] == (0, {1})

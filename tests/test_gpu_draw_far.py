@@ -260,3 +260,75 @@ def test_powers_from_a_table_are_the_same_numbers(dr):
     one = dr.sf_token_sample(x, u)
     many = dr.sf_token_sample(x.repeat(20, 1), u.repeat(20))
     assert (many[0].view(20, N) == one[0]).all() and (many[1].view(20, N) == one[1]).all()
+
+
+# -- what p leaves of q, or next to nothing -----------------------------------------
+
+def swapped(V, share, kind="f32"):
+    """A target's and a draft's row that are the same but for two unlikely tokens, j
+    and d, which change places: the draft has d where the target has j, and ``share``
+    of its distribution is left.  Nothing else is: p = q there, bit for bit."""
+    j, d = V // 3, V // 2
+    p = torch.zeros(1, V, dtype=torch.float64)
+    p[0, j], p[0, d] = math.log(share * (V - 2) / (1 - share)), -80.0
+    q = p.clone()
+    q[0, j], q[0, d] = p[0, d], p[0, j]
+    target = torch.cat([p, torch.zeros(1, V)]).to(KINDS[kind])
+    return target.to(DEV), q.to(KINDS[kind]).to(DEV), j, d
+
+
+@pytest.mark.parametrize("V,times", [(1000, 1), (1000, 1500), (9000, 1), (9000, 300), (70001, 1), (70001, 40)])
+@pytest.mark.parametrize("share", [2.0 ** -20, 2.0 ** -28, 2.0 ** -29, 1.02 * 2.0 ** -30, 0.98 * 2.0 ** -30, 2.0 ** -32, 2.0 ** -50])
+def test_residual_of_next_to_nothing(dr, V, times, share):
+    """A refused draft's token is drawn from what is left down to 2^-30, below that
+    from p."""
+    target, drafts, j, d = swapped(V, share)
+    for v in (0.25, 0.9):
+        u = [0.5, float(np.float32(v))]
+        k, near, logp, _ = ref.verify(f64(target), f64(drafts), [d], u, 1.0, 1.0)
+        assert k == 0 and (near == {j} if share > ref.LEAST else j not in near)
+        got = repeated(dr, target, drafts, torch.tensor([d], device=DEV), torch.tensor([0, 1], device=DEV), torch.tensor(u, device=DEV),
+                       times)
+        t = int(got[1][0, 0])
+        assert not got[0].any() and t in near and (got[1] == torch.tensor([t, -1], device=DEV)).all()
+        assert ((got[2][:, 0].double() - logp(t)).abs() <= ref.logp_bound(logp(t))).all()
+
+
+@pytest.mark.parametrize("kind,V,times", [("bf16", 9000, 1), ("bf16", 9000, 300), ("bf16", 9000, 1700), ("f16", 9000, 300)])
+@pytest.mark.parametrize("share", [2.0 ** -16, 2.0 ** -28, 2.0 ** -32])
+def test_residual_of_next_to_nothing_in_16_bits(dr, kind, V, times, share):
+    """The same where logits are coarse, among them the sums by table."""
+    target, drafts, j, d = swapped(V, share, kind)
+    p, q = ref.softmax(f64(target)[0], 1.0), ref.softmax(f64(drafts)[0], 1.0)
+    left = float(np.maximum(p - q, 0).sum())
+    assert (left > 1.5 * ref.LEAST) == (share > ref.LEAST) and abs(left / ref.LEAST - 1) > 0.5
+    u = torch.tensor([0.5, 0.25], device=DEV)
+    got = repeated(dr, target, drafts, torch.tensor([d], device=DEV), torch.tensor([0, 1], device=DEV), u, times)
+    want = j if share > ref.LEAST else ref.sample(f64(target)[0], 0.25, 1.0)[1]
+    t = int(got[1][0, 0])
+    assert not got[0].any() and (t == want if share > ref.LEAST else t in want)
+    assert (got[1] == torch.tensor([t, -1], device=DEV)).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("times", [1, 400])
+def test_certain_draft_that_takes_almost_all(dr, kind, times):
+    """A draft without logits that is refused although it has all but 2^-23 or so of
+    the probability: the token is another."""
+    V, d = 9000, 5000
+    target = torch.full((2, V), -4.0)
+    target[0, d] = -4.0 + math.log(V) + 23 * math.log(2.0)
+    target[0, :40] = -INF
+    target = target.to(DEV, KINDS[kind])
+    if kind == "bf16":
+        target[0, d] = 21.125   # (a step of 1/8)
+    p = ref.softmax(f64(target)[0], 1.0)
+    assert 2.0 ** -24 < 1.0 - float(p[d]) < 2.0 ** -22
+    for v in (0.0, 0.6):
+        u = [1 - 2.0 ** -24, float(np.float32(v))]
+        k, near, logp, _ = ref.verify(f64(target), None, [d], u, 1.0, 1.0)
+        assert k == 0 and d not in near
+        got = repeated(dr, target, None, torch.tensor([d], device=DEV), torch.tensor([0, 1], device=DEV), torch.tensor(u, device=DEV),
+                       times)
+        t = int(got[1][0, 0])
+        assert not got[0].any() and t in near and (got[1][:, 0] == t).all()
