@@ -332,3 +332,43 @@ def test_certain_draft_that_takes_almost_all(dr, kind, times):
                        times)
         t = int(got[1][0, 0])
         assert not got[0].any() and t in near and (got[1][:, 0] == t).all()
+
+
+# -- memory -------------------------------------------------------------------------
+
+def test_dropout_at_large_offsets(dr):
+    """Rows that begin beyond 2^31 entries of their buffer, in place: every entry
+    that the mask keeps is there."""
+    C, N, stride = 1031, 5, 600000000
+    buf = torch.empty(stride * (N - 1) + C, dtype=torch.bfloat16, device=DEV)
+    x = buf.as_strided((N, C), (stride, 1))
+    g = torch.Generator().manual_seed(3)
+    values = (torch.randn(N, C, generator=g) * 3.0).to(torch.bfloat16)
+    values[values == 0] = 1.0
+    x.copy_(values)
+    keep = ref.kept(1, 1, 0, 0.5, np.arange(N * C).reshape(N, C))
+    dr.sf_dropout(x, 0.5, torch.tensor([1, 1], device=DEV), out=x)
+    want, bound = ref.dropout(f64(values), keep, 0.5, None, "bf16")
+    assert (np.abs(f64(x) - want) <= bound).all()
+    np.testing.assert_array_equal(f64(x) != 0, keep)
+
+
+@pytest.mark.parametrize("lookup", [False, True])
+@pytest.mark.parametrize("V,B", [(300, 2), (9000, 60), (40000, 200)])
+def test_starts_outside_touch_nothing_else(dr, lookup, V, B):
+    """Starts that the contract rules out: what lies around every output and the
+    workspace stays."""
+    D, g = 3 * B, torch.Generator().manual_seed(1)
+    for kind in ("bf16", "f16"):
+        target, drafts = (torch.randn(n, V, generator=g).to(DEV, KINDS[kind]) for n in (D + B, D))
+        draft, u = torch.randint(0, V, (D,), generator=g).to(DEV), torch.rand(D + B, generator=g).to(DEV)
+        need = dr.sf_draft_verify_workspace(KINDS[kind], D, B, V)
+        for bad in ([-5, 3, 6], [0, 900000, 6], [0, 1 << 62, -(1 << 62)], [D, 0, D], [3, 3, 3], [D, D, 0]):
+            start = torch.tensor((bad * B)[:B + 1], device=DEV)
+            guards = [torch.full((n + 128,), 7, dtype=t, device=DEV) for n, t in
+                      ((B, torch.int64), (D + B, torch.int64), (D + B, torch.float32), (need, torch.uint8))]
+            acc, token, logp, space = (t[64:-64] for t in guards)
+            dr.sf_draft_verify(target, None if lookup else drafts, draft, start, u, out_accepted=acc, out_token=token, out_logp=logp,
+                               workspace=space)
+            for t in guards:
+                assert (t[:64] == 7).all() and (t[-64:] == 7).all()
