@@ -13,10 +13,13 @@
  * or on what was drawn before.  So a backward pass makes a mask again instead of
  * storing it, a rank with a part of a tensor draws the part of its mask, and a
  * replayed graph draws anew when the step in device memory has been raised.
- * Tokens are decided in 64-bit arithmetic: they are those of the definition,
- * whatever the sizes, the strides and the split of the work, but where a uniform
- * number lies within about 2^-38 of a border between two.  Probabilities below
- * 2^-700 of a row's largest may count as 0.
+ * Tokens are decided in 64-bit arithmetic, by powers within 2^-39.7: they are
+ * those of the definition, whatever the sizes, the strides and the split of the
+ * work, but where a uniform number lies within about 2^-38 of a border between
+ * two.  (A draft's acceptance: within 2^-38 of p_d relative to it.  A token from
+ * what a target leaves of a draft's distribution: within 2^-37 / R, where R is the
+ * share that is left, 2^-30 at least.)  Probabilities below 2^-700 of a row's
+ * largest may count as 0.
  *
  * Conventions are those of stagefrontier.h: device pointers, asynchronous on
  * the caller's stream, buffers and workspaces allocated by the caller, no
@@ -122,7 +125,12 @@ int sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t C, int64_t x_str
  * Logits of -inf are never drawn.  A row of nothing else has token -1 and
  * logp -inf; one that holds +inf or NaN has token -1 and logp NaN.  Of the
  * largest logits the first is drawn by a uniform number of 0 at a temperature
- * near 0.  Returns SF_OK, SF_EINVAL or SF_EHIP.
+ * near 0.
+ *
+ * A uniform number is as fine as it is given.  By those of sf_uniform a token
+ * comes in a multiple of 2^-24 of the draws, within 2^-24 of p_token (one less
+ * probable than that in 2^-24 of them or never), while its logp is that of
+ * p_token.  Returns SF_OK, SF_EINVAL or SF_EHIP.
  */
 int sf_token_sample(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t row_stride,
                     const float* uniform, float inv_temperature, int64_t* out_token,
@@ -150,7 +158,8 @@ int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V);
  * Without draft_logits every draft is taken as certain (looked up, or the
  * likeliest of a model): q_d = 1.
  * The tokens so emitted are distributed as if drawn from p one after the other,
- * where drafts were drawn from q.
+ * where drafts were drawn from q, but for the steps of the uniform numbers (see
+ * sf_token_sample).
  *
  *   target_logits    [D + B][target_stride], the first V entries of each row
  *                    used.  Aligned to the element size.
@@ -178,8 +187,9 @@ int64_t sf_token_sample_workspace(int32_t dtype, int64_t N, int64_t V);
  * Rows behind the draft that is refused may be read or not.
  *
  * A sequence ends without a token drawn (-1) at a row that is reached where the
- * uniform number lies outside [0, 1) (logp 0), the target's logits are all -inf
- * (logp -inf), or they or the draft's hold +inf or NaN (logp NaN).  A draft's
+ * uniform number, or that of the sequence's last row where a token is to be drawn,
+ * lies outside [0, 1) (logp 0), the target's logits are all -inf (logp -inf), or
+ * they or the draft's hold +inf or NaN (logp NaN).  A draft's
  * row of -inf alone has q = 0.  Returns SF_OK, SF_EINVAL or SF_EHIP.
  */
 int sf_draft_verify(const void* target_logits, const void* draft_logits, int32_t dtype, int64_t D,

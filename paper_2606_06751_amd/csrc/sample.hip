@@ -10,7 +10,7 @@
 //
 // What bounds it: 18 instructions an entry, 14 of them of 64 bits, which issue at
 // the rate of 32-bit ones but draw power enough to lower the clock (2.1 GHz).  302
-// million bfloat16 entries take 196 us at 81% of the issue slots, 115 us by a table
+// million bfloat16 entries take 192 us at 81% of the issue slots, 115 us by a table
 // of powers in LDS, and HBM alone 85 us.
 
 #include "sf_draw.h"
@@ -53,8 +53,8 @@ __device__ __forceinline__ void draw_token(const typename Elem<DT>::T* row, cons
 }
 
 // Rows of one segment, LIVE vectors a lane: a wave each, which keeps the powers
-// from the sum to the choice, with the next row on its way.  (16000 x 515 f16: 14.4
-// us, in place of 48 by segments of 2048 places and a second read; 372 instructions a
+// from the sum to the choice, with the next row on its way.  (16000 x 515 f16: 14.5
+// us, in place of 48 by segments of 2048 places and a second read; 370 instructions a
 // row are 10 us of it, 144 of them the powers of 512 entries.)
 template <int DT, int LIVE>
 __global__ __launch_bounds__(kRowsWG) void k_token_short(const typename Elem<DT>::T* __restrict__ logits, int64_t N,
@@ -223,9 +223,9 @@ __global__ __launch_bounds__(kTableWG) void k_row_table(const __bf16* __restrict
 }
 
 // Whether rows' sums go by a table: many of bfloat16, at a temperature not too far
-// from 1.  (us by the kernels without / with it: 128 rows of 131072, 8192 segments,
-// 19.1 / 15.2; 1000 rows 84 / 55; 32 x 4 drafts of 65536 22 / 26;
-// 128 x 4 drafts of 65536 49 / 43; 256 x 4 drafts of 131072 224 / 147.)
+// from 1.  (us of the sums without / with it: 128 rows of 131072, 8192 segments, 14.0 /
+// 12.0; 1000 rows 82 / 52; 64 x 4 drafts of 65536, 576 rows, 27.4 / 20.4; 128 x 4 of
+// 65536 50 / 32; 256 x 4 of 131072 192 / 115.)
 static inline bool by_table(int32_t dtype, int64_t rows, const RowArg& z)
 {
     return dtype == SF_BF16 && rows * z.nseg >= kTableSegments && rows * z.nseg < (int64_t)1 << 30 && table_begin(z.c) >= 0;
@@ -824,7 +824,11 @@ static int verify(const void* target, const void* drafts, int64_t D, int64_t B, 
         // 5 us.  (f16, us with the first 1 / 2 / 3 rows / all at once: 256 x 4 drafts of
         // 131072, 79% accepted, 230 / 224 / 233 / 245; 128 x 4 125 / 125 / 130 / 133; 64 x 4
         // 78 / 76 / 76 / 77; 200 x 9 without logits of 50001, 12% accepted, 36 / 40 / 38 / 56.
-        // By a table, all at once, 256 x 4 bf16 take 140, and 156 in two rounds.)
+        // By a table, all at once, 256 x 4 bf16 take 140, and 156 in two rounds.)  How many
+        // will be accepted is not known to the host, and rounds pay where it is few: us in
+        // rounds / all at once under replay, f16, 256 x 4 drafts of 131072, 15% accepted 191 /
+        // 259, 38% 200 / 246, 58% 208 / 239, 86% 222 / 221, all 221 / 203; 200 x 0 to 9 without
+        // logits of 50001, 2% 34 / 49, 14% 44 / 54, 38% 51 / 47, 68% 58 / 48, all 56 / 45.
         int64_t k0 = 0, k1 = drafts ? 1 + D / B / 3 : 1, all = (int64_t)1 << 31;
         const int64_t kinds = drafts ? 2 : 1, rest = kinds * (D / B - k1 + 1);
         void* first[] = {(void*)&a, (void*)&k0, (void*)&k1, (void*)&outcomes, (void*)&sums};
